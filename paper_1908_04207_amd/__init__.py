@@ -6,7 +6,7 @@ first use so that `python -m paper_1908_04207_amd.build` can run before the libr
 """
 import importlib
 
-__all__ = ["binding", "build"]
+__all__ = ["binding", "build", "model_ops"]
 
 
 def __getattr__(name):

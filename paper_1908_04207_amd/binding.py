@@ -41,6 +41,9 @@ EXPORTS = (
     "eager_stats_attach", "eager_get_valid",
     "eager_set_valid", "eager_set_launch", "eager_calib_copy", "eager_calib_read",
     "eager_calib_mix",
+    "eager_qk_norm_rope", "eager_qk_norm_rope_workspace_bytes", "eager_qk_norm_rope_backward",
+    "eager_attention", "eager_attention_workspace_bytes", "eager_attention_backward",
+    "eager_cross_entropy", "eager_cross_entropy_workspace_bytes", "eager_cross_entropy_backward",
 )
 
 
@@ -63,6 +66,25 @@ class Plan(ctypes.Structure):
 class Opt(ctypes.Structure):
     _fields_ = [("params", ctypes.c_void_p), ("momentum", ctypes.c_void_p),
                 ("lr", ctypes.c_float), ("mu", ctypes.c_float)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class Packed(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("sequences", ctypes.c_int32), ("cu_seqlens", ctypes.c_void_p)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("cos_table", ctypes.c_void_p), ("sin_table", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("table_rows", ctypes.c_int64)]
+
+
+class Projection(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64)]
 
 
 def _load() -> ctypes.CDLL:
@@ -123,6 +145,16 @@ def _load() -> ctypes.CDLL:
     lib.eager_calib_read.argtypes = [vp, i64, vp, vp]
     lib.eager_calib_mix.argtypes = [ctypes.POINTER(vp), i32, u64, ctypes.POINTER(vp), i32, i64, i32,
                                     vp, vp]
+    H, Pk, Rt, Pj, f32 = (*(ctypes.POINTER(t) for t in (Heads, Packed, Rotation, Projection)), ctypes.c_float)
+    lib.eager_qk_norm_rope.argtypes = [i32, Pk, H, H, vp, vp, Rt, f32, H, H, vp]
+    lib.eager_qk_norm_rope_workspace_bytes.argtypes = [i32, Pk, ctypes.POINTER(i64)]
+    lib.eager_qk_norm_rope_backward.argtypes = [i32, Pk, H, H, H, H, vp, vp, Rt, f32, H, H, vp, vp, vp, i64, vp]
+    lib.eager_attention.argtypes = [i32, Pk, H, H, H, f32, H, vp, vp]
+    lib.eager_attention_workspace_bytes.argtypes = [i32, Pk, ctypes.POINTER(i64)]
+    lib.eager_attention_backward.argtypes = [i32, Pk, H, H, H, H, vp, H, f32, H, H, H, vp, i64, vp]
+    lib.eager_cross_entropy.argtypes = [i32, Pj, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.eager_cross_entropy_workspace_bytes.argtypes = [i32, Pj, i32, ctypes.POINTER(i64)]
+    lib.eager_cross_entropy_backward.argtypes = [i32, Pj, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
     return lib
 
 
@@ -506,3 +538,83 @@ def eager_calib_mix(read, write, n_vec: int, read_half_mask: int = 0, waves_per_
                              _ptr(sink), _stream(stream))
     if st != OK:
         raise EagerError(st, f"eager_calib_mix: {status_string(st)}")
+
+
+# ------------------------------------------------------------- operators of a transformer step
+
+def _status(st: int, what: str) -> None:
+    if st != OK:
+        raise EagerError(st, f"{what}: {status_string(st)}")
+
+
+def heads(x) -> Heads:
+    """The view of a tensor [tokens, heads, head_dim] whose last axis is contiguous."""
+    if x.dim() != 3 or (x.shape[2] > 1 and x.stride(2) != 1):
+        raise EagerError(EINVAL, f"expected [tokens, heads, head_dim] with contiguous heads, got {tuple(x.shape)} "
+                                 f"with strides {x.stride()}")
+    return Heads(x.data_ptr(), x.stride(0), x.stride(1))
+
+
+def packed(tokens: int, q_heads: int, kv_heads: int, head_dim: int, cu_seqlens=None) -> Packed:
+    """Shape of a packed batch; cu_seqlens: device tensor of sequences + 1 int32 values."""
+    if cu_seqlens is None:
+        return Packed(tokens, q_heads, kv_heads, head_dim, 0, None)
+    return Packed(tokens, q_heads, kv_heads, head_dim, cu_seqlens.numel() - 1, cu_seqlens.data_ptr())
+
+
+def _workspace_bytes(fn, what, *args) -> int:
+    n = ctypes.c_int64()
+    _status(fn(*args, ctypes.byref(n)), what)
+    return n.value
+
+
+def eager_qk_norm_rope(dtype: int, shape: Packed, q: Heads, k: Heads, wq, wk, rotation: Rotation, eps: float,
+                       q_out: Heads, k_out: Heads, stream=None) -> None:
+    _status(lib.eager_qk_norm_rope(dtype, shape, q, k, _ptr(wq), _ptr(wk), rotation, eps, q_out, k_out,
+                                   _stream(stream)), "eager_qk_norm_rope")
+
+
+def eager_qk_norm_rope_workspace_bytes(dtype: int, shape: Packed) -> int:
+    return _workspace_bytes(lib.eager_qk_norm_rope_workspace_bytes, "eager_qk_norm_rope_workspace_bytes", dtype, shape)
+
+
+def eager_qk_norm_rope_backward(dtype: int, shape: Packed, dq_out: Heads, dk_out: Heads, q: Heads, k: Heads, wq, wk,
+                                rotation: Rotation, eps: float, dq: Heads, dk: Heads, dwq, dwk, workspace,
+                                workspace_bytes: int, stream=None) -> None:
+    _status(lib.eager_qk_norm_rope_backward(dtype, shape, dq_out, dk_out, q, k, _ptr(wq), _ptr(wk), rotation, eps,
+                                            dq, dk, _ptr(dwq), _ptr(dwk), _ptr(workspace), workspace_bytes,
+                                            _stream(stream)), "eager_qk_norm_rope_backward")
+
+
+def eager_attention(dtype: int, shape: Packed, q: Heads, k: Heads, v: Heads, scale: float, out: Heads, lse,
+                    stream=None) -> None:
+    _status(lib.eager_attention(dtype, shape, q, k, v, scale, out, _ptr(lse), _stream(stream)), "eager_attention")
+
+
+def eager_attention_workspace_bytes(dtype: int, shape: Packed) -> int:
+    return _workspace_bytes(lib.eager_attention_workspace_bytes, "eager_attention_workspace_bytes", dtype, shape)
+
+
+def eager_attention_backward(dtype: int, shape: Packed, q: Heads, k: Heads, v: Heads, out: Heads, lse, dout: Heads,
+                             scale: float, dq: Heads, dk: Heads, dv: Heads, workspace, workspace_bytes: int,
+                             stream=None) -> None:
+    _status(lib.eager_attention_backward(dtype, shape, q, k, v, out, _ptr(lse), dout, scale, dq, dk, dv,
+                                         _ptr(workspace), workspace_bytes, _stream(stream)), "eager_attention_backward")
+
+
+def eager_cross_entropy(dtype: int, shape: Projection, x, w, target, loss, lse, workspace, workspace_bytes: int,
+                        stream=None) -> None:
+    _status(lib.eager_cross_entropy(dtype, shape, _ptr(x), _ptr(w), _ptr(target), _ptr(loss), _ptr(lse),
+                                    _ptr(workspace), workspace_bytes, _stream(stream)), "eager_cross_entropy")
+
+
+def eager_cross_entropy_workspace_bytes(dtype: int, shape: Projection, backward: bool) -> int:
+    return _workspace_bytes(lib.eager_cross_entropy_workspace_bytes, "eager_cross_entropy_workspace_bytes", dtype,
+                            shape, int(backward))
+
+
+def eager_cross_entropy_backward(dtype: int, shape: Projection, x, w, target, lse, dloss, dx, dw, workspace,
+                                 workspace_bytes: int, stream=None) -> None:
+    _status(lib.eager_cross_entropy_backward(dtype, shape, _ptr(x), _ptr(w), _ptr(target), _ptr(lse), _ptr(dloss),
+                                             _ptr(dx), _ptr(dw), _ptr(workspace), workspace_bytes, _stream(stream)),
+            "eager_cross_entropy_backward")

@@ -29,7 +29,8 @@ SOURCES = ["eager_round_kernels.hip", "eager_chunk_f32.hip", "eager_chunk_f32_st
            "eager_chunk_bf16_stats.hip", "eager_chunk_f32_fast.hip", "eager_chunk_f32_fast_stats.hip",
            "eager_chunk_bf16_fast.hip", "eager_chunk_bf16_fast_stats.hip", "eager_short_f32.hip", "eager_short_f32_fast.hip",
            "eager_short_bf16.hip", "eager_short_bf16_fast.hip", "eager_aux_kernels.hip", "eager_static_kernels.hip",
-           "eager_calib_kernels.hip", "eager_api.cpp"]
+           "eager_calib_kernels.hip", "eager_api.cpp", "eager_norm_rope.hip", "eager_attention.hip",
+           "eager_attention_backward.hip", "eager_cross_entropy.hip", "eager_model_api.cpp"]
 
 # -ffp-contract=off: the fixed-order mode defines every rounding; fused multiply-adds are
 # written out where they are meant.  Packed fp32 instructions are switched off: a feature of

@@ -1,0 +1,128 @@
+// Causal attention over packed sequences, forward.
+//
+//   s_ij = scale <q_i, k_j>,  m_i = max s_i,  l_i = sum exp(s_ij - m_i),  out_i = sum exp(s_ij - m_i) v_j / l_i
+//
+// One pass over the keys with the running maximum and sum of every row.  The products are formed
+// transposed, S^T = K Q^T and O^T = V^T P^T: a lane then holds scores of one row only, so maximum
+// and sum are taken in registers (one exchange between the halves of a wavefront), the rescaling
+// of O is one factor a lane, and P^T is the second product's operand as it stands.
+#include "eager_packed.h"
+
+namespace eager {
+namespace {
+
+constexpr int kRows = 128;           // query rows of a workgroup: 32 a wavefront
+constexpr int kKeys = 64;            // keys of a tile
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void attention_kernel(const AttentionArgs a)
+{
+    constexpr int Chunks = DP * sizeof(T) / 16, TileBytes = kKeys * Chunks * 16, Steps = DP / 16;
+    __shared__ __align__(1024) char tiles[2][2][TileBytes];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int head = blockIdx.x % a.q_heads;
+    const Tile t = find_tile<kRows>(a.cu, a.sequences, static_cast<int>(a.tokens),
+                                    (gridDim.x - 1 - blockIdx.x) / a.q_heads);
+    if (t.first >= t.end) return;
+    if (t.segment == 0 || t.segment == a.sequences + 1) {
+        clear_rows<T, kRows>(a.out, head, t.first, t.end, a.dim);
+        for (int i = threadIdx.x; i < min(kRows, t.end - t.first); i += 256)
+            a.lse[head * a.tokens + t.first + i] = -__builtin_inff();
+        return;
+    }
+    const int kv_head = head / (a.q_heads / a.kv_heads);
+    const int wave_row = t.first + 32 * wave, row = wave_row + (lane & 31);
+    const T *q_row = static_cast<const T *>(a.q.data) + static_cast<long long>(row) * a.q.row + head * a.q.head;
+    typename Operand<T>::frag q[Steps];
+#pragma unroll
+    for (int s = 0; s < Steps; ++s) q[s] = row_operand(q_row, s, lane, a.dim, row < t.end);
+
+    const char *k_base = reinterpret_cast<const char *>(static_cast<const T *>(a.k.data) + kv_head * a.k.head);
+    const char *v_base = reinterpret_cast<const char *>(static_cast<const T *>(a.v.data) + kv_head * a.v.head);
+    const long long k_stride = a.k.row * sizeof(T), v_stride = a.v.row * sizeof(T);
+    const int chunks = a.dim * sizeof(T) / 16;
+    auto stage = [&](int key0, int buf) {
+        stage_rows<kKeys, Chunks, 4>(tiles[buf][0], k_base + key0 * k_stride, k_stride, t.end - key0, chunks, wave, lane);
+        stage_rows<kKeys, Chunks, 4>(tiles[buf][1], v_base + key0 * v_stride, v_stride, t.end - key0, chunks, wave, lane);
+    };
+
+    const float c = a.scale * kLog2e;
+    const int last = min(t.end, t.first + kRows);       // no key from here on is seen
+    f32x16 o[DP / 32] = {};
+    float top = -__builtin_inff(), sum = 0.0f;
+    stage(t.begin, 0);
+    for (int key0 = t.begin, buf = 0; key0 < last; key0 += kKeys, buf ^= 1) {
+        wait_loads();
+        __syncthreads();
+        if (key0 + kKeys < last) stage(key0 + kKeys, buf ^ 1);
+        if (key0 >= wave_row + 32) continue;            // every key is later than the wavefront's rows
+        f32x16 s[2] = {};
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < Steps; ++i)
+                s[b] = mma(read_rows<Chunks>(tiles[buf][0], 32 * b, i, lane, static_cast<T *>(nullptr)), q[i], s[b]);
+        if (key0 + kKeys - 1 > wave_row) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (key0 + 32 * b + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > row) s[b][i] = -__builtin_inff();
+        }
+        float best = top;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) best = fmaxf(best, fmaxf(s[0][i], s[1][i]));
+        best = fmaxf(best, __shfl_xor(best, 32, 64));
+        const float base = best == -__builtin_inff() ? 0.0f : best * c;
+        const float keep = exp2_fast(fmaf(top, c, -base));
+        top = best;
+        float add = 0.0f;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[b][i] = exp2_fast(fmaf(s[b][i], c, -base));
+                add += s[b][i];
+            }
+        sum = fmaf(sum, keep, add);
+#pragma unroll
+        for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[b][i] *= keep;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const typename Operand<T>::frag p = as_operand<T>(s[b], h);
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d)
+                    o[d] = mma(read_columns<Chunks>(tiles[buf][1], 32 * d, 32 * b + 16 * h, 4, 8, lane,
+                                                    static_cast<T *>(nullptr)), p, o[d]);
+            }
+    }
+    sum += __shfl_xor(sum, 32, 64);
+    if (row < t.end) {
+        T *out = static_cast<T *>(a.out.data) + static_cast<long long>(row) * a.out.row + head * a.out.head;
+        store_row<T, DP>(out, o, 1.0f / sum, lane, a.dim);
+        if (lane < 32) a.lse[head * a.tokens + row] = fmaf(log2_fast(sum), kLn2, top * a.scale);
+    }
+}
+
+template <typename T>
+void enqueue(const AttentionArgs &a, hipStream_t stream)
+{
+    const dim3 grid(static_cast<unsigned>(tile_numbers(a.tokens, a.sequences, kRows) * a.q_heads));
+    if (a.dim <= 64) hipLaunchKernelGGL((attention_kernel<T, 64>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((attention_kernel<T, 128>), grid, dim3(256), 0, stream, a);
+}
+
+}  // namespace
+
+hipError_t launch_attention(const AttentionArgs &a, bool bf16, hipStream_t stream)
+{
+    if (bf16) enqueue<__bf16>(a, stream);
+    else enqueue<float>(a, stream);
+    return hipGetLastError();
+}
+
+}  // namespace eager

@@ -1,0 +1,170 @@
+// Matrix instructions and the tiles in shared memory that feed them (gfx950).
+//
+// One 32x32x16 step is the unit: a lane holds 8 elements of each operand, of row (column)
+// lane % 32, at k = 8 * (lane / 32) + 0..7; of the result it holds column lane % 32 and rows
+// 8 * (i / 4) + 4 * (lane / 32) + i % 4, i = 0..15.  bf16 takes one instruction for it.  fp32
+// takes eight of 32x32x2, each with one element of every lane: the order of k inside a step is
+// free as long as both operands agree, so both types share every layout below.
+//
+// Tiles come from global memory straight into shared memory, 16 bytes a lane, through buffer
+// descriptors whose length makes reads beyond an operand's end return zeros.  The shared-memory
+// side of such a load is contiguous over the wavefront, so the exchange of 16-byte chunks that
+// keeps reads free of bank conflicts is applied to the global address.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace eager {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+typedef __attribute__((address_space(3))) char lds_char;
+
+template <typename T> struct Operand;
+template <> struct Operand<__bf16> {
+    typedef bf16x8 frag;
+    typedef bf16x4 quad;
+};
+template <> struct Operand<float> {
+    typedef f32x8 frag;
+    typedef f32x4 quad;
+};
+
+__device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+}
+
+// Four results rounded to the type of an operand or an output (round to nearest even).
+__device__ __forceinline__ bf16x4 to_quad(f32x4 x, __bf16 *) { return __builtin_convertvector(x, bf16x4); }
+__device__ __forceinline__ f32x4 to_quad(f32x4 x, float *) { return x; }
+
+// Rows 8t .. 8t+7 of a lane's results (t = 0, 1) as an operand whose k order is that of the
+// results: k = 16 t + 8 (j / 4) + 4 (lane / 32) + j % 4.
+template <typename T>
+__device__ __forceinline__ typename Operand<T>::frag as_operand(const f32x16 &c, int t)
+{
+    typename Operand<T>::frag f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = static_cast<T>(c[8 * t + j]);
+    return f;
+}
+
+constexpr unsigned kOutside = 0x80000000u;     // an offset no descriptor covers
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *base, unsigned bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, bytes, 0x00020000);
+}
+
+__device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t r, char *lds, unsigned offset)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds), 16, offset, 0, 0, 0);
+}
+
+// What this wavefront has asked for in shared memory is there (its loads from global memory are
+// waited for); a barrier after it says the same of the other wavefronts'.
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
+
+// ---- tiles whose rows are operand rows and hold consecutive k: `Chunks` 16-byte chunks a row.
+// Reads take the same chunk of 32 rows; the exchange spreads 8 (16) consecutive rows over the
+// banks, and the four rows of a transposing read over different pairs of chunks.
+template <int Chunks>
+__device__ __forceinline__ int exchange(int row)
+{
+    if (Chunks >= 16) return ((row & 3) << 2) | ((row >> 2) & 3);
+    return ((row & 2) << 1) | ((row >> 1) & 2) | (row & 1);
+}
+
+// Rows [first, first + Rows) of a matrix at `base` (row `first`) into a tile; rows from rows_left
+// on and chunks from chunks_left on are zeros.  stride: bytes.
+template <int Rows, int Chunks, int Waves>
+__device__ __forceinline__ void stage_rows(char *tile, const char *base, long long stride, int rows_left,
+                                           int chunks_left, int wave, int lane)
+{
+    static_assert(Rows * Chunks % (64 * Waves) == 0, "whole loads");
+    const unsigned bytes = rows_left <= 0 || chunks_left <= 0 ? 0u
+        : static_cast<unsigned>((min(rows_left, Rows) - 1) * stride + min(chunks_left, Chunks) * 16);
+    const __amdgpu_buffer_rsrc_t r = buffer(base, bytes);
+#pragma unroll
+    for (int s = 0; s < Rows * Chunks / 64 / Waves; ++s) {
+        const int piece = s * Waves + wave;
+        const int id = piece * 64 + lane;
+        const int row = id / Chunks, chunk = (id % Chunks) ^ exchange<Chunks>(row);
+        const unsigned at = static_cast<unsigned>(row * static_cast<unsigned>(stride)) + chunk * 16;
+        load_lds16(r, tile + piece * 1024, chunk < chunks_left ? at : kOutside);
+    }
+}
+
+// Operand of 32 rows from `row0` on, k step `step` (16 elements), from such a tile.
+template <int Chunks>
+__device__ __forceinline__ bf16x8 read_rows(const char *tile, int row0, int step, int lane, __bf16 *)
+{
+    const int row = row0 + (lane & 31), chunk = 2 * step + (lane >> 5);
+    return *reinterpret_cast<const bf16x8 *>(tile + row * Chunks * 16 + (chunk ^ exchange<Chunks>(row)) * 16);
+}
+template <int Chunks>
+__device__ __forceinline__ f32x8 read_rows(const char *tile, int row0, int step, int lane, float *)
+{
+    const int row = row0 + (lane & 31), chunk = 4 * step + 2 * (lane >> 5), x = exchange<Chunks>(row);
+    const f32x4 a = *reinterpret_cast<const f32x4 *>(tile + row * Chunks * 16 + (chunk ^ x) * 16);
+    const f32x4 b = *reinterpret_cast<const f32x4 *>(tile + row * Chunks * 16 + ((chunk + 1) ^ x) * 16);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// The transposed operand from such a tile: rows are columns col0 .. col0 + 31 of the tile, k runs
+// over tile rows: j = 0..3 of the lane's half from k0 + k_half * (lane / 32) on, j = 4..7 from
+// k_quad later.  bf16 has a read for it: 16 lanes get 16 columns of 4 rows.
+template <int Chunks, int Shift>
+__device__ __forceinline__ int exchange_of(int row) { return Shift < 0 ? exchange<Chunks>(row) : (row & 3) << Shift; }
+
+template <int Chunks, int Shift = -1>
+__device__ __forceinline__ bf16x8 read_columns(const char *tile, int col0, int k0, int k_half, int k_quad, int lane,
+                                               __bf16 *)
+{
+    const int i = lane & 15;
+    const int chunk = (col0 >> 3) + 2 * ((lane >> 4) & 1) + ((i >> 1) & 1);
+    const int row = k0 + k_half * (lane >> 5) + (i >> 2), later = row + k_quad;
+    const char *a = tile + row * Chunks * 16 + (chunk ^ exchange_of<Chunks, Shift>(row)) * 16 + (i & 1) * 8;
+    const char *b = tile + later * Chunks * 16 + (chunk ^ exchange_of<Chunks, Shift>(later)) * 16 + (i & 1) * 8;
+    const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(a));
+    const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(b));
+    typedef short i16x8 __attribute__((ext_vector_type(8)));
+    const i16x8 z = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(bf16x8, z);
+}
+template <int Chunks, int Shift = -1>
+__device__ __forceinline__ f32x8 read_columns(const char *tile, int col0, int k0, int k_half, int k_quad, int lane,
+                                              float *)
+{
+    const int col = col0 + (lane & 31), first = k0 + k_half * (lane >> 5);
+    f32x8 f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int row = first + (j & 3) + (j >> 2) * k_quad;
+        f[j] = *reinterpret_cast<const float *>(tile + row * Chunks * 16 +
+                                                ((col >> 2) ^ exchange_of<Chunks, Shift>(row)) * 16 + (col & 3) * 4);
+    }
+    return f;
+}
+
+// base-2 exponential and logarithm of the hardware: one unit in the last place for normal results
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+}  // namespace eager

@@ -1,0 +1,267 @@
+"""The operators of a transformer training step on torch tensors.
+
+`binding` marshals the calls of eager_model.h with buffers that the caller owns; the functions
+here check shapes, types and devices, allocate what the caller does not bring (outputs,
+workspaces, through torch's allocator) and call them.  Outputs that are given (gradients of
+weights in a process's gradient arena, parts of one buffer) are written in place.  All calls go to
+the current stream, none of them waits.
+
+    q, k = qk_norm_rope(q, k, wq, wk, cos, sin, positions)
+    out, lse = attention(q, k, v, cu_seqlens)
+    loss, lse = cross_entropy(x, w, target)
+
+each with its `_backward`, and `QKNormRope`, `Attention`, `CrossEntropy` for torch's autograd.
+"""
+from __future__ import annotations
+
+import math
+from typing import Optional
+
+import torch
+
+from . import binding as eb
+
+_DTYPES = {torch.float32: eb.F32, torch.bfloat16: eb.BF16}
+
+
+def _refuse(text: str):
+    raise eb.EagerError(eb.EINVAL, text)
+
+
+def _dtype(*tensors) -> int:
+    first = tensors[0]
+    if first.dtype not in _DTYPES:
+        _refuse(f"unsupported type {first.dtype}: float32 or bfloat16")
+    for t in tensors:
+        if t.dtype != first.dtype or t.device != first.device:
+            _refuse(f"expected {first.dtype} on {first.device}, got {t.dtype} on {t.device}")
+    if not first.is_cuda:
+        _refuse("expected tensors on the GPU")
+    return _DTYPES[first.dtype]
+
+
+def _expect(t, shape, dtype, device, name, contiguous=True):
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or (contiguous and not t.is_contiguous()):
+        _refuse(f"{name}: expected {'contiguous ' if contiguous else ''}{dtype} {tuple(shape)} on {device}, got "
+                f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+
+
+def _workspace(nbytes: int, like):
+    return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=like.device)
+
+
+def _on(t):
+    """Calls go to the current stream of the tensors' device."""
+    return torch.cuda.device(t.device) if t.device.index != torch.cuda.current_device() else _NOTHING
+
+
+class _Nothing:
+    def __enter__(self):
+        return None
+
+    def __exit__(self, *_):
+        return False
+
+
+_NOTHING = _Nothing()
+
+
+# ------------------------------------------------------------------------------ heads
+
+def _rotation(q, cos, sin, positions):
+    T, _, D = q.shape
+    if cos.dim() != 2:
+        _refuse("cos: expected [positions, head_dim / 2]")
+    _expect(cos, (cos.shape[0], D // 2), torch.float32, q.device, "cos")
+    _expect(sin, cos.shape, torch.float32, q.device, "sin")
+    _expect(positions, (T,), torch.int32, q.device, "positions")
+    return eb.Rotation(cos.data_ptr(), sin.data_ptr(), positions.data_ptr(), cos.shape[0])
+
+
+def _heads_shape(q, k, wq, wk):
+    if q.dim() != 3 or k.dim() != 3 or q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2]:
+        _refuse(f"expected q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim], got {tuple(q.shape)}, {tuple(k.shape)}")
+    for w, name in ((wq, "wq"), (wk, "wk")):
+        _expect(w, (q.shape[2],), q.dtype, q.device, name)
+    return eb.packed(q.shape[0], q.shape[1], k.shape[1], q.shape[2])
+
+
+def qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps: float = 1e-6, q_out=None, k_out=None):
+    """RMS norm of every head of q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim]
+    with gains wq, wk [head_dim], then the rotation by `positions` (int32 [tokens]) of the tables
+    cos, sin (fp32 [positions, head_dim / 2]).  q_out, k_out may be q, k."""
+    dtype = _dtype(q, k)
+    shape = _heads_shape(q, k, wq, wk)
+    rotation = _rotation(q, cos, sin, positions)
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+    k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
+    _expect(q_out, q.shape, q.dtype, q.device, "q_out", False)
+    _expect(k_out, k.shape, k.dtype, k.device, "k_out", False)
+    with _on(q):
+        eb.eager_qk_norm_rope(dtype, shape, eb.heads(q), eb.heads(k), wq, wk, rotation, eps, eb.heads(q_out),
+                              eb.heads(k_out))
+    return q_out, k_out
+
+
+def qk_norm_rope_backward(dq_out, dk_out, q, k, wq, wk, cos, sin, positions, eps: float = 1e-6, dq=None, dk=None,
+                          dwq=None, dwk=None):
+    """Gradients dq, dk, dwq, dwk from those of the outputs; dq, dk may be dq_out, dk_out."""
+    dtype = _dtype(q, k, dq_out, dk_out)
+    shape = _heads_shape(q, k, wq, wk)
+    rotation = _rotation(q, cos, sin, positions)
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
+    dwq = torch.empty_like(wq) if dwq is None else dwq
+    dwk = torch.empty_like(wk) if dwk is None else dwk
+    for t, like, name in ((dq_out, q, "dq_out"), (dk_out, k, "dk_out"), (dq, q, "dq"), (dk, k, "dk")):
+        _expect(t, like.shape, q.dtype, q.device, name, False)
+    for t, like, name in ((dwq, wq, "dwq"), (dwk, wk, "dwk")):
+        _expect(t, like.shape, q.dtype, q.device, name)
+    nbytes = eb.eager_qk_norm_rope_workspace_bytes(dtype, shape)
+    with _on(q):
+        eb.eager_qk_norm_rope_backward(dtype, shape, eb.heads(dq_out), eb.heads(dk_out), eb.heads(q), eb.heads(k), wq,
+                                       wk, rotation, eps, eb.heads(dq), eb.heads(dk), dwq, dwk,
+                                       _workspace(nbytes, q), nbytes)
+    return dq, dk, dwq, dwk
+
+
+class QKNormRope(torch.autograd.Function):
+    """q, k = QKNormRope.apply(q, k, wq, wk, cos, sin, positions, eps)"""
+
+    @staticmethod
+    def forward(ctx, q, k, wq, wk, cos, sin, positions, eps):
+        ctx.save_for_backward(q, k, wq, wk, cos, sin, positions)
+        ctx.eps = eps
+        return qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps)
+
+    @staticmethod
+    def backward(ctx, dq_out, dk_out):
+        q, k, wq, wk, cos, sin, positions = ctx.saved_tensors
+        return (*qk_norm_rope_backward(dq_out.contiguous(), dk_out.contiguous(), q, k, wq, wk, cos, sin, positions,
+                                       ctx.eps), None, None, None, None)
+
+
+# ------------------------------------------------------------------------------ attention
+
+def _packed_shape(q, k, v, cu_seqlens):
+    if q.dim() != 3 or k.dim() != 3 or q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2]:
+        _refuse(f"expected q [tokens, q_heads, head_dim], k and v [tokens, kv_heads, head_dim], got {tuple(q.shape)}, {tuple(k.shape)}")
+    _expect(v, k.shape, k.dtype, k.device, "v", False)
+    if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
+        _refuse("cu_seqlens: expected sequences + 1 values")
+    _expect(cu_seqlens, cu_seqlens.shape, torch.int32, q.device, "cu_seqlens")
+    return eb.packed(q.shape[0], q.shape[1], k.shape[1], q.shape[2], cu_seqlens)
+
+
+def attention(q, k, v, cu_seqlens, scale: Optional[float] = None, out=None):
+    """Causal attention inside each of the packed sequences [cu_seqlens[s], cu_seqlens[s + 1])
+    (int32, on the GPU) of q [tokens, q_heads, head_dim] over k, v [tokens, kv_heads, head_dim].
+    Returns out, like q, and the log-sum-exp of every row's scores, fp32 [q_heads, tokens]."""
+    dtype = _dtype(q, k, v)
+    shape = _packed_shape(q, k, v, cu_seqlens)
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+    _expect(out, q.shape, q.dtype, q.device, "out", False)
+    lse = torch.empty(q.shape[1], q.shape[0], dtype=torch.float32, device=q.device)
+    with _on(q):
+        eb.eager_attention(dtype, shape, eb.heads(q), eb.heads(k), eb.heads(v),
+                           1.0 / math.sqrt(q.shape[2]) if scale is None else scale, eb.heads(out), lse)
+    return out, lse
+
+
+def attention_backward(dout, q, k, v, out, lse, cu_seqlens, scale: Optional[float] = None, dq=None, dk=None, dv=None):
+    """Gradients dq, dk, dv from dout and what the forward pass took and gave."""
+    dtype = _dtype(q, k, v, out, dout)
+    shape = _packed_shape(q, k, v, cu_seqlens)
+    dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if d is None else d
+                  for d, x in ((dq, q), (dk, k), (dv, v)))
+    for t, like, name in ((dout, q, "dout"), (out, q, "out"), (dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
+        _expect(t, like.shape, q.dtype, q.device, name, False)
+    _expect(lse, (q.shape[1], q.shape[0]), torch.float32, q.device, "lse")
+    nbytes = eb.eager_attention_workspace_bytes(dtype, shape)
+    with _on(q):
+        eb.eager_attention_backward(dtype, shape, eb.heads(q), eb.heads(k), eb.heads(v), eb.heads(out), lse,
+                                    eb.heads(dout), 1.0 / math.sqrt(q.shape[2]) if scale is None else scale,
+                                    eb.heads(dq), eb.heads(dk), eb.heads(dv), _workspace(nbytes, q), nbytes)
+    return dq, dk, dv
+
+
+class Attention(torch.autograd.Function):
+    """out = Attention.apply(q, k, v, cu_seqlens, scale)"""
+
+    @staticmethod
+    def forward(ctx, q, k, v, cu_seqlens, scale):
+        out, lse = attention(q, k, v, cu_seqlens, scale)
+        ctx.save_for_backward(q, k, v, out, lse, cu_seqlens)
+        ctx.scale = scale
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        q, k, v, out, lse, cu_seqlens = ctx.saved_tensors
+        return (*attention_backward(dout.contiguous(), q, k, v, out, lse, cu_seqlens, ctx.scale), None, None)
+
+
+# ------------------------------------------------------------------------------ loss
+
+def _projection(x, w, target):
+    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1] or x.stride(1) != 1 or w.stride(1) != 1:
+        _refuse(f"expected x [rows, width] and w [vocab, width] with contiguous rows, got {tuple(x.shape)}, {tuple(w.shape)} "
+                f"with strides {x.stride()}, {w.stride()}")
+    _expect(target, (x.shape[0],), torch.int64, x.device, "target")
+    # a lone row may have any stride
+    return eb.Projection(x.shape[0], x.shape[1], w.shape[0], x.stride(0) if x.shape[0] > 1 else x.shape[1],
+                         w.stride(0) if w.shape[0] > 1 else w.shape[1])
+
+
+def cross_entropy(x, w, target):
+    """Losses log sum exp(x w^T) - (x w^T)[target], fp32 [rows], and the log-sum-exps, of hidden
+    states x [rows, width], projection w [vocab, width] and int64 targets; a negative target masks
+    its row (loss 0).  No logits are kept."""
+    dtype = _dtype(x, w)
+    shape = _projection(x, w, target)
+    loss, lse = (torch.empty(x.shape[0], dtype=torch.float32, device=x.device) for _ in range(2))
+    nbytes = eb.eager_cross_entropy_workspace_bytes(dtype, shape, False)
+    with _on(x):
+        eb.eager_cross_entropy(dtype, shape, x, w, target, loss, lse, _workspace(nbytes, x), nbytes)
+    return loss, lse
+
+
+def cross_entropy_backward(dloss, x, w, target, lse, dx=None, dw=None, want=(True, True)):
+    """Gradients dx, dw from those of the losses (fp32 [rows]); want: which of the two are formed.
+    dx and dw are laid out like x and w."""
+    dtype = _dtype(x, w)
+    shape = _projection(x, w, target)
+    _expect(dloss, target.shape, torch.float32, x.device, "dloss")
+    _expect(lse, target.shape, torch.float32, x.device, "lse")
+
+    def like(t, given, name):
+        if given is None:
+            return torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device)
+        _expect(given, t.shape, t.dtype, t.device, name, False)
+        if given.stride(1) != 1 or (t.shape[0] > 1 and given.stride(0) != t.stride(0)):
+            _refuse(f"{name}: expected strides {t.stride()}, got {given.stride()}")
+        return given
+
+    dx = like(x, dx, "dx") if want[0] or dx is not None else None
+    dw = like(w, dw, "dw") if want[1] or dw is not None else None
+    nbytes = eb.eager_cross_entropy_workspace_bytes(dtype, shape, True)
+    with _on(x):
+        eb.eager_cross_entropy_backward(dtype, shape, x, w, target, lse, dloss, dx, dw, _workspace(nbytes, x), nbytes)
+    return dx, dw
+
+
+class CrossEntropy(torch.autograd.Function):
+    """losses = CrossEntropy.apply(x, w, target)"""
+
+    @staticmethod
+    def forward(ctx, x, w, target):
+        loss, lse = cross_entropy(x, w, target)
+        ctx.save_for_backward(x, w, target, lse)
+        return loss
+
+    @staticmethod
+    def backward(ctx, dloss):
+        x, w, target, lse = ctx.saved_tensors
+        if not any(ctx.needs_input_grad[:2]):
+            return None, None, None
+        return (*cross_entropy_backward(dloss.contiguous(), x, w, target, lse, want=ctx.needs_input_grad[:2]), None)
