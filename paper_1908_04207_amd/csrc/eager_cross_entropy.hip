@@ -14,6 +14,9 @@
 #include "eager_matrix.h"
 #include "eager_model.h"
 
+#include <algorithm>
+#include <type_traits>
+
 namespace eager {
 namespace {
 
@@ -29,7 +32,7 @@ struct Side {
 struct Product {
     Side a, b;
     int tiles_a, tiles_b, slices;
-    int steps;               // k tiles of a slice
+    int steps, all_steps;    // k tiles of a slice, of the product
 
     // what becomes of it
     void *out;               // [b row][a row]
@@ -46,37 +49,55 @@ struct Product {
 
 enum Epilogue { kStats, kDlogits, kSums, kResult };
 
-// Bytes of a tile: Rows * 128 whatever the layout (kDepth values of k are 128 bytes)
+// A tile of one side has Rows * 128 bytes whatever the layout: kDepth values of k are 128 bytes.
 template <typename T> constexpr int kDepth = 128 / sizeof(T);
 
+// Tile after tile of one side into shared memory.  A lane's chunk is the same in each of its
+// loads, whose rows are row_step bytes apart; what lies beyond the operand reads as zeros.
 template <typename T, int Rows, bool Columns, int Waves>
-__device__ __forceinline__ void stage_side(char *tile, const Side &s, long long row0, long long k0,
-                                           int wave, int lane)
-{
-    constexpr int E = 16 / sizeof(T);
-    const char *data = static_cast<const char *>(s.data);
-    if (!Columns) {
-        stage_rows<Rows, 8, Waves>(tile, data + (row0 * s.stride + k0) * sizeof(T), s.stride * sizeof(T),
-                                   static_cast<int>(min(s.rows - row0, static_cast<long long>(Rows))),
-                                   static_cast<int>(min((s.k - k0) / E, 8ll)), wave, lane);
-    } else {
-        constexpr int Chunks = Rows / E;
-        const int rows_left = static_cast<int>(min(s.k - k0, static_cast<long long>(kDepth<T>)));
-        const int chunks_left = static_cast<int>(min((s.rows - row0) / E, static_cast<long long>(Chunks)));
-        const char *base = data + (k0 * s.stride + row0) * sizeof(T);
+struct Source {
+    static constexpr int E = 16 / sizeof(T), Chunks = Columns ? Rows / E : 8, Loads = Rows / 8 / Waves;
+    static_assert(Rows % (8 * Waves) == 0 && (Waves * 64 / Chunks % 4 == 0 || sizeof(T) == 4), "whole loads");
+    const char *base;
+    long long bytes, advance;
+    unsigned offset, row_step;
+    int chunk, chunks_left, wave;
+
+    __device__ __forceinline__ Source(const Side &s, long long row0, long long k0, int wave, int lane) : wave(wave)
+    {
         const long long stride = s.stride * sizeof(T);
-        const unsigned bytes = rows_left <= 0 || chunks_left <= 0 ? 0u
-            : static_cast<unsigned>((rows_left - 1) * stride + chunks_left * 16);
-        const __amdgpu_buffer_rsrc_t r = buffer(base, bytes);
-#pragma unroll
-        for (int i = 0; i < Rows * 8 / 64 / Waves; ++i) {
-            const int piece = i * Waves + wave, id = piece * 64 + lane;
-            const int row = id / Chunks, chunk = (id % Chunks) ^ (sizeof(T) == 2 ? (row & 3) << 2 : 0);
-            load_lds16(r, tile + piece * 1024,
-                       chunk < chunks_left ? static_cast<unsigned>(row * static_cast<unsigned>(stride)) + chunk * 16 : kOutside);
+        const int id = wave * 64 + lane, row = id / Chunks;
+        row_step = static_cast<unsigned>(Waves * 64 / Chunks * stride);
+        if (Columns) {
+            base = static_cast<const char *>(s.data) + k0 * stride + row0 * sizeof(T);
+            const long long there = min((s.rows - row0) / E, static_cast<long long>(Chunks));
+            bytes = (s.k - k0 - 1) * stride + there * 16;
+            advance = kDepth<T> * stride;
+            chunk = (id % Chunks) ^ (sizeof(T) == 2 ? (row & 3) << 2 : 0);
+            offset = chunk < there ? static_cast<unsigned>(row * stride) + chunk * 16 : kOutside;
+        } else {
+            base = static_cast<const char *>(s.data) + row0 * stride + k0 * sizeof(T);
+            bytes = (min(s.rows - row0, static_cast<long long>(Rows)) - 1) * stride + (s.k - k0) * sizeof(T);
+            advance = 128;
+            chunk = (id % 8) ^ exchange<8>(row);
+            chunks_left = static_cast<int>((s.k - k0) / E);
+            offset = static_cast<unsigned>(row * stride) + chunk * 16;
         }
     }
-}
+
+    // the next tile; zeros instead where !live
+    __device__ __forceinline__ void load(char *tile, bool live)
+    {
+        const long long n = min(max(live ? bytes : 0ll, 0ll), 0x7fffffffll);
+        const __amdgpu_buffer_rsrc_t r = buffer(base, static_cast<unsigned>(n));
+        const unsigned at = Columns || chunk < chunks_left ? offset : kOutside;
+#pragma unroll
+        for (int i = 0; i < Loads; ++i) load_lds16(r, tile + (i * Waves + wave) * 1024, at + i * row_step);
+        base += advance;
+        bytes -= advance;
+        if (!Columns) chunks_left -= 8;
+    }
+};
 
 template <typename T, int Rows, bool Columns>
 __device__ __forceinline__ typename Operand<T>::frag read_side(const char *tile, int row0, int step, int lane)
@@ -85,70 +106,133 @@ __device__ __forceinline__ typename Operand<T>::frag read_side(const char *tile,
     return read_columns<Rows * sizeof(T) / 16, sizeof(T) == 2 ? 2 : 31>(tile, row0, 16 * step, 8, 4, lane, static_cast<T *>(nullptr));
 }
 
+// The tile of workgroup `id`: workgroups id, id + 8, ... run on the same chiplet (one second-level
+// cache), so each chiplet gets a contiguous share of the tiles, in which 8 tiles of b are gone
+// through for every tile of a.
+__device__ __forceinline__ void place(int id, int tiles_a, int tiles_b, int &tile_a, int &tile_b)
+{
+    constexpr int Group = 8;
+    const int all = tiles_a * tiles_b, chiplet = id & 7, share = all >> 3, rest = all & 7;
+    const int n = chiplet * share + min(chiplet, rest) + (id >> 3);
+    const int group = n / (Group * tiles_a), first = group * Group, width = min(Group, tiles_b - first);
+    const int in = n - group * Group * tiles_a;
+    tile_b = first + in % width;
+    tile_a = in / width;
+}
+
+// One workgroup computes BM x BN results with WM x WN wavefronts.  Two tiles in shared memory take
+// turns: while one is multiplied, the next is on its way into the other.  A step's operands are
+// read while the step before is multiplied, the first step's of a tile during the last one of the
+// tile before, so the barrier between tiles stands in the shadow of matrix instructions.
 template <typename T, int BM, int BN, int WM, int WN, bool ColumnsA, bool ColumnsB, int Epi>
-__global__ __launch_bounds__(64 * WM * WN) void product_kernel(const Product p)
+__device__ __forceinline__ void product(const Product &p, int id, char *tile0, char *tile1)
 {
     constexpr int Waves = WM * WN, MI = BM / WM / 32, NI = BN / WN / 32, Steps = kDepth<T> / 16;
-    __shared__ __align__(1024) char tiles[2][(BM + BN) * 128];
+    typedef typename Operand<T>::frag frag;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tile_b = blockIdx.x % p.tiles_b, rest = blockIdx.x / p.tiles_b;
-    const int tile_a = rest % p.tiles_a, slice = rest / p.tiles_a;
+    const int slice = id / (p.tiles_a * p.tiles_b);
+    int tile_a, tile_b;
+    place(id - slice * p.tiles_a * p.tiles_b, p.tiles_a, p.tiles_b, tile_a, tile_b);
     const long long a0 = static_cast<long long>(tile_a) * BM, b0 = static_cast<long long>(tile_b) * BN;
     const int wave_a = wave % WM * (BM / WM), wave_b = wave / WM * (BN / WN);
-    const long long k_first = static_cast<long long>(slice) * p.steps * kDepth<T>;
-    const long long k_last = min(max(p.a.k, p.b.k), k_first + static_cast<long long>(p.steps) * kDepth<T>);
-    auto stage = [&](long long k0, int buf) {
-        stage_side<T, BM, ColumnsA, Waves>(tiles[buf], p.a, a0, k0, wave, lane);
-        stage_side<T, BN, ColumnsB, Waves>(tiles[buf] + BM * 128, p.b, b0, k0, wave, lane);
+    const int first = slice * p.steps;
+    const int count = max(0, min(p.steps, p.all_steps - first));
+    const long long k0 = static_cast<long long>(first) * kDepth<T>;
+    Source<T, BM, ColumnsA, Waves> side_a(p.a, a0, k0, wave, lane);
+    Source<T, BN, ColumnsB, Waves> side_b(p.b, b0, k0, wave, lane);
+    auto stage = [&](char *tile, int t) {
+        side_a.load(tile, t < count);
+        side_b.load(tile + BM * 128, t < count);
     };
     f32x16 c[MI][NI] = {};
-    if (k_first < k_last) stage(k_first, 0);
-    int buf = 0;
-    for (long long k0 = k_first; k0 < k_last; k0 += kDepth<T>, buf ^= 1) {
-        wait_loads();
-        __syncthreads();
-        if (k0 + kDepth<T> < k_last) stage(k0 + kDepth<T>, buf ^ 1);
+    frag a[2][MI], b[2][NI];
+    auto read = [&](const char *tile, int step, int set) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) a[set][i] = read_side<T, BM, ColumnsA>(tile, wave_a + 32 * i, step, lane);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) b[set][j] = read_side<T, BN, ColumnsB>(tile + BM * 128, wave_b + 32 * j, step, lane);
+    };
+    // reads of shared memory a step, spread evenly over its matrix instructions
+    constexpr int Reads = MI * (ColumnsA ? 2 : 1) + NI * (ColumnsB ? 2 : 1), Products = MI * NI;
+    constexpr int Loads = (BM + BN) / 8 / Waves;
+    auto body = [&](char *here, char *next, int t) {
 #pragma unroll
         for (int s = 0; s < Steps; ++s) {
-            typename Operand<T>::frag a[MI], b[NI];
-#pragma unroll
-            for (int i = 0; i < MI; ++i) a[i] = read_side<T, BM, ColumnsA>(tiles[buf], wave_a + 32 * i, s, lane);
-#pragma unroll
-            for (int j = 0; j < NI; ++j) b[j] = read_side<T, BN, ColumnsB>(tiles[buf] + BM * 128, wave_b + 32 * j, s, lane);
+            if (s + 1 < Steps) {
+                read(here, s + 1, (s + 1) & 1);
+            } else {
+                wait_loads();
+                __syncthreads();
+                stage(here, t + 2);
+                read(next, 0, 0);
+            }
 #pragma unroll
             for (int i = 0; i < MI; ++i)
 #pragma unroll
-                for (int j = 0; j < NI; ++j) c[i][j] = mma(a[i], b[j], c[i][j]);
+                for (int j = 0; j < NI; ++j) c[i][j] = mma(a[s & 1][i], b[s & 1][j], c[i][j]);
+            if constexpr (sizeof(T) == 2) {
+                if (s + 1 < Steps) spread<Products, Reads, 0>();
+                else spread<Products, Reads, Loads>();
+            }
         }
+    };
+    static_assert(Steps % 2 == 0, "a tile ends with the operand registers it began with");
+    stage(tile0, 0);
+    wait_loads();
+    __syncthreads();
+    stage(tile1, 1);
+    read(tile0, 0, 0);
+    int t = 0;
+    for (; t + 1 < count; t += 2) {
+        body(tile0, tile1, t);
+        body(tile1, tile0, t + 1);
     }
+    if (t < count) body(tile0, tile1, t);
+    wait_loads();
 
     const int half = lane >> 5;
     if (Epi == kStats) {
         __syncthreads();
-        float2 *parts = reinterpret_cast<float2 *>(tiles[0]);          // [WM][BN]
+        float2 *parts = reinterpret_cast<float2 *>(tile0);             // [WM][BN]
+        const int live = static_cast<int>(min(p.live - a0, static_cast<long long>(BM))) - wave_a - 4 * half;
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
             const long long row = b0 + wave_b + 32 * j + (lane & 31);
             const long long target = row < p.b.rows ? p.target[row] : -1;
-            float top = -__builtin_inff(), sum = 0.0f;
+            // the target's place among the lane's results, if it has it
+            const long long from = target - a0 - wave_a - 4 * half;
+            const int at = from >= 0 && from < min(live, 32 * MI) ? static_cast<int>(from) : -1;
+            float top = -__builtin_inff(), sum = 0.0f, right = 0.0f;
+            // few wavefronts hold a target or the end of the vocabulary
+            if (__any(at >= 0)) {
 #pragma unroll
-            for (int i = 0; i < MI; ++i)
+                for (int i = 0; i < MI; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const long long v = a0 + wave_a + 32 * i + 8 * (r >> 2) + 4 * half + (r & 3);
-                    if (v >= p.live) c[i][j][r] = -__builtin_inff();
-                    else if (v == target) p.right[row] = c[i][j][r];
-                    top = fmaxf(top, c[i][j][r]);
-                }
-            const float base = top == -__builtin_inff() ? 0.0f : top * kLog2e;
+                    for (int r = 0; r < 16; ++r)
+                        if (32 * i + 8 * (r >> 2) + (r & 3) == at) right = c[i][j][r];
+                if (at >= 0 && (at & 4) == 0) p.right[row] = right;
+            }
+            auto reduce = [&](auto whole) {
 #pragma unroll
-            for (int i = 0; i < MI; ++i)
+                for (int i = 0; i < MI; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sum += exp2_fast(fmaf(c[i][j][r], kLog2e, -base));
+                    for (int r = 0; r < 16; ++r)
+                        if (whole || 32 * i + 8 * (r >> 2) + (r & 3) < live) top = fmaxf(top, c[i][j][r]);
+                const float base = top == -__builtin_inff() ? 0.0f : top * kLog2e;
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const float e = exp2_fast(fmaf(c[i][j][r], kLog2e, -base));
+                        if (whole || 32 * i + 8 * (r >> 2) + (r & 3) < live) sum += e;
+                    }
+            };
+            if (__all(live >= 32 * MI)) reduce(std::true_type());
+            else reduce(std::false_type());
             const float other = __shfl_xor(top, 32, 64), other_sum = __shfl_xor(sum, 32, 64);
             const float both = fmaxf(top, other);
-            const float at = both == -__builtin_inff() ? 0.0f : both;
-            sum = sum * exp2_fast((top - at) * kLog2e) + other_sum * exp2_fast((other - at) * kLog2e);
+            const float zero = both == -__builtin_inff() ? 0.0f : both;
+            sum = sum * exp2_fast((top - zero) * kLog2e) + other_sum * exp2_fast((other - zero) * kLog2e);
             if (half == 0) parts[wave % WM * BN + wave_b + 32 * j + lane] = make_float2(both, sum);
         }
         __syncthreads();
@@ -157,77 +241,149 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const Product p)
 #pragma unroll
             for (int i = 1; i < WM; ++i) {
                 const float2 q = parts[i * BN + n];
-                const float both = fmaxf(all.x, q.x), at = both == -__builtin_inff() ? 0.0f : both;
-                all = make_float2(both, all.y * exp2_fast((all.x - at) * kLog2e) + q.y * exp2_fast((q.x - at) * kLog2e));
+                const float both = fmaxf(all.x, q.x), zero = both == -__builtin_inff() ? 0.0f : both;
+                all = make_float2(both, all.y * exp2_fast((all.x - zero) * kLog2e) + q.y * exp2_fast((q.x - zero) * kLog2e));
             }
             if (b0 + n < p.b.rows) p.stats[tile_a * p.b.rows + b0 + n] = all;
         }
         return;
     }
     typedef typename Operand<T>::quad quad;
+    T *const type = nullptr;
+    // bf16 results cross shared memory, so that stores are whole cache lines; a row of BM results is
+    // BM / 8 chunks, exchanged among themselves against bank conflicts
+    constexpr bool Across = sizeof(T) == 2 && Epi != kSums;
+    constexpr int RowChunks = BM / 8, RowsOfTile0 = (BM + BN) * 128 / (BM * 2);
+    static_assert(!Across || BN <= 2 * RowsOfTile0, "results fit the tiles");
+    if (Across) __syncthreads();
+    auto place_of = [&](int row, int chunk) {
+        char *tile = row < RowsOfTile0 ? tile0 + row * BM * 2 : tile1 + (row - RowsOfTile0) * BM * 2;
+        return tile + (chunk ^ (row & (RowChunks - 1) & 31)) * 16;
+    };
+    const int live = static_cast<int>(min(p.live - a0, static_cast<long long>(BM)));
+    const long long rows = Epi == kResult ? p.live : p.b.rows;
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
-        const long long row = b0 + wave_b + 32 * j + (lane & 31);
-        long long target = -1;
-        float lse = 0.0f, g = 0.0f;
-        if (Epi == kDlogits && row < p.b.rows) {
-            target = p.target[row];
-            lse = p.lse[row] * kLog2e;
-            g = target < 0 ? 0.0f : target >= p.vocab ? __builtin_nanf("") : p.dloss[row];
-            target -= p.first;
+        const int in_b = wave_b + 32 * j + (lane & 31);
+        const long long row = b0 + in_b;
+        if (Epi == kDlogits) {
+            float lse = 0.0f, g = 0.0f;
+            int target = -1;
+            if (row < rows) {
+                const long long v = p.target[row];
+                lse = p.lse[row] * kLog2e;
+                g = v < 0 ? 0.0f : v >= p.vocab ? __builtin_nanf("") : p.dloss[row];
+                const long long from = v - p.first - a0;
+                target = from >= wave_a && from < wave_a + 32 * MI ? static_cast<int>(from) : -1;
+            }
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) c[i][j][r] = exp2_fast(fmaf(c[i][j][r], kLog2e, -lse));
+            if (__any(target >= 0 || live < wave_a + 32 * MI)) {
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int in = wave_a + 32 * i + 8 * (r >> 2) + 4 * half + (r & 3);
+                        if (in == target) c[i][j][r] -= 1.0f;
+                        if (in >= live) c[i][j][r] = 0.0f;
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) c[i][j][r] = g == 0.0f ? 0.0f : g * c[i][j][r];
         }
+        const long long from = a0 + wave_a + 4 * half;
+        const int limit = Epi == kDlogits ? BM : row < rows ? static_cast<int>(min(p.a.rows - from, static_cast<long long>(BM))) : 0;
+        float *const sums = static_cast<float *>(p.out) + (slice * p.b.rows + row) * p.out_stride + from;
+        T *const out = static_cast<T *>(p.out) + row * p.out_stride + from;
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const long long at = a0 + wave_a + 32 * i + 8 * r + 4 * half;
+                const int at = 32 * i + 8 * r;
                 f32x4 x;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[e] = c[i][j][4 * r + e];
-                if (Epi == kDlogits) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float q = exp2_fast(fmaf(x[e], kLog2e, -lse)) - (at + e == target ? 1.0f : 0.0f);
-                        x[e] = g == 0.0f || at + e >= p.live ? 0.0f : g * q;
-                    }
-                    *reinterpret_cast<quad *>(static_cast<T *>(p.out) + row * p.out_stride + at) = to_quad(x, static_cast<T *>(nullptr));
-                } else if (row < (Epi == kResult ? p.live : p.b.rows) && at < p.a.rows) {
+                if (Across) {
+                    *reinterpret_cast<quad *>(place_of(in_b, (wave_a + at) >> 3) + 8 * half) = to_quad(x, type);
+                } else if (at < limit) {
                     if (Epi == kSums) {
-                        f32x4 *y = reinterpret_cast<f32x4 *>(static_cast<float *>(p.out) + (slice * p.b.rows + row) * p.out_stride + at);
-                        if (p.accumulate) x += *y;
-                        *y = x;
+                        if (p.accumulate) x += *reinterpret_cast<const f32x4 *>(sums + at);
+                        *reinterpret_cast<f32x4 *>(sums + at) = x;
                     } else {
-                        *reinterpret_cast<quad *>(static_cast<T *>(p.out) + row * p.out_stride + at) = to_quad(x, static_cast<T *>(nullptr));
+                        *reinterpret_cast<quad *>(out + at) = to_quad(x, type);
                     }
                 }
             }
     }
+    if (Across) {
+        __syncthreads();
+#pragma unroll 4
+        for (int id = threadIdx.x; id < BN * RowChunks; id += 64 * Waves) {
+            const int in_b = id / RowChunks, chunk = id % RowChunks;
+            const long long row = b0 + in_b, at = a0 + chunk * 8;
+            if (Epi == kDlogits || (row < rows && at < p.a.rows))
+                *reinterpret_cast<bf16x8 *>(static_cast<T *>(p.out) + row * p.out_stride + at) =
+                    *reinterpret_cast<const bf16x8 *>(place_of(in_b, chunk));
+        }
+    }
 }
 
-// loss and lse of 64 rows from the tiles' statistics: four wavefronts share the tiles
-__global__ __launch_bounds__(256) void rows_kernel(const float2 *stats, const float *right, const long long *target,
-                                                   float *loss, float *lse, long long rows, int tiles, int vocab)
+constexpr int kTileA = 256, kTileB = 256, kThreads = 512;
+
+// Two arrays, so that the compiler knows a load into one apart from a read of the other.
+#define EAGER_TILES __shared__ __align__(1024) char tile0[(kTileA + kTileB) * 128]; \
+                    __shared__ __align__(1024) char tile1[(kTileA + kTileB) * 128]
+
+template <typename T, int Epi>
+__global__ __launch_bounds__(kThreads) void logits_kernel(const Product p)
 {
-    __shared__ float2 part[4][64];
+    EAGER_TILES;
+    product<T, kTileA, kTileB, 2, 4, false, false, Epi>(p, blockIdx.x, tile0, tile1);
+}
+
+// dw and dx of a piece in one launch: what one leaves idle in its last round the other fills.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void gradients_kernel(const Product dw, const Product dx, int dw_tiles)
+{
+    EAGER_TILES;
+    const int id = blockIdx.x;
+    if (id < dw_tiles) product<T, kTileA, kTileB, 2, 4, true, true, kResult>(dw, id, tile0, tile1);
+    else product<T, kTileA, kTileB, 2, 4, true, false, kSums>(dx, id - dw_tiles, tile0, tile1);
+}
+
+__device__ __forceinline__ void join(float &top, float &sum, float2 q)
+{
+    const float both = fmaxf(top, q.x), zero = both == -__builtin_inff() ? 0.0f : both;
+    sum = sum * exp2_fast((top - zero) * kLog2e) + q.y * exp2_fast((q.x - zero) * kLog2e);
+    top = both;
+}
+
+// loss and lse of 64 rows from the tiles' statistics: 16 wavefronts share the tiles, four loads of
+// each under way at a time
+__global__ __launch_bounds__(1024) void rows_kernel(const float2 *stats, const float *right, const long long *target,
+                                                    float *loss, float *lse, long long rows, int tiles, int vocab)
+{
+    __shared__ float2 part[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long row = static_cast<long long>(blockIdx.x) * 64 + lane;
     float top = -__builtin_inff(), sum = 0.0f;
     if (row < rows)
-        for (int t = wave; t < tiles; t += 4) {
-            const float2 q = stats[t * rows + row];
-            const float both = fmaxf(top, q.x), at = both == -__builtin_inff() ? 0.0f : both;
-            sum = sum * exp2_fast((top - at) * kLog2e) + q.y * exp2_fast((q.x - at) * kLog2e);
-            top = both;
+        for (int t = wave; t < tiles; t += 64) {
+            float2 q[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                q[i] = t + 16 * i < tiles ? stats[(t + 16 * i) * rows + row] : make_float2(-__builtin_inff(), 0.0f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) join(top, sum, q[i]);
         }
     part[wave][lane] = make_float2(top, sum);
     __syncthreads();
     if (wave || row >= rows) return;
-    for (int i = 1; i < 4; ++i) {
-        const float2 q = part[i][lane];
-        const float both = fmaxf(top, q.x), at = both == -__builtin_inff() ? 0.0f : both;
-        sum = sum * exp2_fast((top - at) * kLog2e) + q.y * exp2_fast((q.x - at) * kLog2e);
-        top = both;
-    }
+    for (int i = 1; i < 16; ++i) join(top, sum, part[i][lane]);
     const float all = fmaf(log2_fast(sum), kLn2, top);
     const long long t = target[row];
     lse[row] = all;
@@ -246,33 +402,57 @@ __global__ __launch_bounds__(256) void sums_kernel(const float *sums, T *dx, lon
     *reinterpret_cast<typename Operand<T>::quad *>(dx + i / quads * stride + i % quads * 4) = to_quad(x, static_cast<T *>(nullptr));
 }
 
-constexpr int kTileA = 128, kTileB = 128;
-
 long long round_up(long long x, long long to) { return (x + to - 1) / to * to; }
 
-template <typename T, bool ColumnsA, bool ColumnsB, int Epi>
-void multiply(Product p, hipStream_t stream)
+// Tiles of a product, and their number.
+template <typename T>
+int lay_out(Product &p)
 {
     p.tiles_a = static_cast<int>(round_up(p.a.rows, kTileA) / kTileA);
     p.tiles_b = static_cast<int>(round_up(p.b.rows, kTileB) / kTileB);
-    const long long steps = round_up(p.a.k > p.b.k ? p.a.k : p.b.k, kDepth<T>) / kDepth<T>;
-    p.steps = static_cast<int>(round_up(steps, p.slices) / p.slices);
-    const unsigned grid = static_cast<unsigned>(static_cast<long long>(p.tiles_a) * p.tiles_b * p.slices);
-    hipLaunchKernelGGL((product_kernel<T, kTileA, kTileB, 2, 2, ColumnsA, ColumnsB, Epi>), dim3(grid), dim3(256), 0, stream, p);
+    p.all_steps = static_cast<int>(round_up(std::max(p.a.k, p.b.k), kDepth<T>) / kDepth<T>);
+    p.steps = (p.all_steps + p.slices - 1) / p.slices;
+    return p.tiles_a * p.tiles_b * p.slices;
 }
 
-// Vocabulary rows of a piece and slices of dx for a workspace of so many bytes (at most what
-// cross_entropy_workspace_bytes asks for); 0 if it is too small.
-struct Pieces {
-    long long rows_padded, piece;
+// How the backward pass is cut: vocabulary rows of a piece (a multiple of kTileA) and, for dx, slices
+// of a piece that are summed apart.  One workgroup has a compute unit, so a product takes as
+// long as its rounds of 256 tiles: k tiles each and about 8 more for filling and emptying (a tile
+// of k is 1.5 us, the rest of a logits tile about 12 us).  The cut with the least of that is taken among those
+// whose dl fit 512 MiB; 50257 x 1600 on 8191 rows: TODO figures.
+struct Cut {
+    long long piece;
     int slices;
 };
 
-long long piece_of(long long rows, int vocab, int bytes)
+Cut cut(long long rows, int width, int vocab, int bytes)
 {
-    const long long rows_padded = round_up(rows > 0 ? rows : 1, kTileB), all = round_up(vocab, kTileA);
-    const long long fit = (1ll << 28) / bytes / rows_padded / kTileA * kTileA;
-    return fit < kTileA ? kTileA : fit < all ? fit : all;
+    const long long depth = 128 / bytes, tiles_b = round_up(rows > 0 ? rows : 1, kTileB) / kTileB;
+    const long long tiles_v = round_up(vocab, kTileA) / kTileA, tiles_w = round_up(width, kTileA) / kTileA;
+    const long long fit = std::max(1ll, (1ll << 29) / bytes / (tiles_b * kTileB) / kTileA);
+    const long long fewest = (tiles_v + fit - 1) / fit;
+    auto rounds = [](long long tiles) { return (tiles + 255) / 256; };
+    Cut best = {};
+    double least = 0;
+    for (long long n = fewest; n < fewest + 8 && n <= tiles_v; ++n) {
+        const long long piece = (tiles_v + n - 1) / n, pieces = (tiles_v + piece - 1) / piece;
+        for (int slices = 1; slices <= 16; slices *= 2) {
+            double cost = 0;
+            for (long long i = 0; i < pieces; i += pieces > 1 ? pieces - 1 : 1) {      // the full ones, then the last
+                const long long tiles = i + 1 < pieces ? piece : tiles_v - piece * (pieces - 1);
+                const long long times = i + 1 < pieces ? pieces - 1 : 1;
+                const double dw = rows / depth + 8, dx = tiles * kTileA / depth / slices + 8;
+                const double both = tiles * tiles_w * dw + tiles_w * tiles_b * slices * dx;
+                cost += times * (rounds(tiles * tiles_b) * (width / depth + 8) + both / 256 + std::max(dw, dx) / 2 +
+                                 slices * static_cast<double>(rows) * width * 8 / 6e6);
+            }
+            if (!best.piece || cost < least) {
+                least = cost;
+                best = {piece * kTileA, slices};
+            }
+        }
+    }
+    return best;
 }
 
 template <typename T>
@@ -287,8 +467,9 @@ hipError_t forward(const CrossEntropyArgs &a, hipStream_t stream)
     const long long tiles = round_up(a.vocab, kTileA) / kTileA;
     p.stats = reinterpret_cast<float2 *>(a.workspace);
     p.right = reinterpret_cast<float *>(p.stats + tiles * a.rows);
-    multiply<T, false, false, kStats>(p, stream);
-    hipLaunchKernelGGL(rows_kernel, dim3(static_cast<unsigned>((a.rows + 63) / 64)), dim3(256), 0, stream, p.stats, p.right,
+    const int tiles_all = lay_out<T>(p);
+    hipLaunchKernelGGL((logits_kernel<T, kStats>), dim3(tiles_all), dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL(rows_kernel, dim3(static_cast<unsigned>((a.rows + 63) / 64)), dim3(1024), 0, stream, p.stats, p.right,
                        a.target, a.loss, a.lse, a.rows, static_cast<int>(tiles), a.vocab);
     return hipGetLastError();
 }
@@ -296,54 +477,57 @@ hipError_t forward(const CrossEntropyArgs &a, hipStream_t stream)
 template <typename T>
 hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
 {
-    const long long rows_padded = round_up(a.rows, kTileB), piece = piece_of(a.rows, a.vocab, sizeof(T));
+    const Cut c = cut(a.rows, a.width, a.vocab, sizeof(T));
+    const long long rows_padded = round_up(a.rows, kTileB), piece = c.piece;
     const T *w = static_cast<const T *>(a.w);
     T *dl = reinterpret_cast<T *>(a.workspace);
     float *sums = reinterpret_cast<float *>(a.workspace + rows_padded * piece * sizeof(T));
-    const int slices = 1;
     for (long long first = 0; first < a.vocab; first += piece) {
-        const int live = static_cast<int>(a.vocab - first < piece ? a.vocab - first : piece);
+        const int live = static_cast<int>(std::min<long long>(a.vocab - first, piece));
         const long long padded = round_up(live, kTileA);
-        Product p = {};
         if (a.rows) {
+            Product p = {};
             p.a = {w + first * a.w_stride, a.w_stride, live, a.width};
             p.b = {a.x, a.x_stride, a.rows, a.width};
-            p.vocab = a.vocab;
             p.slices = 1;
             p.first = first;
             p.live = live;
+            p.vocab = a.vocab;
             p.target = a.target;
             p.lse = a.lse;
             p.dloss = a.dloss;
             p.out = dl;
             p.out_stride = padded;
-            multiply<T, false, false, kDlogits>(p, stream);
+            const int tiles = lay_out<T>(p);
+            hipLaunchKernelGGL((logits_kernel<T, kDlogits>), dim3(tiles), dim3(kThreads), 0, stream, p);
         }
+        Product dx = {}, dw = {};
+        int dx_tiles = 0, dw_tiles = 0;
         if (a.dx && a.rows) {
-            p = {};
             // dl is zero from `live` to `padded`, so its last chunk may be read whole
-            p.a = {w + first * a.w_stride, a.w_stride, a.width, live};
-            p.b = {dl, padded, a.rows, round_up(live, 16 / sizeof(T))};
-            p.slices = slices;
-            p.out = sums;
-            p.out_stride = a.width;
-            p.accumulate = first > 0;
-            multiply<T, true, false, kSums>(p, stream);
+            dx.a = {w + first * a.w_stride, a.w_stride, a.width, live};
+            dx.b = {dl, padded, a.rows, round_up(live, 16 / sizeof(T))};
+            dx.slices = c.slices;
+            dx.out = sums;
+            dx.out_stride = a.width;
+            dx.accumulate = first > 0;
+            dx_tiles = lay_out<T>(dx);
         }
         if (a.dw) {
-            p = {};
-            p.a = {a.x, a.x_stride, a.width, a.rows};
-            p.b = {dl, padded, padded, a.rows};
-            p.slices = 1;
-            p.live = live;
-            p.out = static_cast<T *>(a.dw) + first * a.w_stride;
-            p.out_stride = a.w_stride;
-            multiply<T, true, true, kResult>(p, stream);
+            dw.a = {a.x, a.x_stride, a.width, a.rows};
+            dw.b = {dl, padded, padded, a.rows};
+            dw.slices = 1;
+            dw.live = live;
+            dw.out = static_cast<T *>(a.dw) + first * a.w_stride;
+            dw.out_stride = a.w_stride;
+            dw_tiles = lay_out<T>(dw);
         }
+        if (dx_tiles + dw_tiles)
+            hipLaunchKernelGGL((gradients_kernel<T>), dim3(dx_tiles + dw_tiles), dim3(kThreads), 0, stream, dw, dx, dw_tiles);
     }
     if (a.dx && a.rows)
         hipLaunchKernelGGL((sums_kernel<T>), dim3(static_cast<unsigned>((a.rows * (a.width / 4) + 255) / 256)), dim3(256), 0, stream,
-                           sums, static_cast<T *>(a.dx), a.x_stride, a.rows, a.width, slices);
+                           sums, static_cast<T *>(a.dx), a.x_stride, a.rows, a.width, c.slices);
     return hipGetLastError();
 }
 
@@ -353,7 +537,8 @@ long long cross_entropy_workspace_bytes(long long rows, int width, int vocab, bo
 {
     if (!backward) return round_up(rows * (round_up(vocab, kTileA) / kTileA * 8 + 4), 16) + 16;
     const int bytes = bf16 ? 2 : 4;
-    return round_up(rows, kTileB) * piece_of(rows, vocab, bytes) * bytes + rows * width * 4 + 16;
+    const Cut c = cut(rows, width, vocab, bytes);
+    return round_up(rows, kTileB) * c.piece * bytes + c.slices * rows * width * 4 + 16;
 }
 
 hipError_t launch_cross_entropy(const CrossEntropyArgs &a, bool bf16, hipStream_t stream)

@@ -81,13 +81,13 @@ __device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t r, char *lds, 
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
 
 // ---- tiles whose rows are operand rows and hold consecutive k: `Chunks` 16-byte chunks a row.
-// Reads take the same chunk of 32 rows; the exchange spreads 8 (16) consecutive rows over the
-// banks, and the four rows of a transposing read over different pairs of chunks.
+// Reads take the same chunk of 32 rows; the exchange spreads 16 consecutive rows over the 256 bytes
+// of banks, and the four rows of a transposing read over different pairs of chunks.
 template <int Chunks>
 __device__ __forceinline__ int exchange(int row)
 {
     if (Chunks >= 16) return ((row & 3) << 2) | ((row >> 2) & 3);
-    return ((row & 2) << 1) | ((row >> 1) & 2) | (row & 1);
+    return ((row & 2) << 1) | ((row >> 1) & 2) | ((row >> 3) & 1);
 }
 
 // Rows [first, first + Rows) of a matrix at `base` (row `first`) into a tile; rows from rows_left
@@ -160,6 +160,21 @@ __device__ __forceinline__ f32x8 read_columns(const char *tile, int col0, int k0
                                                 ((col >> 2) ^ exchange_of<Chunks, Shift>(row)) * 16 + (col & 3) * 4);
     }
     return f;
+}
+
+// Tells the compiler's scheduler to issue Reads reads of shared memory and Loads loads from global
+// memory evenly among the next Products matrix instructions.
+template <int Products, int Reads, int Loads, int I = 0>
+__device__ __forceinline__ void spread()
+{
+    if constexpr (I < Products) {
+        constexpr int reads = (I + 1) * Reads / Products - I * Reads / Products;
+        constexpr int loads = (I + 1) * Loads / Products - I * Loads / Products;
+        if constexpr (reads > 0) __builtin_amdgcn_sched_group_barrier(0x100, reads, 0);
+        if constexpr (loads > 0) __builtin_amdgcn_sched_group_barrier(0x20, loads, 0);
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        spread<Products, Reads, Loads, I + 1>();
+    }
 }
 
 // base-2 exponential and logarithm of the hardware: one unit in the last place for normal results
