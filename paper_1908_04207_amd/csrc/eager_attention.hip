@@ -15,10 +15,15 @@ constexpr int kRows = 128;           // query rows of a workgroup: 32 a wavefron
 constexpr int kKeys = 64;            // keys of a tile
 
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void attention_kernel(const AttentionArgs a)
+__global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attention_kernel(const AttentionArgs a)
 {
     constexpr int Chunks = DP * sizeof(T) / 16, TileBytes = kKeys * Chunks * 16, Steps = DP / 16;
-    __shared__ __align__(1024) char tiles[2][2][TileBytes];
+    // arrays of their own, so that the compiler knows a load into one apart from a read of another
+    __shared__ __align__(1024) char k_tile0[TileBytes];
+    __shared__ __align__(1024) char v_tile0[TileBytes];
+    __shared__ __align__(1024) char k_tile1[TileBytes];
+    __shared__ __align__(1024) char v_tile1[TileBytes];
+    T *const type = nullptr;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int head = blockIdx.x % a.q_heads;
     const Tile t = find_tile<kRows>(a.cu, a.sequences, static_cast<int>(a.tokens),
@@ -41,54 +46,56 @@ __global__ __launch_bounds__(256) void attention_kernel(const AttentionArgs a)
     const char *v_base = reinterpret_cast<const char *>(static_cast<const T *>(a.v.data) + kv_head * a.v.head);
     const long long k_stride = a.k.row * sizeof(T), v_stride = a.v.row * sizeof(T);
     const int chunks = a.dim * sizeof(T) / 16;
-    auto stage = [&](int key0, int buf) {
-        stage_rows<kKeys, Chunks, 4>(tiles[buf][0], k_base + key0 * k_stride, k_stride, t.end - key0, chunks, wave, lane);
-        stage_rows<kKeys, Chunks, 4>(tiles[buf][1], v_base + key0 * v_stride, v_stride, t.end - key0, chunks, wave, lane);
+    auto stage = [&](int key0, char *k_tile, char *v_tile) {
+        stage_rows<kKeys, Chunks, 4>(k_tile, k_base + key0 * k_stride, k_stride, t.end - key0, chunks, wave, lane);
+        stage_rows<kKeys, Chunks, 4>(v_tile, v_base + key0 * v_stride, v_stride, t.end - key0, chunks, wave, lane);
     };
 
     const float c = a.scale * kLog2e;
     const int last = min(t.end, t.first + kRows);       // no key from here on is seen
     f32x16 o[DP / 32] = {};
     float top = -__builtin_inff(), sum = 0.0f;
-    stage(t.begin, 0);
-    for (int key0 = t.begin, buf = 0; key0 < last; key0 += kKeys, buf ^= 1) {
+    auto tile = [&](int key0, char *k_tile, char *v_tile, char *next_k, char *next_v) {
         wait_loads();
         __syncthreads();
-        if (key0 + kKeys < last) stage(key0 + kKeys, buf ^ 1);
-        if (key0 >= wave_row + 32) continue;            // every key is later than the wavefront's rows
+        stage(key0 + kKeys, next_k, next_v);            // beyond the sequence: zeros
+        if (key0 >= wave_row + 32) return;              // every key is later than the wavefront's rows
         f32x16 s[2] = {};
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int i = 0; i < Steps; ++i)
 #pragma unroll
-            for (int i = 0; i < Steps; ++i)
-                s[b] = mma(read_rows<Chunks>(tiles[buf][0], 32 * b, i, lane, static_cast<T *>(nullptr)), q[i], s[b]);
+            for (int b = 0; b < 2; ++b) s[b] = mma(read_rows<Chunks>(k_tile, 32 * b, i, lane, type), q[i], s[b]);
         if (key0 + kKeys - 1 > wave_row) {
+            const int seen = row - key0 - 4 * (lane >> 5);
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (key0 + 32 * b + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > row) s[b][i] = -__builtin_inff();
+                    if (32 * b + 8 * (i >> 2) + (i & 3) > seen) s[b][i] = -__builtin_inff();
         }
         float best = top;
 #pragma unroll
         for (int i = 0; i < 16; ++i) best = fmaxf(best, fmaxf(s[0][i], s[1][i]));
-        best = fmaxf(best, __shfl_xor(best, 32, 64));
+        best = both_max(best);
         const float base = best == -__builtin_inff() ? 0.0f : best * c;
-        const float keep = exp2_fast(fmaf(top, c, -base));
-        top = best;
-        float add = 0.0f;
+        if (__any(best != top)) {                       // a new maximum: rare after the first tiles
+            const float keep = exp2_fast(fmaf(top, c, -base));
+            top = best;
+            sum *= keep;
+#pragma unroll
+            for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[b][i] *= keep;
+        }
+        float add[2] = {};
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 s[b][i] = exp2_fast(fmaf(s[b][i], c, -base));
-                add += s[b][i];
+                add[b] += s[b][i];
             }
-        sum = fmaf(sum, keep, add);
-#pragma unroll
-        for (int b = 0; b < DP / 32; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[b][i] *= keep;
+        sum += add[0] + add[1];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -96,11 +103,16 @@ __global__ __launch_bounds__(256) void attention_kernel(const AttentionArgs a)
                 const typename Operand<T>::frag p = as_operand<T>(s[b], h);
 #pragma unroll
                 for (int d = 0; d < DP / 32; ++d)
-                    o[d] = mma(read_columns<Chunks>(tiles[buf][1], 32 * d, 32 * b + 16 * h, 4, 8, lane,
-                                                    static_cast<T *>(nullptr)), p, o[d]);
+                    o[d] = mma(read_columns<Chunks>(v_tile, 32 * d, 32 * b + 16 * h, 4, 8, lane, type), p, o[d]);
             }
+    };
+    stage(t.begin, k_tile0, v_tile0);
+    for (int key0 = t.begin; key0 < last; key0 += 2 * kKeys) {
+        tile(key0, k_tile0, v_tile0, k_tile1, v_tile1);
+        tile(key0 + kKeys, k_tile1, v_tile1, k_tile0, v_tile0);
     }
-    sum += __shfl_xor(sum, 32, 64);
+    wait_loads();
+    sum = both_sum(sum);
     if (row < t.end) {
         T *out = static_cast<T *>(a.out.data) + static_cast<long long>(row) * a.out.row + head * a.out.head;
         store_row<T, DP>(out, o, 1.0f / sum, lane, a.dim);

@@ -16,10 +16,14 @@ constexpr int kRows = 128;           // queries (keys) of a workgroup: 32 a wave
 constexpr int kTile = 64;            // keys (queries) of a tile
 
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void queries_kernel(const AttentionArgs a)
+__global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void queries_kernel(const AttentionArgs a)
 {
     constexpr int Chunks = DP * sizeof(T) / 16, TileBytes = kTile * Chunks * 16, Steps = DP / 16;
-    __shared__ __align__(1024) char tiles[2][2][TileBytes];
+    // arrays of their own, so that the compiler knows a load into one apart from a read of another
+    __shared__ __align__(1024) char k_tile0[TileBytes];
+    __shared__ __align__(1024) char v_tile0[TileBytes];
+    __shared__ __align__(1024) char k_tile1[TileBytes];
+    __shared__ __align__(1024) char v_tile1[TileBytes];
     T *const type = nullptr;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int head = blockIdx.x % a.q_heads;
@@ -46,7 +50,7 @@ __global__ __launch_bounds__(256) void queries_kernel(const AttentionArgs a)
 #pragma unroll
         for (int j = 0; j < 8; ++j) delta = fmaf(static_cast<float>(g[s][j]), static_cast<float>(o[j]), delta);
     }
-    delta += __shfl_xor(delta, 32, 64);
+    delta = both_sum(delta);
     float lse = 0.0f;
     if (there) {
         lse = a.lse[head * a.tokens + row] * kLog2e;
@@ -57,64 +61,90 @@ __global__ __launch_bounds__(256) void queries_kernel(const AttentionArgs a)
     const char *v_base = reinterpret_cast<const char *>(static_cast<const T *>(a.v.data) + kv_head * a.v.head);
     const long long k_stride = a.k.row * sizeof(T), v_stride = a.v.row * sizeof(T);
     const int chunks = a.dim * sizeof(T) / 16;
-    auto stage = [&](int key0, int buf) {
-        stage_rows<kTile, Chunks, 4>(tiles[buf][0], k_base + key0 * k_stride, k_stride, t.end - key0, chunks, wave, lane);
-        stage_rows<kTile, Chunks, 4>(tiles[buf][1], v_base + key0 * v_stride, v_stride, t.end - key0, chunks, wave, lane);
+    auto stage = [&](int key0, char *k_tile, char *v_tile) {
+        stage_rows<kTile, Chunks, 4>(k_tile, k_base + key0 * k_stride, k_stride, t.end - key0, chunks, wave, lane);
+        stage_rows<kTile, Chunks, 4>(v_tile, v_base + key0 * v_stride, v_stride, t.end - key0, chunks, wave, lane);
     };
 
     const float c = a.scale * kLog2e;
     const int last = min(t.end, t.first + kRows);
     f32x16 dq[DP / 32] = {};
-    stage(t.begin, 0);
-    for (int key0 = t.begin, buf = 0; key0 < last; key0 += kTile, buf ^= 1) {
+    auto tile = [&](int key0, char *k_tile, char *v_tile, char *next_k, char *next_v) {
         wait_loads();
         __syncthreads();
-        if (key0 + kTile < last) stage(key0 + kTile, buf ^ 1);
-        const bool diagonal = key0 + kTile - 1 > wave_row;
+        stage(key0 + kTile, next_k, next_v);            // beyond the sequence: zeros
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             if (key0 + 32 * b >= wave_row + 32) continue;
             f32x16 s = {}, dp = {};
 #pragma unroll
             for (int i = 0; i < Steps; ++i) {
-                s = mma(read_rows<Chunks>(tiles[buf][0], 32 * b, i, lane, type), q[i], s);
-                dp = mma(read_rows<Chunks>(tiles[buf][1], 32 * b, i, lane, type), g[i], dp);
+                s = mma(read_rows<Chunks>(k_tile, 32 * b, i, lane, type), q[i], s);
+                dp = mma(read_rows<Chunks>(v_tile, 32 * b, i, lane, type), g[i], dp);
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float p = exp2_fast(fmaf(s[i], c, -lse));
-                if (diagonal && key0 + 32 * b + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > row) p = 0.0f;
-                s[i] = p * (dp[i] - delta);
+            for (int i = 0; i < 16; ++i) s[i] = exp2_fast(fmaf(s[i], c, -lse));
+            if (key0 + 32 * b + 31 > wave_row) {
+                const int seen = row - key0 - 32 * b - 4 * (lane >> 5);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (8 * (i >> 2) + (i & 3) > seen) s[i] = 0.0f;
             }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] *= dp[i] - delta;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const typename Operand<T>::frag ds = as_operand<T>(s, h);
 #pragma unroll
                 for (int d = 0; d < DP / 32; ++d)
-                    dq[d] = mma(read_columns<Chunks>(tiles[buf][0], 32 * d, 32 * b + 16 * h, 4, 8, lane, type), ds, dq[d]);
+                    dq[d] = mma(read_columns<Chunks>(k_tile, 32 * d, 32 * b + 16 * h, 4, 8, lane, type), ds, dq[d]);
             }
         }
+    };
+    stage(t.begin, k_tile0, v_tile0);
+    for (int key0 = t.begin; key0 < last; key0 += 2 * kTile) {
+        tile(key0, k_tile0, v_tile0, k_tile1, v_tile1);
+        tile(key0 + kTile, k_tile1, v_tile1, k_tile0, v_tile0);
     }
+    wait_loads();
     if (there) {
         T *y = static_cast<T *>(a.dq.data) + static_cast<long long>(row) * a.dq.row + head * a.dq.head;
         store_row<T, DP>(y, dq, a.scale, lane, a.dim);
     }
 }
 
+// The query heads that share a key head fall into `parts` parts, each with workgroups of its own:
+// with few keys and heads there would be too few of them, and those of the first keys, which have
+// the most queries, would run alone at the end.  With more than one part the sums of each go to the
+// workspace in fp32 and parts_kernel adds them.
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void keys_kernel(const AttentionArgs a)
+__global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void keys_kernel(const AttentionArgs a)
 {
     constexpr int Chunks = DP * sizeof(T) / 16, TileBytes = kTile * Chunks * 16, Steps = DP / 16;
-    __shared__ __align__(1024) char tiles[2][2][TileBytes];
-    __shared__ __align__(1024) float rows[2][2][kTile];
+    __shared__ __align__(1024) char q_tile0[TileBytes];
+    __shared__ __align__(1024) char g_tile0[TileBytes];
+    __shared__ __align__(1024) char q_tile1[TileBytes];
+    __shared__ __align__(1024) char g_tile1[TileBytes];
+    __shared__ __align__(1024) float rows0[2][kTile];
+    __shared__ __align__(1024) float rows1[2][kTile];
     T *const type = nullptr;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int kv_head = blockIdx.x % a.kv_heads, group = a.q_heads / a.kv_heads;
-    const Tile t = find_tile<kRows>(a.cu, a.sequences, static_cast<int>(a.tokens), blockIdx.x / a.kv_heads);
+    const int shared = blockIdx.x % (a.kv_heads * a.parts), kv_head = shared / a.parts, part = shared % a.parts;
+    const int heads = a.q_heads / a.kv_heads / a.parts;
+    const Tile t = find_tile<kRows>(a.cu, a.sequences, static_cast<int>(a.tokens), blockIdx.x / (a.kv_heads * a.parts));
     if (t.first >= t.end) return;
+    // where the sums go: [part][k, v][kv head][token][dim]
+    float *const sums = a.sums + (static_cast<long long>(part) * 2 * a.kv_heads + kv_head) * a.tokens * a.dim;
+    const long long to_v = static_cast<long long>(a.kv_heads) * a.tokens * a.dim;
     if (t.segment == 0 || t.segment == a.sequences + 1) {
-        clear_rows<T, kRows>(a.dk, kv_head, t.first, t.end, a.dim);
-        clear_rows<T, kRows>(a.dv, kv_head, t.first, t.end, a.dim);
+        if (a.parts == 1) {
+            clear_rows<T, kRows>(a.dk, kv_head, t.first, t.end, a.dim);
+            clear_rows<T, kRows>(a.dv, kv_head, t.first, t.end, a.dim);
+        } else {
+            const Heads y = {sums, a.dim, 0}, z = {sums + to_v, a.dim, 0};
+            clear_rows<float, kRows>(y, 0, t.first, t.end, a.dim);
+            clear_rows<float, kRows>(z, 0, t.first, t.end, a.dim);
+        }
         return;
     }
     const int wave_key = t.first + 32 * wave, key = wave_key + (lane & 31);
@@ -129,71 +159,113 @@ __global__ __launch_bounds__(256) void keys_kernel(const AttentionArgs a)
     }
     const long long q_stride = a.q.row * sizeof(T), g_stride = a.dout.row * sizeof(T);
     const int chunks = a.dim * sizeof(T) / 16;
-    const int first_row = t.first;                      // a multiple of kTile rows from the sequence's first
-    const int tiles_a_head = (t.end - first_row + kTile - 1) / kTile;
-    auto stage = [&](int n, int buf) {
-        const int head = kv_head * group + n / tiles_a_head, row0 = first_row + n % tiles_a_head * kTile;
-        const char *q = reinterpret_cast<const char *>(static_cast<const T *>(a.q.data) + head * a.q.head) + row0 * q_stride;
-        const char *g = reinterpret_cast<const char *>(static_cast<const T *>(a.dout.data) + head * a.dout.head) + row0 * g_stride;
-        stage_rows<kTile, Chunks, 4>(tiles[buf][0], q, q_stride, t.end - row0, chunks, wave, lane);
-        stage_rows<kTile, Chunks, 4>(tiles[buf][1], g, g_stride, t.end - row0, chunks, wave, lane);
+    // tiles of queries of one head after the other
+    int next_head = (kv_head * a.parts + part) * heads, next_row = t.first;
+    const int last_head = next_head + heads;
+    auto stage = [&](char *q_tile, char *g_tile, float (*rows)[kTile]) {
+        const int left = next_head < last_head ? t.end - next_row : 0;
+        const int head = min(next_head, last_head - 1);
+        const char *q = reinterpret_cast<const char *>(static_cast<const T *>(a.q.data) + head * a.q.head) + next_row * q_stride;
+        const char *g = reinterpret_cast<const char *>(static_cast<const T *>(a.dout.data) + head * a.dout.head) + next_row * g_stride;
+        stage_rows<kTile, Chunks, 4>(q_tile, q, q_stride, left, chunks, wave, lane);
+        stage_rows<kTile, Chunks, 4>(g_tile, g, g_stride, left, chunks, wave, lane);
         // rows beyond the sequence: zeros, with which P = 1, but dO and dP - delta are zeros too
-        const float *per_row = (wave & 1 ? a.delta : a.lse) + head * a.tokens + row0;
+        const float *per_row = (wave & 1 ? a.delta : a.lse) + head * a.tokens + next_row;
         if (wave < 2)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(per_row, min(kTile, t.end - row0) * 4),
-                                                     (__attribute__((address_space(3))) void *)(rows[buf][wave]), 4,
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(per_row, min(kTile, left) * 4),
+                                                     (__attribute__((address_space(3))) void *)(rows[wave]), 4,
                                                      lane * 4, 0, 0, 0);
+        next_row += kTile;
+        if (next_row >= t.end) {
+            next_row = t.first;
+            ++next_head;
+        }
     };
 
     const float c = a.scale * kLog2e;
     f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
-    const int count = group * tiles_a_head;
-    stage(0, 0);
-    for (int n = 0, buf = 0; n < count; ++n, buf ^= 1) {
-        const int row0 = first_row + n % tiles_a_head * kTile;
+    const int tiles_a_head = (t.end - t.first + kTile - 1) / kTile, count = heads * tiles_a_head;
+    int row0 = t.first;
+    auto tile = [&](char *q_tile, char *g_tile, float (*rows)[kTile], char *next_q, char *next_g, float (*next_rows)[kTile]) {
         wait_loads();
         __syncthreads();
-        if (n + 1 < count) stage(n + 1, buf ^ 1);
-        const bool diagonal = row0 < wave_key + 31;
+        stage(next_q, next_g, next_rows);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             if (row0 + 32 * b + 31 < wave_key) continue;        // all rows come before the wavefront's keys
             f32x16 s = {}, dp = {};
 #pragma unroll
             for (int i = 0; i < Steps; ++i) {
-                s = mma(read_rows<Chunks>(tiles[buf][0], 32 * b, i, lane, type), k[i], s);
-                dp = mma(read_rows<Chunks>(tiles[buf][1], 32 * b, i, lane, type), v[i], dp);
+                s = mma(read_rows<Chunks>(q_tile, 32 * b, i, lane, type), k[i], s);
+                dp = mma(read_rows<Chunks>(g_tile, 32 * b, i, lane, type), v[i], dp);
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int at = 32 * b + 8 * r + 4 * (lane >> 5);
-                const f32x4 lse = *reinterpret_cast<const f32x4 *>(&rows[buf][0][at]);
-                const f32x4 delta = *reinterpret_cast<const f32x4 *>(&rows[buf][1][at]);
+                const f32x4 lse = *reinterpret_cast<const f32x4 *>(&rows[0][32 * b + 8 * r + 4 * (lane >> 5)]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float p = exp2_fast(fmaf(s[4 * r + i], c, -lse[i] * kLog2e));
-                    if (diagonal && key > row0 + at + i) p = 0.0f;
-                    s[4 * r + i] = p;
-                    dp[4 * r + i] = p * (dp[4 * r + i] - delta[i]);
-                }
+                for (int i = 0; i < 4; ++i) s[4 * r + i] = exp2_fast(fmaf(s[4 * r + i], c, -lse[i] * kLog2e));
+            }
+            if (row0 + 32 * b < wave_key + 31) {
+                const int seen = key - row0 - 32 * b - 4 * (lane >> 5);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (8 * (i >> 2) + (i & 3) < seen) s[i] = 0.0f;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const f32x4 delta = *reinterpret_cast<const f32x4 *>(&rows[1][32 * b + 8 * r + 4 * (lane >> 5)]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    dp[4 * r + i] = s[4 * r + i] * (dp[4 * r + i] - delta[i]);
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const typename Operand<T>::frag p = as_operand<T>(s, h), ds = as_operand<T>(dp, h);
 #pragma unroll
                 for (int d = 0; d < DP / 32; ++d) {
-                    dv[d] = mma(read_columns<Chunks>(tiles[buf][1], 32 * d, 32 * b + 16 * h, 4, 8, lane, type), p, dv[d]);
-                    dk[d] = mma(read_columns<Chunks>(tiles[buf][0], 32 * d, 32 * b + 16 * h, 4, 8, lane, type), ds, dk[d]);
+                    dv[d] = mma(read_columns<Chunks>(g_tile, 32 * d, 32 * b + 16 * h, 4, 8, lane, type), p, dv[d]);
+                    dk[d] = mma(read_columns<Chunks>(q_tile, 32 * d, 32 * b + 16 * h, 4, 8, lane, type), ds, dk[d]);
                 }
             }
         }
+        row0 += kTile;
+        if (row0 >= t.end) row0 = t.first;
+    };
+    stage(q_tile0, g_tile0, rows0);
+    int n = 0;
+    for (; n + 1 < count; n += 2) {
+        tile(q_tile0, g_tile0, rows0, q_tile1, g_tile1, rows1);
+        tile(q_tile1, g_tile1, rows1, q_tile0, g_tile0, rows0);
     }
-    if (there) {
+    if (n < count) tile(q_tile0, g_tile0, rows0, q_tile1, g_tile1, rows1);
+    wait_loads();
+    if (!there) return;
+    if (a.parts == 1) {
         T *yk = static_cast<T *>(a.dk.data) + static_cast<long long>(key) * a.dk.row + kv_head * a.dk.head;
         T *yv = static_cast<T *>(a.dv.data) + static_cast<long long>(key) * a.dv.row + kv_head * a.dv.head;
         store_row<T, DP>(yk, dk, a.scale, lane, a.dim);
         store_row<T, DP>(yv, dv, 1.0f, lane, a.dim);
+    } else {
+        store_row<float, DP>(sums + static_cast<long long>(key) * a.dim, dk, a.scale, lane, a.dim);
+        store_row<float, DP>(sums + to_v + static_cast<long long>(key) * a.dim, dv, 1.0f, lane, a.dim);
     }
+}
+
+// dk (blockIdx.y = 0) and dv (1) from the parts' sums, four values a thread, in the parts' order
+template <typename T>
+__global__ __launch_bounds__(256) void parts_kernel(const AttentionArgs a)
+{
+    const Heads &y = blockIdx.y ? a.dv : a.dk;
+    const int quads = a.dim / 4;
+    const long long of_head = a.tokens * quads, all = a.kv_heads * of_head;
+    const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= all) return;
+    const f32x4 *sums = reinterpret_cast<const f32x4 *>(a.sums) + blockIdx.y * all + i;
+    f32x4 x = *sums;
+    for (int part = 1; part < a.parts; ++part) x += sums[part * 2 * all];
+    const long long head = i / of_head, in = i - head * of_head, token = in / quads;
+    T *row = static_cast<T *>(y.data) + token * y.row + head * y.head;
+    *reinterpret_cast<typename Operand<T>::quad *>(row + (in - token * quads) * 4) = to_quad(x, static_cast<T *>(nullptr));
 }
 
 template <typename T, int DP>
@@ -201,14 +273,33 @@ void enqueue(const AttentionArgs &a, hipStream_t stream)
 {
     const long long tiles = tile_numbers(a.tokens, a.sequences, kRows);
     hipLaunchKernelGGL((queries_kernel<T, DP>), dim3(static_cast<unsigned>(tiles * a.q_heads)), dim3(256), 0, stream, a);
-    hipLaunchKernelGGL((keys_kernel<T, DP>), dim3(static_cast<unsigned>(tiles * a.kv_heads)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((keys_kernel<T, DP>), dim3(static_cast<unsigned>(tiles * a.kv_heads * a.parts)), dim3(256), 0, stream, a);
+    if (a.parts > 1) {
+        const long long quads = a.tokens * a.kv_heads * (a.dim / 4);
+        hipLaunchKernelGGL((parts_kernel<T>), dim3(static_cast<unsigned>((quads + 255) / 256), 2), dim3(256), 0, stream, a);
+    }
 }
 
 }  // namespace
 
-long long attention_workspace_bytes(long long tokens, int q_heads)
+// Two workgroups have a compute unit: 512 run at once, and about four rounds of them even out what a
+// causal mask leaves to each.
+int attention_parts(long long tokens, int q_heads, int kv_heads, int sequences)
 {
-    return (tokens * q_heads * 4 + 15) / 16 * 16;
+    const int group = q_heads / kv_heads;
+    const long long workgroups = tile_numbers(tokens, sequences, kRows) * kv_heads;
+    int parts = 1;
+    while (parts < group && workgroups * parts < 2048)
+        do ++parts; while (group % parts);
+    return parts;
+}
+
+long long attention_delta_bytes(long long tokens, int q_heads) { return (tokens * q_heads * 4 + 15) / 16 * 16; }
+
+long long attention_workspace_bytes(long long tokens, int q_heads, int kv_heads, int dim, int sequences)
+{
+    const int parts = attention_parts(tokens, q_heads, kv_heads, sequences);
+    return attention_delta_bytes(tokens, q_heads) + (parts > 1 ? parts * 2ll * kv_heads * tokens * dim * 4 : 0);
 }
 
 hipError_t launch_attention_backward(const AttentionArgs &a, bool bf16, hipStream_t stream)

@@ -90,23 +90,23 @@ __device__ __forceinline__ int exchange(int row)
     return ((row & 2) << 1) | ((row >> 1) & 2) | ((row >> 3) & 1);
 }
 
-// Rows [first, first + Rows) of a matrix at `base` (row `first`) into a tile; rows from rows_left
-// on and chunks from chunks_left on are zeros.  stride: bytes.
+// Rows of a matrix from `base` on into a tile; rows from rows_left on and chunks from chunks_left on
+// are zeros (rows_left may be negative).  stride: bytes.
 template <int Rows, int Chunks, int Waves>
 __device__ __forceinline__ void stage_rows(char *tile, const char *base, long long stride, int rows_left,
                                            int chunks_left, int wave, int lane)
 {
-    static_assert(Rows * Chunks % (64 * Waves) == 0, "whole loads");
-    const unsigned bytes = rows_left <= 0 || chunks_left <= 0 ? 0u
-        : static_cast<unsigned>((min(rows_left, Rows) - 1) * stride + min(chunks_left, Chunks) * 16);
-    const __amdgpu_buffer_rsrc_t r = buffer(base, bytes);
+    constexpr int RowsALoad = Waves * 64 / Chunks;
+    static_assert(Rows % RowsALoad == 0 && (RowsALoad % 16 == 0 || Chunks > 8), "loads of whole rows, the same exchange in each");
+    const int rows = min(max(rows_left, 0), Rows);
+    const unsigned step = static_cast<unsigned>(stride);
+    const __amdgpu_buffer_rsrc_t r = buffer(base, rows ? (rows - 1) * step + chunks_left * 16 : 0u);
+    const int id = wave * 64 + lane, row = id / Chunks;
 #pragma unroll
-    for (int s = 0; s < Rows * Chunks / 64 / Waves; ++s) {
-        const int piece = s * Waves + wave;
-        const int id = piece * 64 + lane;
-        const int row = id / Chunks, chunk = (id % Chunks) ^ exchange<Chunks>(row);
-        const unsigned at = static_cast<unsigned>(row * static_cast<unsigned>(stride)) + chunk * 16;
-        load_lds16(r, tile + piece * 1024, chunk < chunks_left ? at : kOutside);
+    for (int s = 0; s < Rows / RowsALoad; ++s) {
+        const int chunk = (id % Chunks) ^ exchange<Chunks>(row + s * RowsALoad);
+        const unsigned at = chunk < chunks_left ? row * step + chunk * 16 : kOutside;
+        load_lds16(r, tile + (s * Waves + wave) * 1024, at + s * RowsALoad * step);
     }
 }
 

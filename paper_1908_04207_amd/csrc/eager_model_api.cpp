@@ -182,8 +182,9 @@ int eager_attention(int dtype, const eager_packed *shape, const eager_heads *q, 
 
 int eager_attention_workspace_bytes(int dtype, const eager_packed *shape, int64_t *bytes)
 {
-    if (!valid_dtype(dtype) || !valid_shape(shape) || !bytes) return EAGER_EINVAL;
-    *bytes = eager::attention_workspace_bytes(shape->tokens, shape->q_heads);
+    if (!valid_dtype(dtype) || !valid_shape(shape) || shape->sequences < 1 || !bytes) return EAGER_EINVAL;
+    *bytes = eager::attention_workspace_bytes(shape->tokens, shape->q_heads, shape->kv_heads, shape->head_dim,
+                                              shape->sequences);
     return EAGER_OK;
 }
 
@@ -198,13 +199,16 @@ int eager_attention_backward(int dtype, const eager_packed *shape, const eager_h
     for (const eager_heads *h : {dout, dq, dk, dv})
         if (!valid_heads(h, dtype, shape)) return EAGER_EINVAL;
     if (a.tokens == 0) return EAGER_OK;
-    if (!aligned(workspace, 16) || workspace_bytes < eager::attention_workspace_bytes(a.tokens, a.q_heads))
+    if (!aligned(workspace, 16) || 
+        workspace_bytes < eager::attention_workspace_bytes(a.tokens, a.q_heads, a.kv_heads, a.dim, a.sequences))
         return EAGER_EINVAL;
     a.dout = heads(dout);
     a.dq = heads(dq);
     a.dk = heads(dk);
     a.dv = heads(dv);
     a.delta = static_cast<float *>(workspace);
+    a.sums = a.delta + eager::attention_delta_bytes(a.tokens, a.q_heads) / 4;
+    a.parts = eager::attention_parts(a.tokens, a.q_heads, a.kv_heads, a.sequences);
     return status_of(eager::launch_attention_backward(a, dtype == EAGER_BF16, static_cast<hipStream_t>(stream)));
 }
 

@@ -20,35 +20,61 @@ struct Tile {
 
 __device__ __forceinline__ int segment_start(const int *cu, int sequences, int tokens, int i)
 {
-    if (i == 0) return 0;
-    if (i > sequences + 1) return tokens;
-    return min(max(cu[i - 1], 0), tokens);
+    const int bound = cu[min(max(i - 1, 0), sequences)];
+    return i == 0 ? 0 : i > sequences + 1 ? tokens : min(max(bound, 0), tokens);
 }
 
-// Every wavefront searches for itself, 64 candidates at a time.
+// Every wavefront searches for itself, 64 candidates at a time; the last step's candidates are the
+// bounds, so up to 62 sequences take one trip to memory.
 template <int Rows>
 __device__ __forceinline__ Tile find_tile(const int *cu, int sequences, int tokens, int number)
 {
     const int lane = threadIdx.x & 63;
     int lo = 0, count = sequences + 2;
-    while (count > 1) {
+    Tile t;
+    for (;;) {
         const int step = (count + 63) >> 6;
         const int i = lo + lane * step;
-        const bool below = lane * step < count && segment_start(cu, sequences, tokens, i) / Rows + i <= number;
+        const int start = segment_start(cu, sequences, tokens, i), next = segment_start(cu, sequences, tokens, i + 1);
+        const bool below = lane * step < count && start / Rows + i <= number;
         const int k = max(__popcll(__ballot(below)) - 1, 0);
         lo += k * step;
+        if (step == 1) {
+            t.begin = __builtin_amdgcn_readlane(start, k);
+            t.end = max(t.begin, __builtin_amdgcn_readlane(next, k));
+            break;
+        }
         count = min(step, count - k * step);
     }
-    Tile t;
     t.segment = __builtin_amdgcn_readfirstlane(lo);
-    t.begin = __builtin_amdgcn_readfirstlane(segment_start(cu, sequences, tokens, lo));
-    t.end = __builtin_amdgcn_readfirstlane(max(t.begin, segment_start(cu, sequences, tokens, lo + 1)));
-    const long long first = t.begin + static_cast<long long>(number - (t.begin / Rows + lo)) * Rows;
-    t.first = __builtin_amdgcn_readfirstlane(static_cast<int>(min(max(first, 0ll), static_cast<long long>(t.end))));
+    const long long first = t.begin + static_cast<long long>(number - (t.begin / Rows + t.segment)) * Rows;
+    t.first = static_cast<int>(min(max(first, static_cast<long long>(t.begin)), static_cast<long long>(t.end)));
     return t;
 }
 
 inline long long tile_numbers(long long tokens, int sequences, int rows) { return tokens / rows + sequences + 2; }
+
+// The larger of, and the sum over, a lane and the one 32 away.
+__device__ __forceinline__ void both_halves(float &x, float &y)
+{
+    const unsigned a = __builtin_bit_cast(unsigned, x);
+    const auto p = __builtin_amdgcn_permlane32_swap(a, a, false, false);
+    const unsigned low = p[0], high = p[1];     // a cast of p[1] itself would give p[0]
+    x = __builtin_bit_cast(float, low);
+    y = __builtin_bit_cast(float, high);
+}
+__device__ __forceinline__ float both_max(float x)
+{
+    float y;
+    both_halves(x, y);
+    return fmaxf(x, y);
+}
+__device__ __forceinline__ float both_sum(float x)
+{
+    float y;
+    both_halves(x, y);
+    return x + y;
+}
 
 // A lane's operand of one row straight from global memory, k step `step`; zeros where !there and
 // beyond the head's dim elements.
