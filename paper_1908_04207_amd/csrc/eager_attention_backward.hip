@@ -14,6 +14,8 @@ namespace {
 
 constexpr int kRows = 128;           // queries (keys) of a workgroup: 32 a wavefront
 constexpr int kTile = 64;            // keys (queries) of a tile
+// How many halves of a tile are unrolled: with long heads two of them side by side do not fit the registers.
+template <typename T, int DP> constexpr int kHalves = DP * sizeof(T) > 128 ? 1 : 2;
 
 template <typename T, int DP>
 __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void queries_kernel(const AttentionArgs a)
@@ -53,8 +55,12 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void queries_ke
     delta = both_sum(delta);
     float lse = 0.0f;
     if (there) {
-        lse = a.lse[head * a.tokens + row] * kLog2e;
-        if (lane < 32) a.delta[head * a.tokens + row] = delta;
+        lse = a.lse[head * a.tokens + row];
+        if (lane < 32) {                                // what keys_kernel's sums begin with
+            a.delta[head * a.tokens + row] = -delta;
+            a.start[head * a.tokens + row] = -lse / a.scale;
+        }
+        lse *= kLog2e;
     }
 
     const char *k_base = reinterpret_cast<const char *>(static_cast<const T *>(a.k.data) + kv_head * a.k.head);
@@ -73,7 +79,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void queries_ke
         wait_loads();
         __syncthreads();
         stage(key0 + kTile, next_k, next_v);            // beyond the sequence: zeros
-#pragma unroll
+#pragma unroll kHalves<T, DP>
         for (int b = 0; b < 2; ++b) {
             if (key0 + 32 * b >= wave_row + 32) continue;
             f32x16 s = {}, dp = {};
@@ -169,8 +175,8 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void keys_kerne
         const char *g = reinterpret_cast<const char *>(static_cast<const T *>(a.dout.data) + head * a.dout.head) + next_row * g_stride;
         stage_rows<kTile, Chunks, 4>(q_tile, q, q_stride, left, chunks, wave, lane);
         stage_rows<kTile, Chunks, 4>(g_tile, g, g_stride, left, chunks, wave, lane);
-        // rows beyond the sequence: zeros, with which P = 1, but dO and dP - delta are zeros too
-        const float *per_row = (wave & 1 ? a.delta : a.lse) + head * a.tokens + next_row;
+        // -lse / scale and -delta; rows beyond the sequence: zeros, with which P = 1, but dO and dP - delta are zeros too
+        const float *per_row = (wave & 1 ? a.delta : a.start) + head * a.tokens + next_row;
         if (wave < 2)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(per_row, min(kTile, left) * 4),
                                                      (__attribute__((address_space(3))) void *)(rows[wave]), 4,
@@ -190,21 +196,25 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void keys_kerne
         wait_loads();
         __syncthreads();
         stage(next_q, next_g, next_rows);
-#pragma unroll
+#pragma unroll kHalves<T, DP>
         for (int b = 0; b < 2; ++b) {
-            if (row0 + 32 * b + 31 < wave_key) continue;        // all rows come before the wavefront's keys
-            f32x16 s = {}, dp = {};
+            if (row0 + 32 * b + 31 < wave_key) continue;        // all queries come before the wavefront's keys
+            // the sums begin with -lse / scale and -delta: P = exp(scale s), dS = P dp
+            f32x16 s, dp;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int at = 32 * b + 8 * r + 4 * (lane >> 5);
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(&rows[0][at]), y = *reinterpret_cast<const f32x4 *>(&rows[1][at]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[4 * r + i] = x[i], dp[4 * r + i] = y[i];
+            }
 #pragma unroll
             for (int i = 0; i < Steps; ++i) {
                 s = mma(read_rows<Chunks>(q_tile, 32 * b, i, lane, type), k[i], s);
                 dp = mma(read_rows<Chunks>(g_tile, 32 * b, i, lane, type), v[i], dp);
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const f32x4 lse = *reinterpret_cast<const f32x4 *>(&rows[0][32 * b + 8 * r + 4 * (lane >> 5)]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[4 * r + i] = exp2_fast(fmaf(s[4 * r + i], c, -lse[i] * kLog2e));
-            }
+            for (int i = 0; i < 16; ++i) s[i] = exp2_fast(s[i] * c);
             if (row0 + 32 * b < wave_key + 31) {
                 const int seen = key - row0 - 32 * b - 4 * (lane >> 5);
 #pragma unroll
@@ -212,12 +222,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void keys_kerne
                     if (8 * (i >> 2) + (i & 3) < seen) s[i] = 0.0f;
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const f32x4 delta = *reinterpret_cast<const f32x4 *>(&rows[1][32 * b + 8 * r + 4 * (lane >> 5)]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    dp[4 * r + i] = s[4 * r + i] * (dp[4 * r + i] - delta[i]);
-            }
+            for (int i = 0; i < 16; ++i) dp[i] *= s[i];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const typename Operand<T>::frag p = as_operand<T>(s, h), ds = as_operand<T>(dp, h);
@@ -294,12 +299,12 @@ int attention_parts(long long tokens, int q_heads, int kv_heads, int sequences)
     return parts;
 }
 
-long long attention_delta_bytes(long long tokens, int q_heads) { return (tokens * q_heads * 4 + 15) / 16 * 16; }
+long long attention_row_bytes(long long tokens, int q_heads) { return (tokens * q_heads * 4 + 15) / 16 * 16; }
 
 long long attention_workspace_bytes(long long tokens, int q_heads, int kv_heads, int dim, int sequences)
 {
     const int parts = attention_parts(tokens, q_heads, kv_heads, sequences);
-    return attention_delta_bytes(tokens, q_heads) + (parts > 1 ? parts * 2ll * kv_heads * tokens * dim * 4 : 0);
+    return 2 * attention_row_bytes(tokens, q_heads) + (parts > 1 ? parts * 2ll * kv_heads * tokens * dim * 4 : 0);
 }
 
 hipError_t launch_attention_backward(const AttentionArgs &a, bool bf16, hipStream_t stream)

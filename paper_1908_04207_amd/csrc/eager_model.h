@@ -31,7 +31,7 @@ struct NormRopeArgs {
 struct AttentionArgs {
     Heads q, k, v, out, dout, dq, dk, dv;
     float *lse;
-    float *delta;                    // backward: sum(dout * out) per row and head
+    float *delta, *start;            // backward, per row and head: -sum(dout * out), -lse / scale
     float *sums;                     // backward: dk, dv of each part, where there is more than one
     int parts;
     const int *cu;
@@ -60,7 +60,7 @@ int norm_rope_tokens_per_block(int heads);
 hipError_t launch_attention(const AttentionArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_attention_backward(const AttentionArgs &a, bool bf16, hipStream_t stream);
 int attention_parts(long long tokens, int q_heads, int kv_heads, int sequences);
-long long attention_delta_bytes(long long tokens, int q_heads);
+long long attention_row_bytes(long long tokens, int q_heads);
 long long attention_workspace_bytes(long long tokens, int q_heads, int kv_heads, int dim, int sequences);
 
 hipError_t launch_cross_entropy(const CrossEntropyArgs &a, bool bf16, hipStream_t stream);

@@ -207,7 +207,8 @@ int eager_attention_backward(int dtype, const eager_packed *shape, const eager_h
     a.dk = heads(dk);
     a.dv = heads(dv);
     a.delta = static_cast<float *>(workspace);
-    a.sums = a.delta + eager::attention_delta_bytes(a.tokens, a.q_heads) / 4;
+    a.start = a.delta + eager::attention_row_bytes(a.tokens, a.q_heads) / 4;
+    a.sums = a.start + eager::attention_row_bytes(a.tokens, a.q_heads) / 4;
     a.parts = eager::attention_parts(a.tokens, a.q_heads, a.kv_heads, a.sequences);
     return status_of(eager::launch_attention_backward(a, dtype == EAGER_BF16, static_cast<hipStream_t>(stream)));
 }
