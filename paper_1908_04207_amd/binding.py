@@ -169,9 +169,14 @@ class _CtypesOnly:
         return NotImplemented
 
     plan_participation = plan_quorum = round = step = stash = views = _unknown
+    qk_norm_rope = attention = cross_entropy = _unknown
 
     @staticmethod
     def streams(*_):
+        pass
+
+    @staticmethod
+    def bind_model(*_):
         pass
 
 

@@ -9,7 +9,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
-#include "../../include/eager.h"
+#include "../../include/eager_model.h"
 
 #include <limits.h>
 #include <stdint.h>
@@ -332,6 +332,277 @@ PyObject *py_views(PyObject *, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLong(st);
 }
 
+// ---- the operators of a transformer step: torch tensors in, checked as model_ops checks them; any
+// other form than the usual one (and any refusal) is left to model_ops
+
+struct ModelEntry {
+    decltype(&eager_qk_norm_rope) norm;
+    decltype(&eager_qk_norm_rope_workspace_bytes) norm_bytes;
+    decltype(&eager_qk_norm_rope_backward) norm_backward;
+    decltype(&eager_attention) attention;
+    decltype(&eager_attention_workspace_bytes) attention_bytes;
+    decltype(&eager_attention_backward) attention_backward;
+    decltype(&eager_cross_entropy) loss;
+    decltype(&eager_cross_entropy_workspace_bytes) loss_bytes;
+    decltype(&eager_cross_entropy_backward) loss_backward;
+};
+ModelEntry model;
+PyObject *t_f32, *t_bf16, *t_i32, *t_i64, *new_workspace;
+PyObject *s_shape, *s_stride, *s_dtype, *s_get_device;
+
+struct Tensor {
+    void *data;
+    int dims;
+    int64_t size[3], stride[3];
+    PyObject *type;                                         // compared only
+    long device;
+};
+
+bool as_sizes(PyObject *v, int *dims, int64_t (&to)[3])
+{
+    bool ok = v && PyTuple_Check(v) && PyTuple_GET_SIZE(v) >= 1 && PyTuple_GET_SIZE(v) <= 3;
+    if (ok) {
+        *dims = static_cast<int>(PyTuple_GET_SIZE(v));
+        for (int i = 0; ok && i < *dims; ++i) {
+            PyObject *e = PyTuple_GET_ITEM(v, i);
+            ok = PyLong_Check(e);
+            if (ok) to[i] = PyLong_AsLongLong(e);
+        }
+    }
+    Py_XDECREF(v);
+    return ok && !PyErr_Occurred();
+}
+
+bool as_tensor(PyObject *x, Tensor *t)
+{
+    if (x == Py_None || PyLong_Check(x) || !as_pointer(x, &t->data)) return false;
+    int dims;
+    if (!as_sizes(PyObject_GetAttr(x, s_shape), &t->dims, t->size) ||
+        !as_sizes(PyObject_CallMethodNoArgs(x, s_stride), &dims, t->stride) || dims != t->dims)
+        return false;
+    t->type = PyObject_GetAttr(x, s_dtype);
+    if (!t->type) return false;
+    Py_DECREF(t->type);
+    PyObject *d = PyObject_CallMethodNoArgs(x, s_get_device);
+    if (!d) return false;
+    t->device = PyLong_Check(d) ? PyLong_AsLong(d) : -1;
+    Py_DECREF(d);
+    return t->device >= 0;
+}
+
+bool vector_of(const Tensor &t, PyObject *type, long device, int64_t n)
+{
+    return t.dims == 1 && t.type == type && t.device == device && t.size[0] == n && (n < 2 || t.stride[0] == 1);
+}
+
+bool table_of(const Tensor &t, long device, int64_t rows, int64_t columns)
+{
+    return t.dims == 2 && t.type == t_f32 && t.device == device && t.size[0] == rows && t.size[1] == columns &&
+           (columns < 2 || t.stride[1] == 1) && (rows < 2 || t.stride[0] == columns);
+}
+
+// [tokens, heads, head_dim] of the same type on the same device, heads contiguous
+bool heads_like(const Tensor &t, const Tensor &like, int64_t heads, eager_heads *h)
+{
+    if (t.dims != 3 || t.type != like.type || t.device != like.device || t.size[0] != like.size[0] ||
+        t.size[1] != heads || t.size[2] != like.size[2] || (t.size[2] > 1 && t.stride[2] != 1))
+        return false;
+    *h = {t.data, t.stride[0], t.stride[1]};
+    return true;
+}
+
+bool as_dtype(const Tensor &t, int *dtype)
+{
+    *dtype = t.type == t_bf16 ? EAGER_BF16 : EAGER_F32;
+    return t.type == t_bf16 || t.type == t_f32;
+}
+
+bool fits_int(int64_t x) { return x >= 0 && x <= INT_MAX; }
+
+// the current stream, if the current device is the tensors'
+bool stream_of(const Tensor &t, void **stream)
+{
+    if (!get_stream) return false;
+    PyObject *dev = PyObject_CallNoArgs(get_device);
+    if (!dev) return false;
+    const bool here = PyLong_Check(dev) && PyLong_AsLong(dev) == t.device;
+    PyObject *v = here ? PyObject_CallOneArg(get_stream, dev) : nullptr;
+    Py_DECREF(dev);
+    if (!v) return false;
+    const bool ok = PyLong_Check(v) && as_pointer(v, stream);
+    Py_DECREF(v);
+    return ok;
+}
+
+// a tensor of at least n bytes next to `like`, released when the call has been enqueued
+struct Workspace {
+    PyObject *object = nullptr;
+    void *data = nullptr;
+    ~Workspace() { Py_XDECREF(object); }
+    bool take(int64_t n, PyObject *like)
+    {
+        PyObject *bytes = PyLong_FromLongLong(n);
+        if (!bytes) return false;
+        object = PyObject_CallFunctionObjArgs(new_workspace, bytes, like, nullptr);
+        Py_DECREF(bytes);
+        return object && as_pointer(object, &data);
+    }
+};
+
+// qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps, q_out, k_out) or, with the gradients of the outputs,
+// (q, k, wq, wk, cos, sin, positions, eps, dq_out, dk_out, dq, dk, dwq, dwk)
+PyObject *py_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Tensor q, k, wq, wk, c, s, pos, y[4], dw[2];
+    eager_heads hq, hk, h[4];
+    int dtype;
+    float eps;
+    void *stream;
+    const bool backward = n == 14;
+    if ((n != 10 && n != 14) || !t_f32 || !as_tensor(a[0], &q) || !as_tensor(a[1], &k) || !as_tensor(a[2], &wq) ||
+        !as_tensor(a[3], &wk) || !as_tensor(a[4], &c) || !as_tensor(a[5], &s) || !as_tensor(a[6], &pos) || !as_float(a[7], &eps))
+        return other_form();
+    for (int i = 0; i < (backward ? 4 : 2); ++i)
+        if (!as_tensor(a[8 + i], &y[i])) return other_form();
+    if (q.dims != 3 || k.dims != 3 || !as_dtype(q, &dtype) || !heads_like(q, q, q.size[1], &hq) ||
+        !heads_like(k, q, k.size[1], &hk) || !vector_of(wq, q.type, q.device, q.size[2]) ||
+        !vector_of(wk, q.type, q.device, q.size[2]) || !table_of(c, q.device, c.size[0], q.size[2] / 2) ||
+        !table_of(s, q.device, c.size[0], q.size[2] / 2) || !vector_of(pos, t_i32, q.device, q.size[0]) ||
+        !fits_int(q.size[1]) || !fits_int(k.size[1]) || !fits_int(q.size[2]) || !stream_of(q, &stream))
+        return other_form();
+    for (int i = 0; i < (backward ? 4 : 2); ++i)
+        if (!heads_like(y[i], q, i % 2 ? k.size[1] : q.size[1], &h[i])) return other_form();
+    const eager_packed shape = {q.size[0], static_cast<int32_t>(q.size[1]), static_cast<int32_t>(k.size[1]),
+                                static_cast<int32_t>(q.size[2]), 0, nullptr};
+    const eager_rotation rot = {static_cast<float *>(c.data), static_cast<float *>(s.data), static_cast<int32_t *>(pos.data),
+                                c.size[0]};
+    int st;
+    if (!backward) {
+        Py_BEGIN_ALLOW_THREADS
+        st = model.norm(dtype, &shape, &hq, &hk, wq.data, wk.data, &rot, eps, &h[0], &h[1], stream);
+        Py_END_ALLOW_THREADS
+    } else {
+        int64_t bytes;
+        Workspace w;
+        if (!as_tensor(a[12], &dw[0]) || !as_tensor(a[13], &dw[1]) || !vector_of(dw[0], q.type, q.device, q.size[2]) ||
+            !vector_of(dw[1], q.type, q.device, q.size[2]) || model.norm_bytes(dtype, &shape, &bytes) != EAGER_OK ||
+            !w.take(bytes, a[0]))
+            return other_form();
+        Py_BEGIN_ALLOW_THREADS
+        st = model.norm_backward(dtype, &shape, &h[0], &h[1], &hq, &hk, wq.data, wk.data, &rot, eps, &h[2], &h[3],
+                                 dw[0].data, dw[1].data, w.data, bytes, stream);
+        Py_END_ALLOW_THREADS
+    }
+    return st == EAGER_EINVAL ? other_form() : PyLong_FromLong(st);
+}
+
+// attention(q, k, v, cu_seqlens, scale, out, lse) or (q, k, v, cu_seqlens, scale, out, lse, dout, dq, dk, dv)
+PyObject *py_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Tensor q, k, v, cu, out, lse, g[4];
+    eager_heads hq, hk, hv, ho, h[4];
+    int dtype;
+    float scale;
+    void *stream;
+    const bool backward = n == 11;
+    if ((n != 7 && n != 11) || !t_f32 || !as_tensor(a[0], &q) || !as_tensor(a[1], &k) || !as_tensor(a[2], &v) ||
+        !as_tensor(a[3], &cu) || !as_float(a[4], &scale) || !as_tensor(a[5], &out) || !as_tensor(a[6], &lse))
+        return other_form();
+    if (q.dims != 3 || k.dims != 3 || !as_dtype(q, &dtype) || !heads_like(q, q, q.size[1], &hq) ||
+        !heads_like(k, q, k.size[1], &hk) || !heads_like(v, q, k.size[1], &hv) || !heads_like(out, q, q.size[1], &ho) ||
+        cu.dims != 1 || cu.size[0] < 2 || !vector_of(cu, t_i32, q.device, cu.size[0]) ||
+        !table_of(lse, q.device, q.size[1], q.size[0]) || !fits_int(q.size[1]) || !fits_int(k.size[1]) ||
+        !fits_int(q.size[2]) || !fits_int(cu.size[0]) || !stream_of(q, &stream))
+        return other_form();
+    const eager_packed shape = {q.size[0], static_cast<int32_t>(q.size[1]), static_cast<int32_t>(k.size[1]),
+                                static_cast<int32_t>(q.size[2]), static_cast<int32_t>(cu.size[0] - 1),
+                                static_cast<int32_t *>(cu.data)};
+    int st;
+    if (!backward) {
+        Py_BEGIN_ALLOW_THREADS
+        st = model.attention(dtype, &shape, &hq, &hk, &hv, scale, &ho, static_cast<float *>(lse.data), stream);
+        Py_END_ALLOW_THREADS
+    } else {
+        for (int i = 0; i < 4; ++i)
+            if (!as_tensor(a[7 + i], &g[i]) || !heads_like(g[i], q, i < 2 ? q.size[1] : k.size[1], &h[i])) return other_form();
+        int64_t bytes;
+        Workspace w;
+        if (model.attention_bytes(dtype, &shape, &bytes) != EAGER_OK || !w.take(bytes, a[0])) return other_form();
+        Py_BEGIN_ALLOW_THREADS
+        st = model.attention_backward(dtype, &shape, &hq, &hk, &hv, &ho, static_cast<float *>(lse.data), &h[0], scale, &h[1],
+                                      &h[2], &h[3], w.data, bytes, stream);
+        Py_END_ALLOW_THREADS
+    }
+    return st == EAGER_EINVAL ? other_form() : PyLong_FromLong(st);
+}
+
+bool rows_like(const Tensor &t, const Tensor &like)
+{
+    return t.dims == 2 && t.type == like.type && t.device == like.device && t.size[0] == like.size[0] &&
+           t.size[1] == like.size[1] && (t.size[1] < 2 || t.stride[1] == 1) &&
+           (t.size[0] < 2 || t.stride[0] == like.stride[0]);
+}
+
+// cross_entropy(x, w, target, loss, lse) or (x, w, target, lse, dloss, dx, dw), dx or dw None: not wanted
+PyObject *py_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Tensor x, w, target, one, two, dx, dw;
+    int dtype;
+    int64_t bytes;
+    void *stream;
+    const bool backward = n == 7;
+    if ((n != 5 && n != 7) || !t_f32 || !as_tensor(a[0], &x) || !as_tensor(a[1], &w) || !as_tensor(a[2], &target) ||
+        !as_tensor(a[3], &one) || !as_tensor(a[4], &two))
+        return other_form();
+    if (x.dims != 2 || w.dims != 2 || !as_dtype(x, &dtype) || !rows_like(x, x) || !rows_like(w, w) || w.type != x.type ||
+        w.device != x.device || w.size[1] != x.size[1] || !vector_of(target, t_i64, x.device, x.size[0]) ||
+        !vector_of(one, t_f32, x.device, x.size[0]) || !vector_of(two, t_f32, x.device, x.size[0]) || !fits_int(x.size[1]) ||
+        !fits_int(w.size[0]) || !stream_of(x, &stream))
+        return other_form();
+    dx.data = dw.data = nullptr;
+    if (backward && ((a[5] != Py_None && (!as_tensor(a[5], &dx) || !rows_like(dx, x))) ||
+                     (a[6] != Py_None && (!as_tensor(a[6], &dw) || !rows_like(dw, w)))))
+        return other_form();
+    const eager_projection shape = {x.size[0], static_cast<int32_t>(x.size[1]), static_cast<int32_t>(w.size[0]),
+                                    x.size[0] > 1 ? x.stride[0] : x.size[1], w.size[0] > 1 ? w.stride[0] : w.size[1]};
+    Workspace space;
+    if (model.loss_bytes(dtype, &shape, backward, &bytes) != EAGER_OK || !space.take(bytes, a[0])) return other_form();
+    const int64_t *t = static_cast<int64_t *>(target.data);
+    float *p = static_cast<float *>(one.data), *q = static_cast<float *>(two.data);
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = backward ? model.loss_backward(dtype, &shape, x.data, w.data, t, p, q, dx.data, dw.data, space.data, bytes, stream)
+                  : model.loss(dtype, &shape, x.data, w.data, t, p, q, space.data, bytes, stream);
+    Py_END_ALLOW_THREADS
+    return st == EAGER_EINVAL ? other_form() : PyLong_FromLong(st);
+}
+
+// bind_model(addresses, (float32, bfloat16, int32, int64), workspace): workspace(n, like) gives a tensor
+PyObject *py_bind_model(PyObject *, PyObject *args)
+{
+    PyObject *addr, *space, *type[4];
+    if (!PyArg_ParseTuple(args, "O!(OOOO)O", &PyTuple_Type, &addr, &type[0], &type[1], &type[2], &type[3], &space)) return nullptr;
+    constexpr Py_ssize_t kN = sizeof(ModelEntry) / sizeof(void *);
+    if (PyTuple_GET_SIZE(addr) != kN) {
+        PyErr_SetString(PyExc_ValueError, "one address per entry point");
+        return nullptr;
+    }
+    void *p[kN];
+    for (Py_ssize_t i = 0; i < kN; ++i) {
+        p[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(addr, i));
+        if (!p[i]) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "entry point %zd is NULL", i);
+    }
+    __builtin_memcpy(&model, p, sizeof model);
+    PyObject **const to[4] = {&t_f32, &t_bf16, &t_i32, &t_i64};
+    for (int i = 0; i < 4; ++i) {
+        Py_INCREF(type[i]);
+        Py_XSETREF(*to[i], type[i]);
+    }
+    Py_INCREF(space);
+    Py_XSETREF(new_workspace, space);
+    Py_RETURN_NONE;
+}
+
 // bind(addresses, Plan, ctypes.Array)
 PyObject *py_bind(PyObject *, PyObject *args)
 {
@@ -382,8 +653,12 @@ PyMethodDef methods[] = {
     {"step", FAST(py_step), nullptr},
     {"stash", FAST(py_stash), nullptr},
     {"views", FAST(py_views), nullptr},
+    {"bind_model", py_bind_model, METH_VARARGS, nullptr},
+    {"qk_norm_rope", FAST(py_norm), nullptr},
+    {"attention", FAST(py_attention), nullptr},
+    {"cross_entropy", FAST(py_loss), nullptr},
     {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
@@ -391,6 +666,10 @@ PyMODINIT_FUNC PyInit__marshal(void)
 {
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-    if (!s_data_ptr || !s_cuda_stream) return nullptr;
-    return PyModule_Create(&module);
+    s_shape = PyUnicode_InternFromString("shape");
+    s_stride = PyUnicode_InternFromString("stride");
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_get_device = PyUnicode_InternFromString("get_device");
+    if (!s_data_ptr || !s_cuda_stream || !s_shape || !s_stride || !s_dtype || !s_get_device) return nullptr;
+    return PyModule_Create(&definition);
 }

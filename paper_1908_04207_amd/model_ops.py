@@ -6,6 +6,10 @@ workspaces, through torch's allocator) and call them.  Outputs that are given (g
 weights in a process's gradient arena, parts of one buffer) are written in place.  All calls go to
 the current stream, none of them waits.
 
+A small call runs for a few microseconds, so the usual forms (tensors as described, all on the
+current device) are checked and handed over by the extension module _marshal; whatever it does not
+take comes back as NotImplemented and is checked and refused, or called, here.
+
     q, k = qk_norm_rope(q, k, wq, wk, cos, sin, positions)
     out, lse = attention(q, k, v, cu_seqlens)
     loss, lse = cross_entropy(x, w, target)
@@ -14,6 +18,7 @@ each with its `_backward`, and `QKNormRope`, `Attention`, `CrossEntropy` for tor
 """
 from __future__ import annotations
 
+import ctypes
 import math
 from typing import Optional
 
@@ -48,6 +53,21 @@ def _expect(t, shape, dtype, device, name, contiguous=True):
 
 def _workspace(nbytes: int, like):
     return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=like.device)
+
+
+eb._marshal.bind_model(tuple(ctypes.cast(getattr(eb.lib, f), ctypes.c_void_p).value for f in (
+    "eager_qk_norm_rope", "eager_qk_norm_rope_workspace_bytes", "eager_qk_norm_rope_backward",
+    "eager_attention", "eager_attention_workspace_bytes", "eager_attention_backward",
+    "eager_cross_entropy", "eager_cross_entropy_workspace_bytes", "eager_cross_entropy_backward")),
+    (torch.float32, torch.bfloat16, torch.int32, torch.int64), _workspace)
+
+
+def _taken(status, what: str) -> bool:
+    """Whether the extension module has made the call."""
+    if status is NotImplemented:
+        return False
+    eb._status(status, what)
+    return True
 
 
 def _on(t):
@@ -90,11 +110,13 @@ def qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps: float = 1e-6, q_out=Non
     """RMS norm of every head of q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim]
     with gains wq, wk [head_dim], then the rotation by `positions` (int32 [tokens]) of the tables
     cos, sin (fp32 [positions, head_dim / 2]).  q_out, k_out may be q, k."""
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+    k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
+    if _taken(eb._marshal.qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps, q_out, k_out), "eager_qk_norm_rope"):
+        return q_out, k_out
     dtype = _dtype(q, k)
     shape = _heads_shape(q, k, wq, wk)
     rotation = _rotation(q, cos, sin, positions)
-    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
-    k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
     _expect(q_out, q.shape, q.dtype, q.device, "q_out", False)
     _expect(k_out, k.shape, k.dtype, k.device, "k_out", False)
     with _on(q):
@@ -106,13 +128,16 @@ def qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps: float = 1e-6, q_out=Non
 def qk_norm_rope_backward(dq_out, dk_out, q, k, wq, wk, cos, sin, positions, eps: float = 1e-6, dq=None, dk=None,
                           dwq=None, dwk=None):
     """Gradients dq, dk, dwq, dwk from those of the outputs; dq, dk may be dq_out, dk_out."""
-    dtype = _dtype(q, k, dq_out, dk_out)
-    shape = _heads_shape(q, k, wq, wk)
-    rotation = _rotation(q, cos, sin, positions)
     dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
     dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
     dwq = torch.empty_like(wq) if dwq is None else dwq
     dwk = torch.empty_like(wk) if dwk is None else dwk
+    if _taken(eb._marshal.qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps, dq_out, dk_out, dq, dk, dwq, dwk),
+              "eager_qk_norm_rope_backward"):
+        return dq, dk, dwq, dwk
+    dtype = _dtype(q, k, dq_out, dk_out)
+    shape = _heads_shape(q, k, wq, wk)
+    rotation = _rotation(q, cos, sin, positions)
     for t, like, name in ((dq_out, q, "dq_out"), (dk_out, k, "dk_out"), (dq, q, "dq"), (dk, k, "dk")):
         _expect(t, like.shape, q.dtype, q.device, name, False)
     for t, like, name in ((dwq, wq, "dwq"), (dwk, wk, "dwk")):
@@ -157,31 +182,39 @@ def attention(q, k, v, cu_seqlens, scale: Optional[float] = None, out=None):
     """Causal attention inside each of the packed sequences [cu_seqlens[s], cu_seqlens[s + 1])
     (int32, on the GPU) of q [tokens, q_heads, head_dim] over k, v [tokens, kv_heads, head_dim].
     Returns out, like q, and the log-sum-exp of every row's scores, fp32 [q_heads, tokens]."""
+    if q.dim() != 3:
+        _refuse(f"expected q [tokens, q_heads, head_dim], got {tuple(q.shape)}")
+    scale = 1.0 / math.sqrt(q.shape[2]) if scale is None else scale
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+    lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
+    if _taken(eb._marshal.attention(q, k, v, cu_seqlens, scale, out, lse), "eager_attention"):
+        return out, lse
     dtype = _dtype(q, k, v)
     shape = _packed_shape(q, k, v, cu_seqlens)
-    out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
     _expect(out, q.shape, q.dtype, q.device, "out", False)
-    lse = torch.empty(q.shape[1], q.shape[0], dtype=torch.float32, device=q.device)
     with _on(q):
-        eb.eager_attention(dtype, shape, eb.heads(q), eb.heads(k), eb.heads(v),
-                           1.0 / math.sqrt(q.shape[2]) if scale is None else scale, eb.heads(out), lse)
+        eb.eager_attention(dtype, shape, eb.heads(q), eb.heads(k), eb.heads(v), scale, eb.heads(out), lse)
     return out, lse
 
 
 def attention_backward(dout, q, k, v, out, lse, cu_seqlens, scale: Optional[float] = None, dq=None, dk=None, dv=None):
     """Gradients dq, dk, dv from dout and what the forward pass took and gave."""
-    dtype = _dtype(q, k, v, out, dout)
-    shape = _packed_shape(q, k, v, cu_seqlens)
+    if q.dim() != 3:
+        _refuse(f"expected q [tokens, q_heads, head_dim], got {tuple(q.shape)}")
+    scale = 1.0 / math.sqrt(q.shape[2]) if scale is None else scale
     dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if d is None else d
                   for d, x in ((dq, q), (dk, k), (dv, v)))
+    if _taken(eb._marshal.attention(q, k, v, cu_seqlens, scale, out, lse, dout, dq, dk, dv), "eager_attention_backward"):
+        return dq, dk, dv
+    dtype = _dtype(q, k, v, out, dout)
+    shape = _packed_shape(q, k, v, cu_seqlens)
     for t, like, name in ((dout, q, "dout"), (out, q, "out"), (dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
         _expect(t, like.shape, q.dtype, q.device, name, False)
     _expect(lse, (q.shape[1], q.shape[0]), torch.float32, q.device, "lse")
     nbytes = eb.eager_attention_workspace_bytes(dtype, shape)
     with _on(q):
         eb.eager_attention_backward(dtype, shape, eb.heads(q), eb.heads(k), eb.heads(v), eb.heads(out), lse,
-                                    eb.heads(dout), 1.0 / math.sqrt(q.shape[2]) if scale is None else scale,
-                                    eb.heads(dq), eb.heads(dk), eb.heads(dv), _workspace(nbytes, q), nbytes)
+                                    eb.heads(dout), scale, eb.heads(dq), eb.heads(dk), eb.heads(dv), _workspace(nbytes, q), nbytes)
     return dq, dk, dv
 
 
@@ -217,9 +250,12 @@ def cross_entropy(x, w, target):
     """Losses log sum exp(x w^T) - (x w^T)[target], fp32 [rows], and the log-sum-exps, of hidden
     states x [rows, width], projection w [vocab, width] and int64 targets; a negative target masks
     its row (loss 0).  No logits are kept."""
+    loss = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+    lse = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+    if _taken(eb._marshal.cross_entropy(x, w, target, loss, lse), "eager_cross_entropy"):
+        return loss, lse
     dtype = _dtype(x, w)
     shape = _projection(x, w, target)
-    loss, lse = (torch.empty(x.shape[0], dtype=torch.float32, device=x.device) for _ in range(2))
     nbytes = eb.eager_cross_entropy_workspace_bytes(dtype, shape, False)
     with _on(x):
         eb.eager_cross_entropy(dtype, shape, x, w, target, loss, lse, _workspace(nbytes, x), nbytes)
@@ -229,21 +265,21 @@ def cross_entropy(x, w, target):
 def cross_entropy_backward(dloss, x, w, target, lse, dx=None, dw=None, want=(True, True)):
     """Gradients dx, dw from those of the losses (fp32 [rows]); want: which of the two are formed.
     dx and dw are laid out like x and w."""
+    if dx is None and want[0]:
+        dx = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
+    if dw is None and want[1]:
+        dw = torch.empty_strided(w.shape, w.stride(), dtype=w.dtype, device=w.device)
+    if _taken(eb._marshal.cross_entropy(x, w, target, lse, dloss, dx, dw), "eager_cross_entropy_backward"):
+        return dx, dw
     dtype = _dtype(x, w)
     shape = _projection(x, w, target)
     _expect(dloss, target.shape, torch.float32, x.device, "dloss")
     _expect(lse, target.shape, torch.float32, x.device, "lse")
-
-    def like(t, given, name):
-        if given is None:
-            return torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device)
-        _expect(given, t.shape, t.dtype, t.device, name, False)
-        if given.stride(1) != 1 or (t.shape[0] > 1 and given.stride(0) != t.stride(0)):
-            _refuse(f"{name}: expected strides {t.stride()}, got {given.stride()}")
-        return given
-
-    dx = like(x, dx, "dx") if want[0] or dx is not None else None
-    dw = like(w, dw, "dw") if want[1] or dw is not None else None
+    for t, given, name in ((x, dx, "dx"), (w, dw, "dw")):
+        if given is not None:
+            _expect(given, t.shape, t.dtype, t.device, name, False)
+            if given.stride(1) != 1 or (t.shape[0] > 1 and given.stride(0) != t.stride(0)):
+                _refuse(f"{name}: expected strides {t.stride()}, got {given.stride()}")
     nbytes = eb.eager_cross_entropy_workspace_bytes(dtype, shape, True)
     with _on(x):
         eb.eager_cross_entropy_backward(dtype, shape, x, w, target, lse, dloss, dx, dw, _workspace(nbytes, x), nbytes)
