@@ -55,7 +55,7 @@ struct CrossEntropyArgs {
 hipError_t launch_norm_rope(const NormRopeArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_norm_rope_backward(const NormRopeArgs &a, bool bf16, hipStream_t stream);
 int norm_rope_blocks(long long tokens, int q_heads, int kv_heads);
-int norm_rope_tokens_per_block(int heads);
+int norm_rope_tokens_per_block(int heads, bool backward);
 
 hipError_t launch_attention(const AttentionArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_attention_backward(const AttentionArgs &a, bool bf16, hipStream_t stream);

@@ -67,7 +67,7 @@ bool fill(eager::NormRopeArgs &a, int dtype, const eager_packed *s, const eager_
     a.heads[0] = s->q_heads;
     a.heads[1] = s->kv_heads;
     a.dim = s->head_dim;
-    a.per_block = eager::norm_rope_tokens_per_block(s->q_heads + s->kv_heads);
+    a.per_block = eager::norm_rope_tokens_per_block(s->q_heads + s->kv_heads, false);
     a.eps = eps;
     a.inv_dim = 1.0f / static_cast<float>(s->head_dim);
     return true;
@@ -167,6 +167,7 @@ int eager_qk_norm_rope_backward(int dtype, const eager_packed *shape, const eage
     a.dw[0] = dwq;
     a.dw[1] = dwk;
     a.partials = static_cast<float *>(workspace);
+    a.per_block = eager::norm_rope_tokens_per_block(a.heads[0] + a.heads[1], true);
     a.blocks = eager::norm_rope_blocks(a.tokens, a.heads[0], a.heads[1]);
     return status_of(eager::launch_norm_rope_backward(a, dtype == EAGER_BF16, static_cast<hipStream_t>(stream)));
 }

@@ -184,21 +184,25 @@ __global__ __launch_bounds__(256) void norm_rope_backward_kernel(const NormRopeA
     }
 }
 
-// One workgroup a gain: 8 partial sums over the workgroups' records for every column, then their sum.
+// The workgroups' records of 16 columns of one gain (blockIdx.y): 64 sums over every 64th record, then
+// these in order.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_rope_gains_kernel(const NormRopeArgs a)
 {
-    __shared__ float part[8][128];
-    const int col = threadIdx.x % 128, slice = threadIdx.x / 128;
+    __shared__ float part[64][17];
+    const int in = threadIdx.x % 16, col = blockIdx.x * 16 + in, slice = threadIdx.x / 16;
     float sum = 0.0f;
-    if (col < a.dim)
-        for (int b = slice; b < a.blocks; b += 8)
-            sum += a.partials[(static_cast<long long>(b) * 2 + blockIdx.x) * a.dim + col];
-    part[slice][col] = sum;
+    if (col < a.dim) {
+        const float *p = a.partials + blockIdx.y * a.dim + col;
+#pragma unroll 8
+        for (int b = slice; b < a.blocks; b += 64) sum += p[static_cast<long long>(b) * 2 * a.dim];
+    }
+    part[slice][in] = sum;
     __syncthreads();
-    if (slice == 0 && col < a.dim) {
-        for (int i = 1; i < 8; ++i) sum += part[i][col];
-        static_cast<T *>(a.dw[blockIdx.x])[col] = static_cast<T>(sum);
+    if (threadIdx.x < 16 && col < a.dim) {
+#pragma unroll 8
+        for (int i = 1; i < 64; ++i) sum += part[i][in];
+        static_cast<T *>(a.dw[blockIdx.y])[col] = static_cast<T>(sum);
     }
 }
 
@@ -207,7 +211,7 @@ void enqueue(const NormRopeArgs &a, bool backward, hipStream_t stream)
 {
     if (backward) {
         if (a.blocks) hipLaunchKernelGGL((norm_rope_backward_kernel<T, V, G>), dim3(a.blocks), dim3(256), 0, stream, a);
-        hipLaunchKernelGGL((norm_rope_gains_kernel<T>), dim3(2), dim3(1024), 0, stream, a);
+        hipLaunchKernelGGL((norm_rope_gains_kernel<T>), dim3((a.dim + 15) / 16, 2), dim3(1024), 0, stream, a);
     } else {
         const long long blocks = (a.tokens + a.per_block - 1) / a.per_block;
         hipLaunchKernelGGL((norm_rope_kernel<T, V, G>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
@@ -236,16 +240,21 @@ hipError_t dispatch(const NormRopeArgs &a, bool bf16, bool backward, hipStream_t
 
 }  // namespace
 
-int norm_rope_tokens_per_block(int heads)
+// Heads a workgroup takes at a time: two a group of lanes with 4 lanes a head in the forward pass,
+// four in the backward pass, which keeps sums from turn to turn (8192 tokens of 20 heads of 64 in bf16:
+// forward 11.0 us, 12.6 with 256; backward 15.8 us, 20.6 with 128).
+int norm_rope_tokens_per_block(int heads, bool backward)
 {
-    return heads >= 128 ? 1 : 128 / heads;
+    const int want = backward ? 256 : 128;
+    return heads >= want ? 1 : want / heads;
 }
 
+// Workgroups of the backward pass: at most 1024, each with the same number of turns.
 int norm_rope_blocks(long long tokens, int q_heads, int kv_heads)
 {
-    const int per = norm_rope_tokens_per_block(q_heads + kv_heads);
-    const long long all = (tokens + per - 1) / per;
-    return static_cast<int>(all < 1024 ? all : 1024);
+    const int per = norm_rope_tokens_per_block(q_heads + kv_heads, true);
+    const long long all = (tokens + per - 1) / per, rounds = (all + 1023) / 1024;
+    return static_cast<int>(all ? (all + rounds - 1) / rounds : 0);
 }
 
 hipError_t launch_norm_rope(const NormRopeArgs &a, bool bf16, hipStream_t stream)
