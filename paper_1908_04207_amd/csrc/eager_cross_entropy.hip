@@ -166,10 +166,15 @@ __device__ __forceinline__ void product(const Product &p, int id, char *tile0, c
                 stage(here, t + 2);
                 read(next, 0, 0);
             }
+            decltype(operand(frag())) right[NI];
 #pragma unroll
-            for (int i = 0; i < MI; ++i)
+            for (int j = 0; j < NI; ++j) right[j] = operand(b[s & 1][j]);
 #pragma unroll
-                for (int j = 0; j < NI; ++j) c[i][j] = mma(a[s & 1][i], b[s & 1][j], c[i][j]);
+            for (int i = 0; i < MI; ++i) {
+                const auto left = operand(a[s & 1][i]);
+#pragma unroll
+                for (int j = 0; j < NI; ++j) c[i][j] = mma(left, right[j], c[i][j]);
+            }
             if constexpr (sizeof(T) == 2) {
                 if (s + 1 < Steps) spread<Products, Reads, 0>();
                 else spread<Products, Reads, Loads>();
