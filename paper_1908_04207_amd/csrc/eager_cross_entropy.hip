@@ -106,6 +106,15 @@ __device__ __forceinline__ typename Operand<T>::frag read_side(const char *tile,
     return read_columns<Rows * sizeof(T) / 16, sizeof(T) == 2 ? 2 : 31>(tile, row0, 16 * step, 8, 4, lane, static_cast<T *>(nullptr));
 }
 
+// A workgroup's tile, its wavefronts, and how many workgroups have a compute unit (by their shared memory).
+template <int A_, int B_, int WavesA_, int WavesB_, int OfUnit_>
+struct TileShape {
+    static constexpr int A = A_, B = B_, WavesA = WavesA_, WavesB = WavesB_, Threads = 64 * WavesA * WavesB, OfUnit = OfUnit_;
+};
+typedef TileShape<256, 256, 2, 4, 1> Large;
+typedef TileShape<128, 128, 2, 2, 2> Medium;
+typedef TileShape<128, 64, 4, 1, 3> Narrow;
+
 // The tile of workgroup `id`: workgroups id, id + 8, ... run on the same chiplet (one second-level
 // cache), so each chiplet gets a contiguous share of the tiles, in which 8 tiles of b are gone
 // through for every tile of a.
@@ -124,9 +133,10 @@ __device__ __forceinline__ void place(int id, int tiles_a, int tiles_b, int &til
 // turns: while one is multiplied, the next is on its way into the other.  A step's operands are
 // read while the step before is multiplied, the first step's of a tile during the last one of the
 // tile before, so the barrier between tiles stands in the shadow of matrix instructions.
-template <typename T, int BM, int BN, int WM, int WN, bool ColumnsA, bool ColumnsB, int Epi>
+template <typename T, typename Shape, bool ColumnsA, bool ColumnsB, int Epi>
 __device__ __forceinline__ void product(const Product &p, int id, char *tile0, char *tile1)
 {
+    constexpr int BM = Shape::A, BN = Shape::B, WM = Shape::WavesA, WN = Shape::WavesB;
     constexpr int Waves = WM * WN, MI = BM / WM / 32, NI = BN / WN / 32, Steps = kDepth<T> / 16;
     typedef typename Operand<T>::frag frag;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -337,27 +347,26 @@ __device__ __forceinline__ void product(const Product &p, int id, char *tile0, c
     }
 }
 
-constexpr int kTileA = 256, kTileB = 256, kThreads = 512;
-
 // Two arrays, so that the compiler knows a load into one apart from a read of the other.
-#define EAGER_TILES __shared__ __align__(1024) char tile0[(kTileA + kTileB) * 128]; \
-                    __shared__ __align__(1024) char tile1[(kTileA + kTileB) * 128]
+#define EAGER_TILES __shared__ __align__(1024) char tile0[(Shape::A + Shape::B) * 128]; \
+                    __shared__ __align__(1024) char tile1[(Shape::A + Shape::B) * 128]
 
-template <typename T, int Epi>
-__global__ __launch_bounds__(kThreads) void logits_kernel(const Product p)
+template <typename T, typename Shape, int Epi>
+__global__ __launch_bounds__(Shape::Threads) void logits_kernel(const Product p)
 {
     EAGER_TILES;
-    product<T, kTileA, kTileB, 2, 4, false, false, Epi>(p, blockIdx.x, tile0, tile1);
+    product<T, Shape, false, false, Epi>(p, blockIdx.x, tile0, tile1);
 }
 
 // dw and dx of a piece in one launch: what one leaves idle in its last round the other fills.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void gradients_kernel(const Product dw, const Product dx, int dw_tiles)
+// SumsOfDw: dw in slices of the rows, as sums in the workspace.
+template <typename T, typename Shape, bool SumsOfDw>
+__global__ __launch_bounds__(Shape::Threads) void gradients_kernel(const Product dw, const Product dx, int dw_tiles)
 {
     EAGER_TILES;
     const int id = blockIdx.x;
-    if (id < dw_tiles) product<T, kTileA, kTileB, 2, 4, true, true, kResult>(dw, id, tile0, tile1);
-    else product<T, kTileA, kTileB, 2, 4, true, false, kSums>(dx, id - dw_tiles, tile0, tile1);
+    if (id < dw_tiles) product<T, Shape, true, true, SumsOfDw ? kSums : kResult>(dw, id, tile0, tile1);
+    else product<T, Shape, true, false, kSums>(dx, id - dw_tiles, tile0, tile1);
 }
 
 __device__ __forceinline__ void join(float &top, float &sum, float2 q)
@@ -395,85 +404,147 @@ __global__ __launch_bounds__(1024) void rows_kernel(const float2 *stats, const f
     loss[row] = t < 0 ? 0.0f : t >= vocab ? __builtin_nanf("") : all - right[row];
 }
 
-// dx from the slices' sums
+// dx (and dw) from the slices' sums, four values a thread
+struct Sums {
+    const float *sums;       // [slices][rows_padded][width]
+    void *out;
+    long long stride, rows, rows_padded;
+    int slices;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void sums_kernel(const float *sums, T *dx, long long stride, long long rows, int width, int slices)
+__global__ __launch_bounds__(256) void sums_kernel(const Sums dx, const Sums dw, int width)
 {
+    const Sums &s = blockIdx.y ? dw : dx;
     const int quads = width / 4;
-    const long long n = rows * quads, i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= n) return;
-    f32x4 x = *reinterpret_cast<const f32x4 *>(sums + i * 4);
-    for (int s = 1; s < slices; ++s) x += *reinterpret_cast<const f32x4 *>(sums + (s * n + i) * 4);
-    *reinterpret_cast<typename Operand<T>::quad *>(dx + i / quads * stride + i % quads * 4) = to_quad(x, static_cast<T *>(nullptr));
+    const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= s.rows * quads) return;
+    const f32x4 *from = reinterpret_cast<const f32x4 *>(s.sums) + i;
+    f32x4 x = *from;
+#pragma unroll 4
+    for (int n = 1; n < s.slices; ++n) x += from[n * s.rows_padded * quads];
+    const long long row = i / quads, at = (i - row * quads) * 4;
+    *reinterpret_cast<typename Operand<T>::quad *>(static_cast<T *>(s.out) + row * s.stride + at) = to_quad(x, static_cast<T *>(nullptr));
 }
 
 long long round_up(long long x, long long to) { return (x + to - 1) / to * to; }
 
+// What a product costs in a shape of tiles: rounds of as many tiles as run at once, each a number of
+// steps of k (128 bytes) and what filling and emptying takes, in microseconds.
+struct Cost {
+    double step, rest;
+};
+template <typename Shape> Cost cost_of(int bytes);
+template <> Cost cost_of<Large>(int bytes) { return bytes == 2 ? Cost{1.4, 13} : Cost{5.9, 13}; }
+template <> Cost cost_of<Medium>(int bytes) { return bytes == 2 ? Cost{1.0, 9} : Cost{3.0, 9}; }
+template <> Cost cost_of<Narrow>(int bytes) { return bytes == 2 ? Cost{0.9, 6} : Cost{2.5, 6}; }
+
+template <typename Shape>
+double rounds_of(long long tiles) { return static_cast<double>((tiles + 256 * Shape::OfUnit - 1) / (256 * Shape::OfUnit)); }
+
+template <typename Shape>
+double logits_time(long long rows, int width, long long vocab, int bytes)
+{
+    const Cost c = cost_of<Shape>(bytes);
+    const long long tiles = round_up(rows, Shape::B) / Shape::B * (round_up(vocab, Shape::A) / Shape::A);
+    return rounds_of<Shape>(tiles) * (round_up(width, 128 / bytes) / (128 / bytes) * c.step + c.rest);
+}
+
+// dw and dx of a piece: their tiles follow each other, so only the last round is not full
+template <typename Shape>
+double gradients_time(long long rows, int width, long long live, int dw_slices, int dx_slices, int bytes)
+{
+    const Cost c = cost_of<Shape>(bytes);
+    const long long depth = 128 / bytes, tiles_w = round_up(width, Shape::A) / Shape::A;
+    const double dw = ((rows + depth - 1) / depth + dw_slices - 1) / dw_slices * c.step + c.rest;
+    const double dx = ((live + depth - 1) / depth + dx_slices - 1) / dx_slices * c.step + c.rest;
+    const long long dw_tiles = tiles_w * (round_up(live, Shape::B) / Shape::B) * dw_slices;
+    const long long dx_tiles = tiles_w * (round_up(rows, Shape::B) / Shape::B) * dx_slices;
+    // a slice's sums are written, read and, from the second piece on, read again
+    const double sums = (dx_slices * static_cast<double>(rows) + (dw_slices > 1 ? dw_slices * static_cast<double>(live) : 0)) * width * 12;
+    return std::max((dw_tiles * dw + dx_tiles * dx) / (256 * Shape::OfUnit) + std::max(dw, dx) / 2, std::max(dw, dx)) + sums / 5e6;
+}
+
+// How the backward pass is cut: vocabulary rows of a piece; slices that are summed apart, of a
+// piece for dx and, where there is one piece, of the rows for dw; the shapes of tiles.  The fastest cut by
+// the above is taken among those whose dl fit 512 MiB.
+enum { kLarge, kMedium, kNarrow };
+struct Cut {
+    long long rows_padded, piece;
+    int dx_slices, dw_slices, logits, gradients;
+};
+
+int logits_shape(long long rows, int width, long long vocab, int bytes)
+{
+    const double t[3] = {logits_time<Large>(rows, width, vocab, bytes), logits_time<Medium>(rows, width, vocab, bytes),
+                         logits_time<Narrow>(rows, width, vocab, bytes)};
+    return static_cast<int>(std::min_element(t, t + 3) - t);
+}
+
+constexpr int kSides[3][2] = {{Large::A, Large::B}, {Medium::A, Medium::B}, {Narrow::A, Narrow::B}};
+
+Cut cut_of(long long rows, int width, int vocab, int bytes)
+{
+    const long long padded = round_up(std::max(rows, 1ll), 256);
+    const long long fit = std::max(256ll, (1ll << 29) / bytes / padded / 256 * 256);
+    const long long fewest = (vocab + fit - 1) / fit;
+    Cut best = {padded, 0, 1, 1, 0, 0};
+    double least = 0;
+    for (long long n = fewest; n < fewest + 6; ++n) {
+        const long long piece = round_up((vocab + n - 1) / n, 256), pieces = (vocab + piece - 1) / piece;
+        const int shape = logits_shape(rows, width, piece, bytes);
+        const double logits = std::min({logits_time<Large>(rows, width, piece, bytes), logits_time<Medium>(rows, width, piece, bytes),
+                                        logits_time<Narrow>(rows, width, piece, bytes)});
+        for (int dx = 1; dx <= 32; dx *= 2)
+            for (int dw = 1; dw <= (pieces > 1 ? 1 : 32); dw *= 2)
+                for (int g = dw > 1 ? kMedium : kLarge; g <= kMedium; ++g) {
+                    const double one = g == kLarge ? gradients_time<Large>(rows, width, piece, dw, dx, bytes)
+                                                   : gradients_time<Medium>(rows, width, piece, dw, dx, bytes);
+                    const double last = std::max(0.2, static_cast<double>(vocab - (pieces - 1) * piece) / piece);
+                    const double cost = (logits + one) * (pieces > 1 ? pieces - 1 + last : 1);
+                    if (!best.piece || cost < least) {
+                        least = cost;
+                        best = {padded, piece, dx, dw, shape, g};
+                    }
+                }
+        if (piece == 256) break;
+    }
+    return best;
+}
+
 // Tiles of a product, and their number.
 template <typename T>
-int lay_out(Product &p)
+int lay_out(Product &p, int shape)
 {
-    p.tiles_a = static_cast<int>(round_up(p.a.rows, kTileA) / kTileA);
-    p.tiles_b = static_cast<int>(round_up(p.b.rows, kTileB) / kTileB);
+    p.tiles_a = static_cast<int>(round_up(p.a.rows, kSides[shape][0]) / kSides[shape][0]);
+    p.tiles_b = static_cast<int>(round_up(p.b.rows, kSides[shape][1]) / kSides[shape][1]);
     p.all_steps = static_cast<int>(round_up(std::max(p.a.k, p.b.k), kDepth<T>) / kDepth<T>);
     p.steps = (p.all_steps + p.slices - 1) / p.slices;
     return p.tiles_a * p.tiles_b * p.slices;
 }
 
-// How the backward pass is cut: vocabulary rows of a piece (a multiple of kTileA) and, for dx, slices
-// of a piece that are summed apart.  One workgroup has a compute unit, so a product takes as
-// long as its rounds of 256 tiles: k tiles each and about 8 more for filling and emptying (a tile
-// of k is 1.5 us, the rest of a logits tile about 12 us).  The cut with the least of that is taken among those
-// whose dl fit 512 MiB; 50257 x 1600 on 8191 rows: TODO figures.
-struct Cut {
-    long long piece;
-    int slices;
-};
-
-Cut cut(long long rows, int width, int vocab, int bytes)
+template <typename T, int Epi>
+void launch_logits(Product &p, int shape, hipStream_t stream)
 {
-    const long long depth = 128 / bytes, tiles_b = round_up(rows > 0 ? rows : 1, kTileB) / kTileB;
-    const long long tiles_v = round_up(vocab, kTileA) / kTileA, tiles_w = round_up(width, kTileA) / kTileA;
-    const long long fit = std::max(1ll, (1ll << 29) / bytes / (tiles_b * kTileB) / kTileA);
-    const long long fewest = (tiles_v + fit - 1) / fit;
-    auto rounds = [](long long tiles) { return (tiles + 255) / 256; };
-    Cut best = {};
-    double least = 0;
-    for (long long n = fewest; n < fewest + 8 && n <= tiles_v; ++n) {
-        const long long piece = (tiles_v + n - 1) / n, pieces = (tiles_v + piece - 1) / piece;
-        for (int slices = 1; slices <= 16; slices *= 2) {
-            double cost = 0;
-            for (long long i = 0; i < pieces; i += pieces > 1 ? pieces - 1 : 1) {      // the full ones, then the last
-                const long long tiles = i + 1 < pieces ? piece : tiles_v - piece * (pieces - 1);
-                const long long times = i + 1 < pieces ? pieces - 1 : 1;
-                const double dw = rows / depth + 8, dx = tiles * kTileA / depth / slices + 8;
-                const double both = tiles * tiles_w * dw + tiles_w * tiles_b * slices * dx;
-                cost += times * (rounds(tiles * tiles_b) * (width / depth + 8) + both / 256 + std::max(dw, dx) / 2 +
-                                 slices * static_cast<double>(rows) * width * 8 / 6e6);
-            }
-            if (!best.piece || cost < least) {
-                least = cost;
-                best = {piece * kTileA, slices};
-            }
-        }
-    }
-    return best;
+    const dim3 grid(lay_out<T>(p, shape));
+    if (shape == kLarge) hipLaunchKernelGGL((logits_kernel<T, Large, Epi>), grid, dim3(Large::Threads), 0, stream, p);
+    else if (shape == kMedium) hipLaunchKernelGGL((logits_kernel<T, Medium, Epi>), grid, dim3(Medium::Threads), 0, stream, p);
+    else hipLaunchKernelGGL((logits_kernel<T, Narrow, Epi>), grid, dim3(Narrow::Threads), 0, stream, p);
 }
 
 template <typename T>
 hipError_t forward(const CrossEntropyArgs &a, hipStream_t stream)
 {
+    const int shape = logits_shape(a.rows, a.width, a.vocab, sizeof(T));
+    const long long tiles = round_up(a.vocab, kSides[shape][0]) / kSides[shape][0];
     Product p = {};
     p.a = {a.w, a.w_stride, a.vocab, a.width};
     p.b = {a.x, a.x_stride, a.rows, a.width};
     p.slices = 1;
     p.live = a.vocab;
     p.target = a.target;
-    const long long tiles = round_up(a.vocab, kTileA) / kTileA;
     p.stats = reinterpret_cast<float2 *>(a.workspace);
     p.right = reinterpret_cast<float *>(p.stats + tiles * a.rows);
-    const int tiles_all = lay_out<T>(p);
-    hipLaunchKernelGGL((logits_kernel<T, kStats>), dim3(tiles_all), dim3(kThreads), 0, stream, p);
+    launch_logits<T, kStats>(p, shape, stream);
     hipLaunchKernelGGL(rows_kernel, dim3(static_cast<unsigned>((a.rows + 63) / 64)), dim3(1024), 0, stream, p.stats, p.right,
                        a.target, a.loss, a.lse, a.rows, static_cast<int>(tiles), a.vocab);
     return hipGetLastError();
@@ -482,14 +553,15 @@ hipError_t forward(const CrossEntropyArgs &a, hipStream_t stream)
 template <typename T>
 hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
 {
-    const Cut c = cut(a.rows, a.width, a.vocab, sizeof(T));
-    const long long rows_padded = round_up(a.rows, kTileB), piece = c.piece;
+    const Cut c = cut_of(a.rows, a.width, a.vocab, sizeof(T));
     const T *w = static_cast<const T *>(a.w);
     T *dl = reinterpret_cast<T *>(a.workspace);
-    float *sums = reinterpret_cast<float *>(a.workspace + rows_padded * piece * sizeof(T));
-    for (long long first = 0; first < a.vocab; first += piece) {
-        const int live = static_cast<int>(std::min<long long>(a.vocab - first, piece));
-        const long long padded = round_up(live, kTileA);
+    float *sums = reinterpret_cast<float *>(a.workspace + c.rows_padded * c.piece * sizeof(T));
+    float *dw_sums = sums + c.dx_slices * a.rows * a.width;
+    Sums of_dx = {}, of_dw = {};
+    for (long long first = 0; first < a.vocab; first += c.piece) {
+        const int live = static_cast<int>(std::min<long long>(a.vocab - first, c.piece));
+        const long long padded = round_up(live, kSides[c.logits][0]);
         if (a.rows) {
             Product p = {};
             p.a = {w + first * a.w_stride, a.w_stride, live, a.width};
@@ -503,8 +575,7 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
             p.dloss = a.dloss;
             p.out = dl;
             p.out_stride = padded;
-            const int tiles = lay_out<T>(p);
-            hipLaunchKernelGGL((logits_kernel<T, kDlogits>), dim3(tiles), dim3(kThreads), 0, stream, p);
+            launch_logits<T, kDlogits>(p, c.logits, stream);
         }
         Product dx = {}, dw = {};
         int dx_tiles = 0, dw_tiles = 0;
@@ -512,27 +583,37 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
             // dl is zero from `live` to `padded`, so its last chunk may be read whole
             dx.a = {w + first * a.w_stride, a.w_stride, a.width, live};
             dx.b = {dl, padded, a.rows, round_up(live, 16 / sizeof(T))};
-            dx.slices = c.slices;
+            dx.slices = c.dx_slices;
             dx.out = sums;
             dx.out_stride = a.width;
             dx.accumulate = first > 0;
-            dx_tiles = lay_out<T>(dx);
+            dx_tiles = lay_out<T>(dx, c.gradients);
         }
         if (a.dw) {
             dw.a = {a.x, a.x_stride, a.width, a.rows};
             dw.b = {dl, padded, padded, a.rows};
-            dw.slices = 1;
+            dw.slices = c.dw_slices;
             dw.live = live;
-            dw.out = static_cast<T *>(a.dw) + first * a.w_stride;
-            dw.out_stride = a.w_stride;
-            dw_tiles = lay_out<T>(dw);
+            dw.out = c.dw_slices > 1 ? dw_sums : static_cast<void *>(static_cast<T *>(a.dw) + first * a.w_stride);
+            dw.out_stride = c.dw_slices > 1 ? a.width : a.w_stride;
+            dw_tiles = lay_out<T>(dw, c.gradients);
+            of_dw.rows_padded = padded;
         }
-        if (dx_tiles + dw_tiles)
-            hipLaunchKernelGGL((gradients_kernel<T>), dim3(dx_tiles + dw_tiles), dim3(kThreads), 0, stream, dw, dx, dw_tiles);
+        const dim3 grid(dx_tiles + dw_tiles);
+        if (!(dx_tiles + dw_tiles)) continue;
+        if (c.gradients == kLarge)
+            hipLaunchKernelGGL((gradients_kernel<T, Large, false>), grid, dim3(Large::Threads), 0, stream, dw, dx, dw_tiles);
+        else if (c.dw_slices > 1)
+            hipLaunchKernelGGL((gradients_kernel<T, Medium, true>), grid, dim3(Medium::Threads), 0, stream, dw, dx, dw_tiles);
+        else
+            hipLaunchKernelGGL((gradients_kernel<T, Medium, false>), grid, dim3(Medium::Threads), 0, stream, dw, dx, dw_tiles);
     }
-    if (a.dx && a.rows)
-        hipLaunchKernelGGL((sums_kernel<T>), dim3(static_cast<unsigned>((a.rows * (a.width / 4) + 255) / 256)), dim3(256), 0, stream,
-                           sums, static_cast<T *>(a.dx), a.x_stride, a.rows, a.width, c.slices);
+    if (a.dx && a.rows) of_dx = {sums, a.dx, a.x_stride, a.rows, a.rows, c.dx_slices};
+    if (a.dw && c.dw_slices > 1) of_dw = {dw_sums, a.dw, a.w_stride, a.vocab, of_dw.rows_padded, c.dw_slices};
+    const long long quads = std::max(of_dx.rows, of_dw.rows) * (a.width / 4);
+    if (quads)
+        hipLaunchKernelGGL((sums_kernel<T>), dim3(static_cast<unsigned>((quads + 255) / 256), of_dw.rows ? 2 : 1), dim3(256), 0,
+                           stream, of_dx, of_dw, a.width);
     return hipGetLastError();
 }
 
@@ -540,10 +621,10 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
 
 long long cross_entropy_workspace_bytes(long long rows, int width, int vocab, bool bf16, bool backward)
 {
-    if (!backward) return round_up(rows * (round_up(vocab, kTileA) / kTileA * 8 + 4), 16) + 16;
+    if (!backward) return round_up(rows * (round_up(vocab, 128) / 128 * 8 + 4), 16) + 16;
     const int bytes = bf16 ? 2 : 4;
-    const Cut c = cut(rows, width, vocab, bytes);
-    return round_up(rows, kTileB) * c.piece * bytes + c.slices * rows * width * 4 + 16;
+    const Cut c = cut_of(rows, width, vocab, bytes);
+    return c.rows_padded * c.piece * bytes + (c.dx_slices * rows + (c.dw_slices > 1 ? c.dw_slices * c.piece : 0)) * width * 4 + 16;
 }
 
 hipError_t launch_cross_entropy(const CrossEntropyArgs &a, bool bf16, hipStream_t stream)
