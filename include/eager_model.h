@@ -129,10 +129,13 @@ typedef struct {
  *
  * Backward, for the upstream gradients dloss[r] (device, fp32) of the losses, with p = softmax(l):
  *     dl_v = dloss[r] * (p_v - [v = target[r]]),  dx_r = sum_v dl_v w_v,  dw_v = sum_r dl_v x_r
- * in pieces of the vocabulary, each piece's logits computed again from x, w and lse.  dx or dw may
- * be NULL (not wanted).  In bf16 the dl of a piece are held in bf16 between the products.
- * workspace_bytes(backward = 0 or 1): what the forward or the backward pass wants at least; the
- * backward pass uses a larger one for larger pieces, up to what workspace_bytes says.
+ * in pieces of the vocabulary, each piece's logits computed again from x, w and lse.  Rows with a
+ * negative target or a dloss of zero are left out from the start: they cost nothing, whatever x
+ * holds there reaches no gradient, and their dx is zero.  dx or dw may be NULL (not wanted).  In bf16
+ * the dl of a piece are held in bf16 between the products.
+ * fp32 products are formed from three bf16 pieces of every operand, whose sum is the operand: within two
+ * roundings of an fp32 product; an infinite operand gives NaN.
+ * workspace_bytes: what the forward (backward = 0) or the backward pass (1) needs.
  */
 int eager_cross_entropy(int dtype, const eager_projection *shape, const void *x, const void *w,
                         const int64_t *target, float *loss, float *lse, void *workspace,

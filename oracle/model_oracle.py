@@ -1,4 +1,4 @@
-"""The operators of a transformer step from their definitions, in 64 bits on the CPU, row by row and
+"""The operators of a transformer step from their definitions, in 64 bits row by row and
 head by head; no code shared with the library.  Next to every result stands the bound that rounding
 gives an implementation which holds its sums in fp32, rounds intermediate matrix operands to the
 inputs' type and its results once (`u`: unit roundoff of that type).
@@ -57,8 +57,8 @@ def attention(q, k, v, cu, scale, dout=None):
     q, k, v = q.to(F), k.to(F), v.to(F)
     T, H, D = q.shape
     Hk = k.shape[1]
-    out, ob = torch.zeros(T, H, D, dtype=F), torch.zeros(T, H, D, dtype=F)
-    lse, lb = torch.full((H, T), -math.inf, dtype=F), torch.zeros(H, T, dtype=F)
+    out, ob = (torch.zeros(T, H, D, dtype=F, device=q.device) for _ in range(2))
+    lse, lb = torch.full((H, T), -math.inf, dtype=F, device=q.device), torch.zeros(H, T, dtype=F, device=q.device)
     grads = {}
     if dout is not None:
         dout = dout.to(F)
@@ -71,7 +71,7 @@ def attention(q, k, v, cu, scale, dout=None):
         for h in range(H):
             g = h // (H // Hk)
             Q, K, V = q[a:b, h], k[a:b, g], v[a:b, g]
-            later = torch.ones(n, n, dtype=torch.bool).triu(1)
+            later = torch.ones(n, n, dtype=torch.bool, device=q.device).triu(1)
             s = scale * (Q @ K.t())
             # products of D terms, the scale folded into the exponential's base-2 argument
             s_err = ((D + 6) * E * scale * (Q.abs() @ K.abs().t())).masked_fill(later, 0).amax(1, keepdim=True) + \
@@ -122,8 +122,9 @@ def cross_entropy(x, w, target, dloss=None):
     s_err = l_err + (V + 16) * E + 8 * E * logits.abs().amax(1) + 4 * E * lse.abs()
     counted = target >= 0
     at = torch.where(counted, target, 0)
-    right = logits[torch.arange(rows), at]
-    zero = torch.zeros(rows, dtype=F)
+    each = torch.arange(rows, device=x.device)
+    right = logits[each, at]
+    zero = torch.zeros(rows, dtype=F, device=x.device)
     result = {"loss": (torch.where(counted, lse - right, zero),
                        torch.where(counted, s_err + l_err + 2 * E * (lse - right).abs(), zero)),
               "lse": (lse, s_err)}
@@ -131,7 +132,7 @@ def cross_entropy(x, w, target, dloss=None):
         return result
     p = torch.exp(logits - lse[:, None])
     one = torch.zeros_like(p)
-    one[torch.arange(rows), at] = 1.0
+    one[each, at] = 1.0
     g = torch.where(counted, dloss.to(F), zero)[:, None]
     dl = g * (p - one)
     dl_err = u * dl.abs() + g.abs() * (p * (s_err + l_err)[:, None] + 2 * E * (p + one))

@@ -11,7 +11,7 @@
 namespace eager {
 namespace {
 
-constexpr int kRows = 128;           // query rows of a workgroup: 32 a wavefront
+constexpr int kRows = kAttentionRows;        // query rows of a workgroup: 32 a wavefront
 constexpr int kKeys = 64;            // keys of a tile
 
 template <typename T, int DP>

@@ -12,7 +12,7 @@
 namespace eager {
 namespace {
 
-constexpr int kRows = 128;           // queries (keys) of a workgroup: 32 a wavefront
+constexpr int kRows = kAttentionRows;        // queries (keys) of a workgroup: 32 a wavefront
 constexpr int kTile = 64;            // keys (queries) of a tile
 // How many halves of a tile are unrolled: with long heads two of them side by side do not fit the registers.
 template <typename T, int DP> constexpr int kHalves = DP * sizeof(T) > 128 ? 1 : 2;
@@ -286,26 +286,6 @@ void enqueue(const AttentionArgs &a, hipStream_t stream)
 }
 
 }  // namespace
-
-// Two workgroups have a compute unit: 512 run at once, and about four rounds of them even out what a
-// causal mask leaves to each.
-int attention_parts(long long tokens, int q_heads, int kv_heads, int sequences)
-{
-    const int group = q_heads / kv_heads;
-    const long long workgroups = tile_numbers(tokens, sequences, kRows) * kv_heads;
-    int parts = 1;
-    while (parts < group && workgroups * parts < 2048)
-        do ++parts; while (group % parts);
-    return parts;
-}
-
-long long attention_row_bytes(long long tokens, int q_heads) { return (tokens * q_heads * 4 + 15) / 16 * 16; }
-
-long long attention_workspace_bytes(long long tokens, int q_heads, int kv_heads, int dim, int sequences)
-{
-    const int parts = attention_parts(tokens, q_heads, kv_heads, sequences);
-    return 2 * attention_row_bytes(tokens, q_heads) + (parts > 1 ? parts * 2ll * kv_heads * tokens * dim * 4 : 0);
-}
 
 hipError_t launch_attention_backward(const AttentionArgs &a, bool bf16, hipStream_t stream)
 {

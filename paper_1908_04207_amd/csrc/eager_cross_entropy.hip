@@ -13,8 +13,8 @@
 // softmax statistics stay within a lane and results are stored four values at a time.
 #include "eager_matrix.h"
 #include "eager_model.h"
+#include "eager_model_rules.h"
 
-#include <algorithm>
 #include <type_traits>
 
 namespace eager {
@@ -45,6 +45,8 @@ struct Product {
     long long first;         // vocabulary index of a row 0
     int live;                // rows of a that are vocabulary (the rest is padding)
     int vocab;
+    const int *counted;      // device: rows of x that count (gather_kernel), or NULL: all of them
+    int counted_k;           // they are k, not the rows of b
 };
 
 enum Epilogue { kStats, kDlogits, kSums, kResult };
@@ -106,15 +108,6 @@ __device__ __forceinline__ typename Operand<T>::frag read_side(const char *tile,
     return read_columns<Rows * sizeof(T) / 16, sizeof(T) == 2 ? 2 : 31>(tile, row0, 16 * step, 8, 4, lane, static_cast<T *>(nullptr));
 }
 
-// A workgroup's tile, its wavefronts, and how many workgroups have a compute unit (by their shared memory).
-template <int A_, int B_, int WavesA_, int WavesB_, int OfUnit_>
-struct TileShape {
-    static constexpr int A = A_, B = B_, WavesA = WavesA_, WavesB = WavesB_, Threads = 64 * WavesA * WavesB, OfUnit = OfUnit_;
-};
-typedef TileShape<256, 256, 2, 4, 1> Large;
-typedef TileShape<128, 128, 2, 2, 2> Medium;
-typedef TileShape<128, 64, 4, 1, 3> Narrow;
-
 // The tile of workgroup `id`: workgroups id, id + 8, ... run on the same chiplet (one second-level
 // cache), so each chiplet gets a contiguous share of the tiles, in which 8 tiles of b are gone
 // through for every tile of a.
@@ -145,11 +138,23 @@ __device__ __forceinline__ void product(const Product &p, int id, char *tile0, c
     place(id - slice * p.tiles_a * p.tiles_b, p.tiles_a, p.tiles_b, tile_a, tile_b);
     const long long a0 = static_cast<long long>(tile_a) * BM, b0 = static_cast<long long>(tile_b) * BN;
     const int wave_a = wave % WM * (BM / WM), wave_b = wave / WM * (BN / WN);
+    Side a_side = p.a, b_side = p.b;
+    int all_steps = p.all_steps;
+    if (Epi != kStats) {
+        const int counted = *p.counted;
+        if (p.counted_k) {
+            a_side.k = b_side.k = counted;
+            all_steps = (counted + kDepth<T> - 1) / kDepth<T>;
+        } else {
+            b_side.rows = counted;
+            if (b0 >= counted) return;
+        }
+    }
     const int first = slice * p.steps;
-    const int count = max(0, min(p.steps, p.all_steps - first));
+    const int count = max(0, min(p.steps, all_steps - first));
     const long long k0 = static_cast<long long>(first) * kDepth<T>;
-    Source<T, BM, ColumnsA, Waves> side_a(p.a, a0, k0, wave, lane);
-    Source<T, BN, ColumnsB, Waves> side_b(p.b, b0, k0, wave, lane);
+    Source<T, BM, ColumnsA, Waves> side_a(a_side, a0, k0, wave, lane);
+    Source<T, BN, ColumnsB, Waves> side_b(b_side, b0, k0, wave, lane);
     auto stage = [&](char *tile, int t) {
         side_a.load(tile, t < count);
         side_b.load(tile + BM * 128, t < count);
@@ -276,18 +281,18 @@ __device__ __forceinline__ void product(const Product &p, int id, char *tile0, c
         return tile + (chunk ^ (row & (RowChunks - 1) & 31)) * 16;
     };
     const int live = static_cast<int>(min(p.live - a0, static_cast<long long>(BM)));
-    const long long rows = Epi == kResult ? p.live : p.b.rows;
+    const long long rows = Epi == kResult ? p.live : b_side.rows;
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
         const int in_b = wave_b + 32 * j + (lane & 31);
         const long long row = b0 + in_b;
         if (Epi == kDlogits) {
-            float lse = 0.0f, g = 0.0f;
+            float lse = __builtin_inff(), g = 0.0f;     // rows that there are not: zeros
             int target = -1;
             if (row < rows) {
                 const long long v = p.target[row];
                 lse = p.lse[row] * kLog2e;
-                g = v < 0 ? 0.0f : v >= p.vocab ? __builtin_nanf("") : p.dloss[row];
+                g = v >= p.vocab ? __builtin_nanf("") : p.dloss[row];
                 const long long from = v - p.first - a0;
                 target = from >= wave_a && from < wave_a + 32 * MI ? static_cast<int>(from) : -1;
             }
@@ -308,7 +313,7 @@ __device__ __forceinline__ void product(const Product &p, int id, char *tile0, c
 #pragma unroll
             for (int i = 0; i < MI; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) c[i][j][r] = g == 0.0f ? 0.0f : g * c[i][j][r];
+                for (int r = 0; r < 16; ++r) c[i][j][r] *= g;
         }
         const long long from = a0 + wave_a + 4 * half;
         const int limit = Epi == kDlogits ? BM : row < rows ? static_cast<int>(min(p.a.rows - from, static_cast<long long>(BM))) : 0;
@@ -404,9 +409,100 @@ __global__ __launch_bounds__(1024) void rows_kernel(const float2 *stats, const f
     loss[row] = t < 0 ? 0.0f : t >= vocab ? __builtin_nanf("") : all - right[row];
 }
 
+// The rows that count in the backward pass - those with a target and a weight - side by side: the
+// products leave the others out, whatever stands in them.
+struct Gather {
+    const void *x;
+    const long long *target;
+    const float *lse, *dloss;
+    long long rows, stride;
+    int width;
+    const int *before;       // per workgroup: counted rows in front of them, or NULL: each counts them
+    void *x_out;             // [counted][width]
+    long long *target_out;
+    float *lse_out, *dloss_out;
+    int *place;              // per row: where it went, -1: nowhere
+    int *counted;
+};
+
+__device__ __forceinline__ bool counts(const Gather &g, long long row) { return (g.target[row] >= 0) & (g.dloss[row] != 0.0f); }
+
+// kGathered rows a workgroup
+template <typename T>
+__global__ __launch_bounds__(1024) void gather_kernel(const Gather g)
+{
+    __shared__ int sums[16], place[kGathered];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long first = static_cast<long long>(blockIdx.x) * kGathered;
+    int before = 0;
+    if (!g.before) {
+#pragma unroll 8
+        for (long long row = threadIdx.x; row < first; row += 1024) before += counts(g, row);
+        for (int m = 1; m < 64; m *= 2) before += __shfl_xor(before, m, 64);
+        if (lane == 0) sums[wave] = before;
+    }
+    __syncthreads();
+    if (wave == 0) {
+        before = g.before ? g.before[blockIdx.x] : 0;
+        if (!g.before)
+            for (int w = 0; w < 16; ++w) before += sums[w];
+        const long long row = first + lane;
+        const bool mine = lane < kGathered && row < g.rows, in = mine && counts(g, row);
+        const unsigned long long mask = __ballot(in);
+        const int to = in ? before + __popcll(mask & ((1ull << lane) - 1)) : -1;
+        if (lane < kGathered) place[lane] = to;
+        if (mine) g.place[row] = to;
+        if (in) {
+            g.target_out[to] = g.target[row];
+            g.lse_out[to] = g.lse[row];
+            g.dloss_out[to] = g.dloss[row];
+        }
+        if (lane == 0 && first + kGathered >= g.rows) *g.counted = before + __popcll(mask);
+    }
+    __syncthreads();
+    constexpr int E = 16 / sizeof(T);
+    const int chunks = g.width / E;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < kGathered * chunks; i += 1024) {
+        const int in = i / chunks, at = (i - in * chunks) * E;
+        if (place[in] >= 0)
+            *reinterpret_cast<f32x4 *>(static_cast<T *>(g.x_out) + static_cast<long long>(place[in]) * g.width + at) =
+                *reinterpret_cast<const f32x4 *>(static_cast<const T *>(g.x) + (first + in) * g.stride + at);
+    }
+}
+
+// `before` of many rows, by one workgroup: 1024 times kGathered rows at a time
+__global__ __launch_bounds__(1024) void before_kernel(const Gather g, int *before)
+{
+    __shared__ int sums[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long blocks = (g.rows + kGathered - 1) / kGathered;
+    int base = 0;
+    for (long long b0 = 0; b0 < blocks; b0 += 1024) {
+        const long long first = (b0 + threadIdx.x) * kGathered;
+        int mine = 0;
+#pragma unroll
+        for (int i = 0; i < kGathered; ++i)
+            if (first + i < g.rows) mine += counts(g, first + i);
+        int upto = mine;
+        for (int m = 1; m < 64; m *= 2) {
+            const int other = __shfl_up(upto, m, 64);
+            if (lane >= m) upto += other;
+        }
+        if (lane == 63) sums[wave] = upto;
+        __syncthreads();
+        int start = base;
+        for (int w = 0; w < wave; ++w) start += sums[w];
+        if (b0 + threadIdx.x < blocks) before[b0 + threadIdx.x] = start + upto - mine;
+        for (int w = 0; w < 16; ++w) base += sums[w];
+        __syncthreads();
+    }
+}
+
 // dx (and dw) from the slices' sums, four values a thread
 struct Sums {
     const float *sums;       // [slices][rows_padded][width]
+    const int *place;        // per row of `out`: its row in the sums, -1: zeros; NULL: the same
     void *out;
     long long stride, rows, rows_padded;
     int slices;
@@ -418,97 +514,15 @@ __global__ __launch_bounds__(256) void sums_kernel(const Sums dx, const Sums dw,
     const int quads = width / 4;
     const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
     if (i >= s.rows * quads) return;
-    const f32x4 *from = reinterpret_cast<const f32x4 *>(s.sums) + i;
-    f32x4 x = *from;
+    const long long row = i / quads, at = (i - row * quads) * 4, place = s.place ? s.place[row] : row;
+    f32x4 x = {};
+    if (place >= 0) {
+        const f32x4 *from = reinterpret_cast<const f32x4 *>(s.sums + place * width + at);
+        x = *from;
 #pragma unroll 4
-    for (int n = 1; n < s.slices; ++n) x += from[n * s.rows_padded * quads];
-    const long long row = i / quads, at = (i - row * quads) * 4;
-    *reinterpret_cast<typename Operand<T>::quad *>(static_cast<T *>(s.out) + row * s.stride + at) = to_quad(x, static_cast<T *>(nullptr));
-}
-
-long long round_up(long long x, long long to) { return (x + to - 1) / to * to; }
-
-// What a product costs in a shape of tiles: rounds of as many tiles as run at once, each a number of
-// steps of k (128 bytes) and what filling and emptying takes, in microseconds.
-struct Cost {
-    double step, rest;
-};
-template <typename Shape> Cost cost_of(int bytes);
-template <> Cost cost_of<Large>(int bytes) { return bytes == 2 ? Cost{1.4, 13} : Cost{5.9, 13}; }
-template <> Cost cost_of<Medium>(int bytes) { return bytes == 2 ? Cost{1.0, 9} : Cost{3.0, 9}; }
-template <> Cost cost_of<Narrow>(int bytes) { return bytes == 2 ? Cost{0.9, 6} : Cost{2.5, 6}; }
-
-template <typename Shape>
-double rounds_of(long long tiles) { return static_cast<double>((tiles + 256 * Shape::OfUnit - 1) / (256 * Shape::OfUnit)); }
-
-template <typename Shape>
-double logits_time(long long rows, int width, long long vocab, int bytes)
-{
-    const Cost c = cost_of<Shape>(bytes);
-    const long long tiles = round_up(rows, Shape::B) / Shape::B * (round_up(vocab, Shape::A) / Shape::A);
-    return rounds_of<Shape>(tiles) * (round_up(width, 128 / bytes) / (128 / bytes) * c.step + c.rest);
-}
-
-// dw and dx of a piece: their tiles follow each other, so only the last round is not full
-template <typename Shape>
-double gradients_time(long long rows, int width, long long live, int dw_slices, int dx_slices, int bytes)
-{
-    const Cost c = cost_of<Shape>(bytes);
-    const long long depth = 128 / bytes, tiles_w = round_up(width, Shape::A) / Shape::A;
-    const double dw = ((rows + depth - 1) / depth + dw_slices - 1) / dw_slices * c.step + c.rest;
-    const double dx = ((live + depth - 1) / depth + dx_slices - 1) / dx_slices * c.step + c.rest;
-    const long long dw_tiles = tiles_w * (round_up(live, Shape::B) / Shape::B) * dw_slices;
-    const long long dx_tiles = tiles_w * (round_up(rows, Shape::B) / Shape::B) * dx_slices;
-    // a slice's sums are written, read and, from the second piece on, read again
-    const double sums = (dx_slices * static_cast<double>(rows) + (dw_slices > 1 ? dw_slices * static_cast<double>(live) : 0)) * width * 12;
-    return std::max((dw_tiles * dw + dx_tiles * dx) / (256 * Shape::OfUnit) + std::max(dw, dx) / 2, std::max(dw, dx)) + sums / 5e6;
-}
-
-// How the backward pass is cut: vocabulary rows of a piece; slices that are summed apart, of a
-// piece for dx and, where there is one piece, of the rows for dw; the shapes of tiles.  The fastest cut by
-// the above is taken among those whose dl fit 512 MiB.
-enum { kLarge, kMedium, kNarrow };
-struct Cut {
-    long long rows_padded, piece;
-    int dx_slices, dw_slices, logits, gradients;
-};
-
-int logits_shape(long long rows, int width, long long vocab, int bytes)
-{
-    const double t[3] = {logits_time<Large>(rows, width, vocab, bytes), logits_time<Medium>(rows, width, vocab, bytes),
-                         logits_time<Narrow>(rows, width, vocab, bytes)};
-    return static_cast<int>(std::min_element(t, t + 3) - t);
-}
-
-constexpr int kSides[3][2] = {{Large::A, Large::B}, {Medium::A, Medium::B}, {Narrow::A, Narrow::B}};
-
-Cut cut_of(long long rows, int width, int vocab, int bytes)
-{
-    const long long padded = round_up(std::max(rows, 1ll), 256);
-    const long long fit = std::max(256ll, (1ll << 29) / bytes / padded / 256 * 256);
-    const long long fewest = (vocab + fit - 1) / fit;
-    Cut best = {padded, 0, 1, 1, 0, 0};
-    double least = 0;
-    for (long long n = fewest; n < fewest + 6; ++n) {
-        const long long piece = round_up((vocab + n - 1) / n, 256), pieces = (vocab + piece - 1) / piece;
-        const int shape = logits_shape(rows, width, piece, bytes);
-        const double logits = std::min({logits_time<Large>(rows, width, piece, bytes), logits_time<Medium>(rows, width, piece, bytes),
-                                        logits_time<Narrow>(rows, width, piece, bytes)});
-        for (int dx = 1; dx <= 32; dx *= 2)
-            for (int dw = 1; dw <= (pieces > 1 ? 1 : 32); dw *= 2)
-                for (int g = dw > 1 ? kMedium : kLarge; g <= kMedium; ++g) {
-                    const double one = g == kLarge ? gradients_time<Large>(rows, width, piece, dw, dx, bytes)
-                                                   : gradients_time<Medium>(rows, width, piece, dw, dx, bytes);
-                    const double last = std::max(0.2, static_cast<double>(vocab - (pieces - 1) * piece) / piece);
-                    const double cost = (logits + one) * (pieces > 1 ? pieces - 1 + last : 1);
-                    if (!best.piece || cost < least) {
-                        least = cost;
-                        best = {padded, piece, dx, dw, shape, g};
-                    }
-                }
-        if (piece == 256) break;
+        for (int n = 1; n < s.slices; ++n) x += from[n * s.rows_padded * quads];
     }
-    return best;
+    *reinterpret_cast<typename Operand<T>::quad *>(static_cast<T *>(s.out) + row * s.stride + at) = to_quad(x, static_cast<T *>(nullptr));
 }
 
 // Tiles of a product, and their number.
@@ -554,25 +568,38 @@ template <typename T>
 hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
 {
     const Cut c = cut_of(a.rows, a.width, a.vocab, sizeof(T));
+    const Layout l = layout_of(c, a.rows, a.width, sizeof(T));
     const T *w = static_cast<const T *>(a.w);
-    T *dl = reinterpret_cast<T *>(a.workspace);
-    float *sums = reinterpret_cast<float *>(a.workspace + c.rows_padded * c.piece * sizeof(T));
-    float *dw_sums = sums + c.dx_slices * a.rows * a.width;
+    T *dl = reinterpret_cast<T *>(a.workspace + l.dl), *x = reinterpret_cast<T *>(a.workspace + l.x);
+    float *sums = reinterpret_cast<float *>(a.workspace + l.dx_sums), *dw_sums = reinterpret_cast<float *>(a.workspace + l.dw_sums);
+    int *counted = reinterpret_cast<int *>(a.workspace + l.counted), *place = reinterpret_cast<int *>(a.workspace + l.place);
     Sums of_dx = {}, of_dw = {};
+    Gather g = {a.x, a.target, a.lse, a.dloss, a.rows, a.x_stride, a.width, nullptr, x,
+                reinterpret_cast<long long *>(a.workspace + l.target), reinterpret_cast<float *>(a.workspace + l.lse),
+                reinterpret_cast<float *>(a.workspace + l.dloss), place, counted};
+    if (a.rows > kCountedByEach) {
+        int *before = reinterpret_cast<int *>(a.workspace + l.before);
+        hipLaunchKernelGGL(before_kernel, dim3(1), dim3(1024), 0, stream, g, before);
+        g.before = before;
+    }
+    // (without rows one workgroup says that none count)
+    hipLaunchKernelGGL((gather_kernel<T>), dim3(static_cast<unsigned>(std::max((a.rows + kGathered - 1) / kGathered, 1ll))),
+                       dim3(1024), 0, stream, g);
     for (long long first = 0; first < a.vocab; first += c.piece) {
         const int live = static_cast<int>(std::min<long long>(a.vocab - first, c.piece));
         const long long padded = round_up(live, kSides[c.logits][0]);
         if (a.rows) {
             Product p = {};
             p.a = {w + first * a.w_stride, a.w_stride, live, a.width};
-            p.b = {a.x, a.x_stride, a.rows, a.width};
+            p.b = {x, a.width, a.rows, a.width};
             p.slices = 1;
             p.first = first;
             p.live = live;
             p.vocab = a.vocab;
-            p.target = a.target;
-            p.lse = a.lse;
-            p.dloss = a.dloss;
+            p.target = g.target_out;
+            p.lse = g.lse_out;
+            p.dloss = g.dloss_out;
+            p.counted = counted;
             p.out = dl;
             p.out_stride = padded;
             launch_logits<T, kDlogits>(p, c.logits, stream);
@@ -583,6 +610,7 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
             // dl is zero from `live` to `padded`, so its last chunk may be read whole
             dx.a = {w + first * a.w_stride, a.w_stride, a.width, live};
             dx.b = {dl, padded, a.rows, round_up(live, 16 / sizeof(T))};
+            dx.counted = counted;
             dx.slices = c.dx_slices;
             dx.out = sums;
             dx.out_stride = a.width;
@@ -590,7 +618,9 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
             dx_tiles = lay_out<T>(dx, c.gradients);
         }
         if (a.dw) {
-            dw.a = {a.x, a.x_stride, a.width, a.rows};
+            dw.a = {x, a.width, a.width, a.rows};
+            dw.counted = counted;
+            dw.counted_k = 1;
             dw.b = {dl, padded, padded, a.rows};
             dw.slices = c.dw_slices;
             dw.live = live;
@@ -608,8 +638,8 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
         else
             hipLaunchKernelGGL((gradients_kernel<T, Medium, false>), grid, dim3(Medium::Threads), 0, stream, dw, dx, dw_tiles);
     }
-    if (a.dx && a.rows) of_dx = {sums, a.dx, a.x_stride, a.rows, a.rows, c.dx_slices};
-    if (a.dw && c.dw_slices > 1) of_dw = {dw_sums, a.dw, a.w_stride, a.vocab, of_dw.rows_padded, c.dw_slices};
+    if (a.dx && a.rows) of_dx = {sums, place, a.dx, a.x_stride, a.rows, a.rows, c.dx_slices};
+    if (a.dw && c.dw_slices > 1) of_dw = {dw_sums, nullptr, a.dw, a.w_stride, a.vocab, of_dw.rows_padded, c.dw_slices};
     const long long quads = std::max(of_dx.rows, of_dw.rows) * (a.width / 4);
     if (quads)
         hipLaunchKernelGGL((sums_kernel<T>), dim3(static_cast<unsigned>((quads + 255) / 256), of_dw.rows ? 2 : 1), dim3(256), 0,
@@ -618,14 +648,6 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
 }
 
 }  // namespace
-
-long long cross_entropy_workspace_bytes(long long rows, int width, int vocab, bool bf16, bool backward)
-{
-    if (!backward) return round_up(rows * (round_up(vocab, 128) / 128 * 8 + 4), 16) + 16;
-    const int bytes = bf16 ? 2 : 4;
-    const Cut c = cut_of(rows, width, vocab, bytes);
-    return c.rows_padded * c.piece * bytes + (c.dx_slices * rows + (c.dw_slices > 1 ? c.dw_slices * c.piece : 0)) * width * 4 + 16;
-}
 
 hipError_t launch_cross_entropy(const CrossEntropyArgs &a, bool bf16, hipStream_t stream)
 {

@@ -54,17 +54,11 @@ struct CrossEntropyArgs {
 
 hipError_t launch_norm_rope(const NormRopeArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_norm_rope_backward(const NormRopeArgs &a, bool bf16, hipStream_t stream);
-int norm_rope_blocks(long long tokens, int q_heads, int kv_heads);
-int norm_rope_tokens_per_block(int heads, bool backward);
 
 hipError_t launch_attention(const AttentionArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_attention_backward(const AttentionArgs &a, bool bf16, hipStream_t stream);
-int attention_parts(long long tokens, int q_heads, int kv_heads, int sequences);
-long long attention_row_bytes(long long tokens, int q_heads);
-long long attention_workspace_bytes(long long tokens, int q_heads, int kv_heads, int dim, int sequences);
 
 hipError_t launch_cross_entropy(const CrossEntropyArgs &a, bool bf16, hipStream_t stream);
 hipError_t launch_cross_entropy_backward(const CrossEntropyArgs &a, bool bf16, hipStream_t stream);
-long long cross_entropy_workspace_bytes(long long rows, int width, int vocab, bool bf16, bool backward);
 
 }  // namespace eager

@@ -1,6 +1,7 @@
 // Host side of the model operators (include/eager_model.h): argument checks, then the launch.
 #include "../../include/eager_model.h"
 #include "eager_model.h"
+#include "eager_model_rules.h"
 
 #include <cmath>
 
@@ -28,7 +29,7 @@ bool valid_shape(const eager_packed *s)
 bool valid_sequences(const eager_packed *s)
 {
     return valid_shape(s) && s->sequences >= 1 && s->sequences <= (1 << 30) && aligned(s->cu_seqlens, 4) &&
-           (s->tokens / 128 + s->sequences + 2) * s->q_heads <= kMaxGrid;
+           eager::tile_numbers(s->tokens, s->sequences, eager::kAttentionRows) * s->q_heads <= kMaxGrid;
 }
 
 // no row or head shares elements with the next one (a broadcast view does)
@@ -101,7 +102,7 @@ bool valid_projection(int dtype, const eager_projection *s)
 {
     return valid_dtype(dtype) && s && s->rows >= 0 && s->rows <= kMaxTokens && s->width >= 8 && s->width % 8 == 0 &&
            s->width <= kMaxStride && s->vocab >= 1 && s->vocab <= (1 << 30) &&
-           (s->vocab / 128 + 1ll) * (s->rows / 128 + 1) <= kMaxGrid && s->rows * (s->width / 8) / 128 < kMaxGrid;
+           (s->vocab / 128 + 1ll) * (s->rows / 64 + 1) <= kMaxGrid && s->rows * (s->width / 8) / 128 < kMaxGrid;
 }
 
 bool fill(eager::CrossEntropyArgs &a, int dtype, const eager_projection *s, const void *x, const void *w,

@@ -240,23 +240,6 @@ hipError_t dispatch(const NormRopeArgs &a, bool bf16, bool backward, hipStream_t
 
 }  // namespace
 
-// Heads a workgroup takes at a time: two a group of lanes with 4 lanes a head in the forward pass,
-// four in the backward pass, which keeps sums from turn to turn (8192 tokens of 20 heads of 64 in bf16:
-// forward 11.0 us, 12.6 with 256; backward 15.8 us, 20.6 with 128).
-int norm_rope_tokens_per_block(int heads, bool backward)
-{
-    const int want = backward ? 256 : 128;
-    return heads >= want ? 1 : want / heads;
-}
-
-// Workgroups of the backward pass: at most 1024, each with the same number of turns.
-int norm_rope_blocks(long long tokens, int q_heads, int kv_heads)
-{
-    const int per = norm_rope_tokens_per_block(q_heads + kv_heads, true);
-    const long long all = (tokens + per - 1) / per, rounds = (all + 1023) / 1024;
-    return static_cast<int>(all ? (all + rounds - 1) / rounds : 0);
-}
-
 hipError_t launch_norm_rope(const NormRopeArgs &a, bool bf16, hipStream_t stream)
 {
     return dispatch(a, bf16, false, stream);

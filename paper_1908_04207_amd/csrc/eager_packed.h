@@ -9,6 +9,7 @@
 
 #include "eager_matrix.h"
 #include "eager_model.h"
+#include "eager_model_rules.h"
 
 namespace eager {
 
@@ -51,8 +52,6 @@ __device__ __forceinline__ Tile find_tile(const int *cu, int sequences, int toke
     t.first = static_cast<int>(min(max(first, static_cast<long long>(t.begin)), static_cast<long long>(t.end)));
     return t;
 }
-
-inline long long tile_numbers(long long tokens, int sequences, int rows) { return tokens / rows + sequences + 2; }
 
 // The larger of, and the sum over, a lane and the one 32 away.
 __device__ __forceinline__ void both_halves(float &x, float &y)
