@@ -27,7 +27,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attention_
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int head = blockIdx.x % a.q_heads;
     const Tile t = find_tile<kRows>(a.cu, a.sequences, static_cast<int>(a.tokens),
-                                    (gridDim.x - 1 - blockIdx.x) / a.q_heads);
+                                    blockIdx.x / a.q_heads, false);
     if (t.first >= t.end) return;
     if (t.segment == 0 || t.segment == a.sequences + 1) {
         clear_rows<T, kRows>(a.out, head, t.first, t.end, a.dim);
@@ -73,9 +73,10 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attention_
                 for (int i = 0; i < 16; ++i)
                     if (32 * b + 8 * (i >> 2) + (i & 3) > seen) s[b][i] = -__builtin_inff();
         }
+        // (a NaN among the scores stays: its row becomes NaN)
         float best = top;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) best = fmaxf(best, fmaxf(s[0][i], s[1][i]));
+        for (int i = 0; i < 16; ++i) best = __builtin_elementwise_maximum(best, __builtin_elementwise_maximum(s[0][i], s[1][i]));
         best = both_max(best);
         const float base = best == -__builtin_inff() ? 0.0f : best * c;
         if (__any(best != top)) {                       // a new maximum: rare after the first tiles

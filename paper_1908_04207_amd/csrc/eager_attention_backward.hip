@@ -30,7 +30,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void queries_ke
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int head = blockIdx.x % a.q_heads;
     const Tile t = find_tile<kRows>(a.cu, a.sequences, static_cast<int>(a.tokens),
-                                    (gridDim.x - 1 - blockIdx.x) / a.q_heads);
+                                    blockIdx.x / a.q_heads, false);
     if (t.first >= t.end) return;
     if (t.segment == 0 || t.segment == a.sequences + 1) {
         clear_rows<T, kRows>(a.dq, head, t.first, t.end, a.dim);
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void keys_kerne
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int shared = blockIdx.x % (a.kv_heads * a.parts), kv_head = shared / a.parts, part = shared % a.parts;
     const int heads = a.q_heads / a.kv_heads / a.parts;
-    const Tile t = find_tile<kRows>(a.cu, a.sequences, static_cast<int>(a.tokens), blockIdx.x / (a.kv_heads * a.parts));
+    const Tile t = find_tile<kRows>(a.cu, a.sequences, static_cast<int>(a.tokens), blockIdx.x / (a.kv_heads * a.parts), true);
     if (t.first >= t.end) return;
     // where the sums go: [part][k, v][kv head][token][dim]
     float *const sums = a.sums + (static_cast<long long>(part) * 2 * a.kv_heads + kv_head) * a.tokens * a.dim;

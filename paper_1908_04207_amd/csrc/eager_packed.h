@@ -2,9 +2,12 @@
 // memory, so that no call waits for lengths.
 //
 // The rows fall into sequences + 2 segments: those before the first sequence, the sequences, those
-// after the last.  Segment i, which begins at row e_i, has the tiles from e_i / Rows + i on: as
-// floor(a + b) >= floor(a) + floor(b), they suffice for its rows, and the numbers ascend, so a
-// search finds a tile's segment.  At most tokens / Rows + sequences + 2 numbers are in use.
+// after the last.  Together they have at most tokens / Rows + sequences + 2 tiles, and as many
+// workgroups (a head) look for theirs.  Under a causal mask a tile's work grows along its sequence (for keys:
+// towards its front), so up to 64 segments are gone through by work: the n-th tile is found from
+// F(j) = sum over segments of max(0, tiles - j), the number of tiles of work j or more.  With more
+// segments, which are short ones then, segment i, which begins at row e_i, has the tiles from e_i / Rows + i on: as
+// floor(a + b) >= floor(a) + floor(b), they suffice for its rows, and the numbers ascend.
 #pragma once
 
 #include "eager_matrix.h"
@@ -25,10 +28,53 @@ __device__ __forceinline__ int segment_start(const int *cu, int sequences, int t
     return i == 0 ? 0 : i > sequences + 1 ? tokens : min(max(bound, 0), tokens);
 }
 
-// Every wavefront searches for itself, 64 candidates at a time; the last step's candidates are the
-// bounds, so up to 62 sequences take one trip to memory.
+// Up to 64 segments: a lane a segment, one trip to memory; then a lane a value of j.
 template <int Rows>
-__device__ __forceinline__ Tile find_tile(const int *cu, int sequences, int tokens, int number)
+__device__ __forceinline__ Tile find_by_work(const int *cu, int sequences, int tokens, int number, bool from_back)
+{
+    const int lane = threadIdx.x & 63;
+    const int begin = segment_start(cu, sequences, tokens, lane), next = segment_start(cu, sequences, tokens, lane + 1);
+    const int tiles = lane < sequences + 2 ? (max(next - begin, 0) + Rows - 1) / Rows : 0;
+    int most = tiles;
+    for (int m = 1; m < 64; m *= 2) most = max(most, __shfl_xor(most, m, 64));
+    most = __builtin_amdgcn_readfirstlane(most);
+    // the largest j with F(j) > number, from the end of [lo, lo + count) that is left
+    int lo = 0, count = most + 1, rest = 0;
+    for (;;) {
+        const int step = (count + 63) >> 6, j = lo + lane * step;
+        int f = 0, after = 0;                           // F(j), F(j + 1)
+        for (int s = 0; s < sequences + 2; ++s) {
+            const int n = __builtin_amdgcn_readlane(tiles, s);
+            f += max(n - j, 0);
+            after += max(n - j - 1, 0);
+        }
+        const int k = __popcll(__ballot(lane * step < count && f > number)) - 1;
+        if (k < 0) {                                    // there are fewer tiles
+            Tile t = {};
+            return t;
+        }
+        lo += k * step;
+        if (step == 1) {
+            rest = number - __builtin_amdgcn_readlane(after, k);
+            break;
+        }
+        count = min(step, count - k * step);
+    }
+    // of the segments with more than lo tiles, the one with `rest` of them in front of it
+    unsigned long long mask = __ballot(tiles > lo);
+    for (; rest > 0; --rest) mask &= mask - 1;
+    const int s = __ffsll(static_cast<long long>(mask)) - 1;
+    Tile t;
+    t.segment = s;
+    t.begin = __builtin_amdgcn_readlane(begin, s);
+    t.end = max(t.begin, __builtin_amdgcn_readlane(next, s));
+    t.first = t.begin + (from_back ? __builtin_amdgcn_readlane(tiles, s) - 1 - lo : lo) * Rows;
+    return t;
+}
+
+// More: 64 candidates at a time.  The last step's candidates are the bounds.
+template <int Rows>
+__device__ __forceinline__ Tile find_by_number(const int *cu, int sequences, int tokens, int number)
 {
     const int lane = threadIdx.x & 63;
     int lo = 0, count = sequences + 2;
@@ -53,6 +99,14 @@ __device__ __forceinline__ Tile find_tile(const int *cu, int sequences, int toke
     return t;
 }
 
+// Every wavefront searches for itself.  from_back: the first tiles of a segment have the most work.
+template <int Rows>
+__device__ __forceinline__ Tile find_tile(const int *cu, int sequences, int tokens, int number, bool from_back)
+{
+    return sequences <= 62 ? find_by_work<Rows>(cu, sequences, tokens, number, from_back)
+                           : find_by_number<Rows>(cu, sequences, tokens, number);
+}
+
 // The larger of, and the sum over, a lane and the one 32 away.
 __device__ __forceinline__ void both_halves(float &x, float &y)
 {
@@ -66,7 +120,7 @@ __device__ __forceinline__ float both_max(float x)
 {
     float y;
     both_halves(x, y);
-    return fmaxf(x, y);
+    return __builtin_elementwise_maximum(x, y);
 }
 __device__ __forceinline__ float both_sum(float x)
 {
