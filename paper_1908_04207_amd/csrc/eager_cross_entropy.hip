@@ -38,13 +38,14 @@ struct Product {
     void *out;               // [b row][a row]
     long long out_stride;
     int accumulate;
-    float2 *stats;           // [a tile][b row]: maximum, sum
+    float2 *stats;           // [a tile][b row]: maximum (as a power of two), sum
     float *right;            // logit of the target
     const long long *target;
     const float *lse, *dloss;
     long long first;         // vocabulary index of a row 0
     int live;                // rows of a that are vocabulary (the rest is padding)
     int vocab;
+    int whole;               // one tile of a holds the vocabulary
     const int *counted;      // device: rows of x that count (gather_kernel), or NULL: all of them
     int counted_k;           // they are k, not the rows of b
 };
@@ -238,7 +239,9 @@ __device__ __forceinline__ void product(const Product &p, int id, char *tile0, c
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
                         if (whole || 32 * i + 8 * (r >> 2) + (r & 3) < live) top = fmaxf(top, c[i][j][r]);
-                const float base = top == -__builtin_inff() ? 0.0f : top * kLog2e;
+                // in powers of two from here on: what rounding leaves of top * kLog2e stays in the exponents
+                top *= kLog2e;
+                const float base = top == -__builtin_inff() ? 0.0f : top;
 #pragma unroll
                 for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -252,7 +255,7 @@ __device__ __forceinline__ void product(const Product &p, int id, char *tile0, c
             const float other = __shfl_xor(top, 32, 64), other_sum = __shfl_xor(sum, 32, 64);
             const float both = fmaxf(top, other);
             const float zero = both == -__builtin_inff() ? 0.0f : both;
-            sum = sum * exp2_fast((top - zero) * kLog2e) + other_sum * exp2_fast((other - zero) * kLog2e);
+            sum = sum * exp2_fast(top - zero) + other_sum * exp2_fast(other - zero);
             if (half == 0) parts[wave % WM * BN + wave_b + 32 * j + lane] = make_float2(both, sum);
         }
         __syncthreads();
@@ -262,7 +265,7 @@ __device__ __forceinline__ void product(const Product &p, int id, char *tile0, c
             for (int i = 1; i < WM; ++i) {
                 const float2 q = parts[i * BN + n];
                 const float both = fmaxf(all.x, q.x), zero = both == -__builtin_inff() ? 0.0f : both;
-                all = make_float2(both, all.y * exp2_fast((all.x - zero) * kLog2e) + q.y * exp2_fast((q.x - zero) * kLog2e));
+                all = make_float2(both, all.y * exp2_fast(all.x - zero) + q.y * exp2_fast(q.x - zero));
             }
             if (b0 + n < p.b.rows) p.stats[tile_a * p.b.rows + b0 + n] = all;
         }
@@ -282,39 +285,87 @@ __device__ __forceinline__ void product(const Product &p, int id, char *tile0, c
     };
     const int live = static_cast<int>(min(p.live - a0, static_cast<long long>(BM)));
     const long long rows = Epi == kResult ? p.live : b_side.rows;
+    if constexpr (Epi == kDlogits) {
+        float g[NI], others[NI], scale[NI];
+        int target[NI];
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-        const int in_b = wave_b + 32 * j + (lane & 31);
-        const long long row = b0 + in_b;
-        if (Epi == kDlogits) {
-            float lse = __builtin_inff(), g = 0.0f;     // rows that there are not: zeros
-            int target = -1;
+        for (int j = 0; j < NI; ++j) {
+            const long long row = b0 + wave_b + 32 * j + (lane & 31);
+            float lse = __builtin_inff();               // rows that there are not: zeros
+            g[j] = 0.0f, others[j] = -1.0f, scale[j] = 1.0f, target[j] = -1;
             if (row < rows) {
-                const long long v = p.target[row];
+                const long long v = p.target[row], from = v - p.first - a0;
                 lse = p.lse[row] * kLog2e;
-                g = v >= p.vocab ? __builtin_nanf("") : p.dloss[row];
-                const long long from = v - p.first - a0;
-                target = from >= wave_a && from < wave_a + 32 * MI ? static_cast<int>(from) : -1;
+                g[j] = v >= p.vocab ? __builtin_nanf("") : p.dloss[row];
+                target[j] = from >= wave_a && from < wave_a + 32 * MI ? static_cast<int>(from) : -1;
             }
 #pragma unroll
             for (int i = 0; i < MI; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) c[i][j][r] = exp2_fast(fmaf(c[i][j][r], kLog2e, -lse));
-            if (__any(target >= 0 || live < wave_a + 32 * MI)) {
+            if (__any(live < wave_a + 32 * MI)) {
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (wave_a + 32 * i + 8 * (r >> 2) + 4 * half + (r & 3) >= live) c[i][j][r] = 0.0f;
+            }
+        }
+        // With the whole vocabulary in one tile p is normalised anew and 1 - p of the target is the sum of the others:
+        // lse in fp32 is up to 2^-24 of itself off, too much for rows whose p is close to 1.
+        if (p.whole) {
+            float2 *parts = reinterpret_cast<float2 *>(tile0);         // [WM][BN]: others, target
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                float sum = 0.0f, its = 0.0f;
 #pragma unroll
                 for (int i = 0; i < MI; ++i)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        const int in = wave_a + 32 * i + 8 * (r >> 2) + 4 * half + (r & 3);
-                        if (in == target) c[i][j][r] -= 1.0f;
-                        if (in >= live) c[i][j][r] = 0.0f;
+                        const bool hit = wave_a + 32 * i + 8 * (r >> 2) + 4 * half + (r & 3) == target[j];
+                        sum += hit ? 0.0f : c[i][j][r];
+                        its += hit ? c[i][j][r] : 0.0f;
                     }
+                sum += __shfl_xor(sum, 32, 64);
+                its += __shfl_xor(its, 32, 64);
+                if (half == 0) parts[wave % WM * BN + wave_b + 32 * j + lane] = make_float2(sum, its);
             }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                float2 all = {};
+#pragma unroll
+                for (int i = 0; i < WM; ++i) {
+                    const float2 q = parts[i * BN + wave_b + 32 * j + (lane & 31)];
+                    all.x += q.x, all.y += q.y;
+                }
+                others[j] = -all.x;
+                scale[j] = 1.0f / (all.x + all.y);
+                if (g[j] == 0.0f) scale[j] = 0.0f;      // rows that there are not
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            if (__any(target[j] >= 0)) {
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (wave_a + 32 * i + 8 * (r >> 2) + 4 * half + (r & 3) == target[j])
+                            c[i][j][r] = p.whole ? others[j] : c[i][j][r] - 1.0f;
+            }
+            const float by = g[j] * scale[j];
 #pragma unroll
             for (int i = 0; i < MI; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) c[i][j][r] *= g;
+                for (int r = 0; r < 16; ++r) c[i][j][r] *= by;
         }
+    }
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+        const int in_b = wave_b + 32 * j + (lane & 31);
+        const long long row = b0 + in_b;
         const long long from = a0 + wave_a + 4 * half;
         const int limit = Epi == kDlogits ? BM : row < rows ? static_cast<int>(min(p.a.rows - from, static_cast<long long>(BM))) : 0;
         float *const sums = static_cast<float *>(p.out) + (slice * p.b.rows + row) * p.out_stride + from;
@@ -377,7 +428,7 @@ __global__ __launch_bounds__(Shape::Threads) void gradients_kernel(const Product
 __device__ __forceinline__ void join(float &top, float &sum, float2 q)
 {
     const float both = fmaxf(top, q.x), zero = both == -__builtin_inff() ? 0.0f : both;
-    sum = sum * exp2_fast((top - zero) * kLog2e) + q.y * exp2_fast((q.x - zero) * kLog2e);
+    sum = sum * exp2_fast(top - zero) + q.y * exp2_fast(q.x - zero);
     top = both;
 }
 
@@ -403,10 +454,11 @@ __global__ __launch_bounds__(1024) void rows_kernel(const float2 *stats, const f
     __syncthreads();
     if (wave || row >= rows) return;
     for (int i = 1; i < 16; ++i) join(top, sum, part[i][lane]);
-    const float all = fmaf(log2_fast(sum), kLn2, top);
+    // the largest logit is not added to the logarithm where the loss takes one away again
+    const float log_sum = log1pf(sum - 1.0f);
     const long long t = target[row];
-    lse[row] = all;
-    loss[row] = t < 0 ? 0.0f : t >= vocab ? __builtin_nanf("") : all - right[row];
+    lse[row] = fmaf(top, kLn2, log_sum);
+    loss[row] = t < 0 ? 0.0f : t >= vocab ? __builtin_nanf("") : fmaf(fmaf(-right[row], kLog2e, top), kLn2, log_sum);
 }
 
 // The rows that count in the backward pass - those with a target and a weight - side by side: the
@@ -596,6 +648,7 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
             p.first = first;
             p.live = live;
             p.vocab = a.vocab;
+            p.whole = a.vocab <= kSides[c.logits][0];
             p.target = g.target_out;
             p.lse = g.lse_out;
             p.dloss = g.dloss_out;

@@ -263,3 +263,24 @@ def test_refusals(ops):
     _refused(lambda: ops.cross_entropy_backward(loss[:5], x, head, target, lse), "dloss")
     _refused(lambda: ops.cross_entropy_backward(loss, x, head, target, lse, dw=head.t().contiguous().t()), "dw")
     _refused(lambda: ops.cross_entropy_backward(loss, x, head, target, lse, want=(False, False)), "eager_cross_entropy_backward")
+
+
+@pytest.mark.parametrize("rows,vocab", [(50, 2), (300, 20), (130, 128), (1000, 101)])
+def test_cross_entropy_of_confident_rows(ops, rows, vocab):
+    """Few classes and targets that lead by 12: losses and 1 - p of about vocab e^-12.  The loss comes from a sum
+    of 1 + vocab e^-12 in fp32, so it is good to vocab 2^-24 of a one; dl's entries are sums and
+    exponentials of their own, good to the logits' error (|l| 2^-24 times a few tens of products' roundings)
+    relative to themselves - and neither loses more to log-sum-exps that are held in fp32."""
+    gen = torch.Generator().manual_seed(vocab)
+    width = 64
+    w = _normal(gen, vocab, width, sigma=0.02).double()
+    target = torch.randint(0, vocab, (rows,), generator=gen)
+    x = (w[target] * (12 / (w[target].square().sum(1, keepdim=True))) + _normal(gen, rows, width).double()).float().cuda()
+    w, target, g = w.float().cuda(), target.cuda(), torch.rand(rows, generator=gen).cuda()
+    loss, lse = ops.cross_entropy(x, w, target)
+    dx, dw = ops.cross_entropy_backward(g, x, w, target, lse)
+    want = mo.cross_entropy(x, w, target, g)
+    assert ((loss.double() - want["loss"][0]).abs() <= 4 * vocab * mo.E + 2e-5 * want["loss"][0]).all()
+    for name, t in (("dx", dx), ("dw", dw)):
+        off = float((t.double() - want[name][0]).norm() / want[name][0].norm())
+        assert off < 1e-4, (name, off)
