@@ -3,10 +3,29 @@
 //   P = exp(scale Q K^T - lse),  dP = dO V^T,  delta = rowsum(dO * O),  dS = P * (dP - delta)
 //   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
 //
-// Two kernels, each with sums of its own in registers, so that no sum depends on the order of
-// workgroups: queries_kernel goes over the keys for a tile of queries (dQ, and delta on the way),
-// keys_kernel over the queries for a tile of keys (dK, dV).  Both form P and dP again from the
-// inputs, transposed to each other, so that the lane's side is the side that is summed for.
+// Two kinds of workgroups, each with sums of its own in registers, so that no sum depends on their
+// order: queries() goes over the keys for a tile of queries (dQ, and delta on the way),
+// keys() over the queries for a tile of keys (dK, dV).  Both form P and dP again from the
+// inputs, transposed to each other, so that the lane's side is the side that is summed for: 7
+// products of 2 D operations an allowed pair where the formulas have 5.  Heads that share keys are
+// summed by `parts` workgroups in fp32 and joined in the parts' order.  Batches of little work have
+// both in one launch (gradients_kernel), the rows' delta then from a launch before it.
+//
+// P and dS are rounded to the inputs' type for the second products: in bf16 those run at 16 times
+// the fp32 rate, and the error is that of the formula's own operands.  Sums are fp32.
+//
+// Bound, heads of 64: the vector instructions beside the matrix ones (an exponential, two products
+// and two conversions an element, on the same SIMD; about 1000 clocks beside 512 in a tile of 64 x 32)
+// and, in short sequences, the last key tile's chain of all its queries.  Heads of 128: one
+// wavefront a SIMD in the keys' kernel (316 registers: two accumulators of 128 x 32), so waits of a
+// tile's loads and of the chain S -> P -> dP -> dS are not covered by another wavefront.
+// Measured: bf16, 16 heads (4 of keys) of 64, 16 sequences, 8192 tokens: 43 us dq, 49 us dk and dv, 12 us
+// parts; 25 heads of 64, 8 sequences of 1024: 68 and 90 us (589 and 597 TFLOP/s, masked pairs not counted); 8
+// heads (2) of 128, one of 16384: 833 and 1364 us (990 and 806 TFLOP/s); fp32, 16 heads (8) of 64, 9 sequences,
+// 4099 tokens: 164 and 171 us.
+//
+// Slower, same sizes: both halves of a tile side by side with heads of 128 (registers spill: 4.8 ms), two tiles of queries
+// a workgroup (dq 84 us instead of 52 in the first).
 #include "eager_packed.h"
 
 namespace eager {
@@ -17,20 +36,23 @@ constexpr int kTile = 64;            // keys (queries) of a tile
 // How many halves of a tile are unrolled: with long heads two of them side by side do not fit the registers.
 template <typename T, int DP> constexpr int kHalves = DP * sizeof(T) > 128 ? 1 : 2;
 
+// Arrays of their own, so that the compiler knows a load into one apart from a read of another.
+#define EAGER_TILES __shared__ __align__(1024) char tile0[kTile * DP * sizeof(T)]; \
+                    __shared__ __align__(1024) char tile1[kTile * DP * sizeof(T)]; \
+                    __shared__ __align__(1024) char tile2[kTile * DP * sizeof(T)]; \
+                    __shared__ __align__(1024) char tile3[kTile * DP * sizeof(T)]
+#define EAGER_ROWS  __shared__ __align__(1024) float rows0[2][kTile]; \
+                    __shared__ __align__(1024) float rows1[2][kTile]
+
+// dq of 128 rows of a head, id.  write: also leaves what keys() begins its sums with, for every row.
 template <typename T, int DP>
-__global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void queries_kernel(const AttentionArgs a)
+__device__ __forceinline__ void queries(const AttentionArgs &a, int id, bool write, char *k_tile0, char *v_tile0, char *k_tile1, char *v_tile1)
 {
-    constexpr int Chunks = DP * sizeof(T) / 16, TileBytes = kTile * Chunks * 16, Steps = DP / 16;
-    // arrays of their own, so that the compiler knows a load into one apart from a read of another
-    __shared__ __align__(1024) char k_tile0[TileBytes];
-    __shared__ __align__(1024) char v_tile0[TileBytes];
-    __shared__ __align__(1024) char k_tile1[TileBytes];
-    __shared__ __align__(1024) char v_tile1[TileBytes];
+    constexpr int Chunks = DP * sizeof(T) / 16, Steps = DP / 16;
     T *const type = nullptr;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int head = blockIdx.x % a.q_heads;
-    const Tile t = find_tile<kRows>(a.cu, a.sequences, static_cast<int>(a.tokens),
-                                    blockIdx.x / a.q_heads, false);
+    const int head = id % a.q_heads;
+    const Tile t = find_tile<kRows>(a.cu, a.sequences, static_cast<int>(a.tokens), id / a.q_heads, false);
     if (t.first >= t.end) return;
     if (t.segment == 0 || t.segment == a.sequences + 1) {
         clear_rows<T, kRows>(a.dq, head, t.first, t.end, a.dim);
@@ -56,7 +78,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void queries_ke
     float lse = 0.0f;
     if (there) {
         lse = a.lse[head * a.tokens + row];
-        if (lane < 32) {                                // what keys_kernel's sums begin with
+        if (lane < 32 && write) {
             a.delta[head * a.tokens + row] = -delta;
             a.start[head * a.tokens + row] = -lse / a.scale;
         }
@@ -124,20 +146,15 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void queries_ke
 // the most queries, would run alone at the end.  With more than one part the sums of each go to the
 // workspace in fp32 and parts_kernel adds them.
 template <typename T, int DP>
-__global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void keys_kernel(const AttentionArgs a)
+__device__ __forceinline__ void keys(const AttentionArgs &a, int id, char *q_tile0, char *g_tile0, char *q_tile1, char *g_tile1,
+                                     float (*rows0)[kTile], float (*rows1)[kTile])
 {
-    constexpr int Chunks = DP * sizeof(T) / 16, TileBytes = kTile * Chunks * 16, Steps = DP / 16;
-    __shared__ __align__(1024) char q_tile0[TileBytes];
-    __shared__ __align__(1024) char g_tile0[TileBytes];
-    __shared__ __align__(1024) char q_tile1[TileBytes];
-    __shared__ __align__(1024) char g_tile1[TileBytes];
-    __shared__ __align__(1024) float rows0[2][kTile];
-    __shared__ __align__(1024) float rows1[2][kTile];
+    constexpr int Chunks = DP * sizeof(T) / 16, Steps = DP / 16;
     T *const type = nullptr;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int shared = blockIdx.x % (a.kv_heads * a.parts), kv_head = shared / a.parts, part = shared % a.parts;
+    const int shared = id % (a.kv_heads * a.parts), kv_head = shared / a.parts, part = shared % a.parts;
     const int heads = a.q_heads / a.kv_heads / a.parts;
-    const Tile t = find_tile<kRows>(a.cu, a.sequences, static_cast<int>(a.tokens), blockIdx.x / (a.kv_heads * a.parts), true);
+    const Tile t = find_tile<kRows>(a.cu, a.sequences, static_cast<int>(a.tokens), id / (a.kv_heads * a.parts), true);
     if (t.first >= t.end) return;
     // where the sums go: [part][k, v][kv head][token][dim]
     float *const sums = a.sums + (static_cast<long long>(part) * 2 * a.kv_heads + kv_head) * a.tokens * a.dim;
@@ -256,6 +273,55 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void keys_kerne
     }
 }
 
+template <typename T, int DP>
+__global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void queries_kernel(const AttentionArgs a)
+{
+    EAGER_TILES;
+    queries<T, DP>(a, blockIdx.x, true, tile0, tile1, tile2, tile3);
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void keys_kernel(const AttentionArgs a)
+{
+    EAGER_TILES;
+    EAGER_ROWS;
+    keys<T, DP>(a, blockIdx.x, tile0, tile1, tile2, tile3, rows0, rows1);
+}
+
+// Both in one launch, after rows_kernel has left what keys() wants of every row.
+template <typename T, int DP>
+__global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void gradients_kernel(const AttentionArgs a, int of_keys)
+{
+    EAGER_TILES;
+    EAGER_ROWS;
+    const int id = blockIdx.x;
+    if (id < of_keys) keys<T, DP>(a, id, tile0, tile1, tile2, tile3, rows0, rows1);
+    else queries<T, DP>(a, id - of_keys, false, tile0, tile1, tile2, tile3);
+}
+
+// delta and lse of 32 rows of a head a wavefront, added in the order of queries()
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void rows_kernel(const AttentionArgs a)
+{
+    const int lane = threadIdx.x & 63, head = blockIdx.x % a.q_heads;
+    const long long row = static_cast<long long>(blockIdx.x / a.q_heads) * kRows + 32 * (threadIdx.x >> 6) + (lane & 31);
+    const bool there = row < a.tokens;
+    const T *do_row = static_cast<const T *>(a.dout.data) + row * a.dout.row + head * a.dout.head;
+    const T *o_row = static_cast<const T *>(a.out.data) + row * a.out.row + head * a.out.head;
+    float delta = 0.0f;
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+        const typename Operand<T>::frag g = row_operand(do_row, s, lane, a.dim, there), o = row_operand(o_row, s, lane, a.dim, there);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) delta = fmaf(static_cast<float>(g[j]), static_cast<float>(o[j]), delta);
+    }
+    delta = both_sum(delta);
+    if (there && lane < 32) {
+        a.delta[head * a.tokens + row] = -delta;
+        a.start[head * a.tokens + row] = -a.lse[head * a.tokens + row] / a.scale;
+    }
+}
+
 // dk (blockIdx.y = 0) and dv (1) from the parts' sums, four values a thread, in the parts' order
 template <typename T>
 __global__ __launch_bounds__(256) void parts_kernel(const AttentionArgs a)
@@ -277,8 +343,15 @@ template <typename T, int DP>
 void enqueue(const AttentionArgs &a, hipStream_t stream)
 {
     const long long tiles = tile_numbers(a.tokens, a.sequences, kRows);
-    hipLaunchKernelGGL((queries_kernel<T, DP>), dim3(static_cast<unsigned>(tiles * a.q_heads)), dim3(256), 0, stream, a);
-    hipLaunchKernelGGL((keys_kernel<T, DP>), dim3(static_cast<unsigned>(tiles * a.kv_heads * a.parts)), dim3(256), 0, stream, a);
+    const unsigned of_queries = static_cast<unsigned>(tiles * a.q_heads), of_keys = static_cast<unsigned>(tiles * a.kv_heads * a.parts);
+    if (attention_together(tiles * a.q_heads, DP)) {
+        const long long blocks = (a.tokens + kRows - 1) / kRows * a.q_heads;
+        hipLaunchKernelGGL((rows_kernel<T, DP>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((gradients_kernel<T, DP>), dim3(of_keys + of_queries), dim3(256), 0, stream, a, static_cast<int>(of_keys));
+    } else {
+        hipLaunchKernelGGL((queries_kernel<T, DP>), dim3(of_queries), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((keys_kernel<T, DP>), dim3(of_keys), dim3(256), 0, stream, a);
+    }
     if (a.parts > 1) {
         const long long quads = a.tokens * a.kv_heads * (a.dim / 4);
         hipLaunchKernelGGL((parts_kernel<T>), dim3(static_cast<unsigned>((quads + 255) / 256), 2), dim3(256), 0, stream, a);

@@ -11,6 +11,20 @@
 // All products are one kernel.  Operand A is the side whose index runs within a lane's results
 // (vocabulary for the logits, width for the gradients), B the side that the lane counts, so that
 // softmax statistics stay within a lane and results are stored four values at a time.
+//
+// Statistics and the sums of dx and dw are fp32; dl is rounded to the inputs' type, since it is the operand of
+// two products whose other side has that type.  fp32 products are six bf16 ones of operands cut into three bf16
+// pieces of 8 bits each: a bf16 instruction has 16 times the rate of the fp32 one, so six cost less than one.
+//
+// Bound by the matrix instructions, busy 45 to 60 % of the time at about 2.1 GHz; what they wait for is the barrier between
+// tiles and, in the last round, tiles that do not fill the card.  Measured (rows x width x vocabulary): 4096 x 1024 x 50257
+// bf16 forward 453 us (930 TFLOP/s), backward with a tenth of the rows masked: dl 446 us, dx and dw 822 us (923 TFLOP/s of the
+// rows that count); 8191 x 1600 x 50257 forward 1157 us (1139 TFLOP/s), two pieces of dl 622 and of dx and dw 1306 us
+// (957 with 5 % masked); fp32 1019 x 1024 x 50257: 684, 691, 1258 us (153 TFLOP/s forward, 150 backward); 61 x 1024 x 50257
+// forward 19.4 us, 5.3 TB/s of the projection.
+//
+// Slower: the compiler's own order of matrix instructions and reads (10 to 15 %, see spread()), 4 wavefronts of 256 x 256
+// (8 %), wavefronts of raised priority (no effect).
 #include "eager_matrix.h"
 #include "eager_model.h"
 #include "eager_model_rules.h"
@@ -462,7 +476,8 @@ __global__ __launch_bounds__(1024) void rows_kernel(const float2 *stats, const f
 }
 
 // The rows that count in the backward pass - those with a target and a weight - side by side: the
-// products leave the others out, whatever stands in them.
+// products leave the others out, whatever stands in them.  Bound by one copy of x; 4096 x 1024 in bf16 7.4 us, and with
+// a tenth of the targets masked the products have a tenth less to do.
 struct Gather {
     const void *x;
     const long long *target;

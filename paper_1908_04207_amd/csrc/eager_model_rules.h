@@ -17,7 +17,10 @@ typedef TileShape<128, 128, 2, 2, 2> Medium;
 typedef TileShape<128, 64, 4, 1, 3> Narrow;
 
 // What a product costs in a shape of tiles: rounds of as many tiles as run at once, each a number of
-// steps of k (128 bytes) and what filling and emptying takes, in microseconds.
+// steps of k (128 bytes) and what filling and emptying takes, in microseconds.  Fitted to sweeps of all three; where they
+// differ most (rows x width x vocabulary, bf16, forward, Large / Medium / Narrow, us): 1019 x 1024 x 50257 128 / 125 / 146,
+// 61 x 1024 x 50257 35 / 27 / 25, 100 x 512 x 3000 21 / 16 / 13; backward, Large / Medium: 4000 x 800 x 500 126 / 77, and 42
+// with dw in slices of the rows.
 struct Cost {
     double step, rest;
 };
@@ -161,7 +164,8 @@ constexpr int kAttentionRows = 128;
 inline long long tile_numbers(long long tokens, int sequences, int rows) { return tokens / rows + sequences + 2; }
 
 // Two workgroups have a compute unit: 512 run at once, and about four rounds of them even out what a
-// causal mask leaves to each.
+// causal mask leaves to each.  Measured (16 heads of 64, 4 of keys, 16 sequences of 8192 tokens, bf16): 4 parts 50 us and
+// 12 for their sums, 2 parts (of a limit of 600) 62 and 8.
 inline int attention_parts(long long tokens, int q_heads, int kv_heads, int sequences)
 {
     const int group = q_heads / kv_heads;
@@ -171,6 +175,14 @@ inline int attention_parts(long long tokens, int q_heads, int kv_heads, int sequ
         do ++parts; while (group % parts);
     return parts;
 }
+
+// The backward pass: both its kernels in one launch (true), or dq's and then the keys'. One launch has both tails at once
+// and runs one kernel's long rows beside the other's; two leave dq's kernel its own registers and so more wavefronts a
+// SIMD. Measured, apart and in one launch, us, by dq's workgroups * dim (bf16 unless said): 1000 tokens as 1 sequence, 8
+// heads of 128 (9216) 83 and 55; 4000 as 1, 16 of 64 (33792) 181 and 152; the same as 4 (36864) 65 and 60, in fp32 336 and
+// 325; 4000 as 4, 8 of 128 (36864) 90 and 68, in fp32 513 and 333; 6000 as 2, 16 of 64 (49152) 160 and 164; 6000 as 12,
+// 8 of 128 (59392) 73 and 76; 8192 as 16, 16 of 64 (81920) 80 and 85.
+inline bool attention_together(long long workgroups, int dim) { return workgroups * dim <= 40960; }
 
 inline long long attention_row_bytes(long long tokens, int q_heads) { return (tokens * q_heads * 4 + 15) / 16 * 16; }
 

@@ -7,6 +7,11 @@
 // A head of D values belongs to a group of lanes, each with V consecutive values of the first half
 // and the V of the second half that they are rotated with, so the rotation needs no exchange and
 // the two means are one butterfly over the group.
+//
+// Bound by memory: forward reads x and writes y once, backward reads x and dy and writes dx; 1/r is formed again from
+// x, which is read anyway.  Means, norms and gains' sums are fp32.  Measured: fp32, 20011 tokens of 50 heads of 64
+// (256 MB an array): forward 93 us (5.5 TB/s), backward 165 us (4.7 TB/s of three arrays) and 7 us for the gains' sums;
+// bf16, 8192 tokens of 20 heads of 64 (21 MB, which the last cache holds): 11.4, 16.5 and 4.1 us; 37 tokens: 4.8 us, a launch.
 #include "eager_matrix.h"
 #include "eager_model.h"
 

@@ -85,6 +85,19 @@ def test_attention_many_tiles(ops, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,kv", [(64, 6), (64, 2), (40, 2), (128, 6), (128, 3), (104, 1)])
+@pytest.mark.parametrize("empty", [0, 120])
+def test_attention_backward_in_one_launch_and_in_two(ops, dtype, D, kv, empty):
+    """The same sequences with and without many empty ones among them, which give the launches more
+    workgroups (all of which find nothing): one launch for all gradients, or one for dq's alone first."""
+    q, k, v, dout, cu = _attention_inputs([130] + [0] * empty + [1, 300, 64], 6, kv, D, dtype, 1, 3, 78)
+    got = _run_attention(ops, q, k, v, dout, cu)
+    want = _on_gpu(mo.attention(q.cuda(), k.cuda(), v.cuda(), cu, D ** -0.5, dout.cuda()))
+    for name in got:
+        _check(name, got[name], *want[name])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("T,kv", [(300, 1), (70000, 1)])
 def test_attention_parts_agree(ops, dtype, T, kv):
     """Heads that share keys, summed in parts (few tokens) or by one workgroup (many): as with the keys
