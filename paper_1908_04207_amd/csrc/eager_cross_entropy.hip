@@ -123,14 +123,18 @@ __device__ __forceinline__ typename Operand<T>::frag read_side(const char *tile,
     return read_columns<Rows * sizeof(T) / 16, sizeof(T) == 2 ? 2 : 31>(tile, row0, 16 * step, 8, 4, lane, static_cast<T *>(nullptr));
 }
 
-// The tile of workgroup `id`: workgroups id, id + 8, ... run on the same chiplet (one second-level
-// cache), so each chiplet gets a contiguous share of the tiles, in which 8 tiles of b are gone
-// through for every tile of a.
-__device__ __forceinline__ void place(int id, int tiles_a, int tiles_b, int &tile_a, int &tile_b)
+// Workgroups id, id + 8, ... run on the same chiplet (one second-level cache): which of `all` pieces of work
+// workgroup `id` takes, so that each chiplet has a contiguous share.
+__device__ __forceinline__ int in_order(int id, int all)
+{
+    const int chiplet = id & 7, share = all >> 3, rest = all & 7;
+    return chiplet * share + min(chiplet, rest) + (id >> 3);
+}
+
+// Tile n: 8 tiles of b are gone through for every tile of a.
+__device__ __forceinline__ void place(int n, int tiles_a, int tiles_b, int &tile_a, int &tile_b)
 {
     constexpr int Group = 8;
-    const int all = tiles_a * tiles_b, chiplet = id & 7, share = all >> 3, rest = all & 7;
-    const int n = chiplet * share + min(chiplet, rest) + (id >> 3);
     const int group = n / (Group * tiles_a), first = group * Group, width = min(Group, tiles_b - first);
     const int in = n - group * Group * tiles_a;
     tile_b = first + in % width;
@@ -142,15 +146,12 @@ __device__ __forceinline__ void place(int id, int tiles_a, int tiles_b, int &til
 // read while the step before is multiplied, the first step's of a tile during the last one of the
 // tile before, so the barrier between tiles stands in the shadow of matrix instructions.
 template <typename T, typename Shape, bool ColumnsA, bool ColumnsB, int Epi>
-__device__ __forceinline__ void product(const Product &p, int id, char *tile0, char *tile1)
+__device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b, int slice, char *tile0, char *tile1)
 {
     constexpr int BM = Shape::A, BN = Shape::B, WM = Shape::WavesA, WN = Shape::WavesB;
     constexpr int Waves = WM * WN, MI = BM / WM / 32, NI = BN / WN / 32, Steps = kDepth<T> / 16;
     typedef typename Operand<T>::frag frag;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int slice = id / (p.tiles_a * p.tiles_b);
-    int tile_a, tile_b;
-    place(id - slice * p.tiles_a * p.tiles_b, p.tiles_a, p.tiles_b, tile_a, tile_b);
     const long long a0 = static_cast<long long>(tile_a) * BM, b0 = static_cast<long long>(tile_b) * BN;
     const int wave_a = wave % WM * (BM / WM), wave_b = wave / WM * (BN / WN);
     Side a_side = p.a, b_side = p.b;
@@ -421,11 +422,41 @@ __device__ __forceinline__ void product(const Product &p, int id, char *tile0, c
 #define EAGER_TILES __shared__ __align__(1024) char tile0[(Shape::A + Shape::B) * 128]; \
                     __shared__ __align__(1024) char tile1[(Shape::A + Shape::B) * 128]
 
+// Large tiles are one to a compute unit, and a last round of a few takes as long as a full one: up to kUnits / 4
+// tiles of it are cut in four, so that every unit has a quarter.
 template <typename T, typename Shape, int Epi>
 __global__ __launch_bounds__(Shape::Threads) void logits_kernel(const Product p)
 {
     EAGER_TILES;
-    product<T, Shape, false, false, Epi>(p, blockIdx.x, tile0, tile1);
+    const int rows = Epi == kStats ? static_cast<int>(p.b.rows) : *p.counted, tiles_b = (rows + Shape::B - 1) / Shape::B;
+    const int all = p.tiles_a * tiles_b;
+    int id = blockIdx.x, tile_a, tile_b;
+    if constexpr (Shape::Quartered) {
+        const int last = all % kUnits <= kUnits / 4 ? all % kUnits : 0, full = all - last;
+        if (id >= full) {
+            id -= full;
+            if (id >= 4 * last) return;
+            const int n = in_order(id, 4 * last);
+            place(full + n / 4, p.tiles_a, tiles_b, tile_a, tile_b);
+            product<T, Quarter, false, false, Epi>(p, tile_a, 4 * tile_b + n % 4, 0, tile0, tile1);
+            return;
+        }
+        place(in_order(id, full), p.tiles_a, tiles_b, tile_a, tile_b);
+    } else {
+        if (id >= all) return;
+        place(in_order(id, all), p.tiles_a, tiles_b, tile_a, tile_b);
+    }
+    product<T, Shape, false, false, Epi>(p, tile_a, tile_b, 0, tile0, tile1);
+}
+
+// The tile of workgroup `id` of a product in slices.
+template <typename T, typename Shape, bool ColumnsB, int Epi>
+__device__ __forceinline__ void gradient(const Product &p, int id, char *tile0, char *tile1)
+{
+    const int all = p.tiles_a * p.tiles_b, slice = id / all;
+    int tile_a, tile_b;
+    place(in_order(id - slice * all, all), p.tiles_a, p.tiles_b, tile_a, tile_b);
+    product<T, Shape, true, ColumnsB, Epi>(p, tile_a, tile_b, slice, tile0, tile1);
 }
 
 // dw and dx of a piece in one launch: what one leaves idle in its last round the other fills.
@@ -435,8 +466,8 @@ __global__ __launch_bounds__(Shape::Threads) void gradients_kernel(const Product
 {
     EAGER_TILES;
     const int id = blockIdx.x;
-    if (id < dw_tiles) product<T, Shape, true, true, SumsOfDw ? kSums : kResult>(dw, id, tile0, tile1);
-    else product<T, Shape, true, false, kSums>(dx, id - dw_tiles, tile0, tile1);
+    if (id < dw_tiles) gradient<T, Shape, true, SumsOfDw ? kSums : kResult>(dw, id, tile0, tile1);
+    else gradient<T, Shape, false, kSums>(dx, id - dw_tiles, tile0, tile1);
 }
 
 __device__ __forceinline__ void join(float &top, float &sum, float2 q)
@@ -606,7 +637,8 @@ int lay_out(Product &p, int shape)
 template <typename T, int Epi>
 void launch_logits(Product &p, int shape, hipStream_t stream)
 {
-    const dim3 grid(lay_out<T>(p, shape));
+    const int tiles = lay_out<T>(p, shape);
+    const dim3 grid(shape == kLarge ? std::min(4 * tiles, tiles + 3 * (kUnits / 4)) : tiles);
     if (shape == kLarge) hipLaunchKernelGGL((logits_kernel<T, Large, Epi>), grid, dim3(Large::Threads), 0, stream, p);
     else if (shape == kMedium) hipLaunchKernelGGL((logits_kernel<T, Medium, Epi>), grid, dim3(Medium::Threads), 0, stream, p);
     else hipLaunchKernelGGL((logits_kernel<T, Narrow, Epi>), grid, dim3(Narrow::Threads), 0, stream, p);

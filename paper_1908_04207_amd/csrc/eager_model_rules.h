@@ -7,12 +7,20 @@ namespace eager {
 
 inline long long round_up(long long x, long long to) { return (x + to - 1) / to * to; }
 
+constexpr int kUnits = 256;      // compute units
+// A quarter of a large tile takes this of its time (bound by shared memory: three reads for two matrix instructions).
+// Measured, three rounds of tiles and 32 more, the 32 whole or in quarters: 2048 rows, width 1024, bf16 135 and 125 us; 1600
+// 186 and 171; fp32 661 (of medium tiles) and 612, 1015 and 943.
+constexpr double kQuarter = 0.45;
+
 // A workgroup's tile, its wavefronts, and how many workgroups have a compute unit (by their shared memory).
 template <int A_, int B_, int WavesA_, int WavesB_, int OfUnit_>
 struct TileShape {
     static constexpr int A = A_, B = B_, WavesA = WavesA_, WavesB = WavesB_, Threads = 64 * WavesA * WavesB, OfUnit = OfUnit_;
+    static constexpr bool Quartered = A == 256 && B == 256;
 };
 typedef TileShape<256, 256, 2, 4, 1> Large;
+typedef TileShape<256, 64, 4, 2, 1> Quarter;             // of a large one: a last round that is not full
 typedef TileShape<128, 128, 2, 2, 2> Medium;
 typedef TileShape<128, 64, 4, 1, 3> Narrow;
 
@@ -37,7 +45,9 @@ double logits_time(long long rows, int width, long long vocab, int bytes)
 {
     const Cost c = cost_of<Shape>(bytes);
     const long long tiles = round_up(rows, Shape::B) / Shape::B * (round_up(vocab, Shape::A) / Shape::A);
-    return rounds_of<Shape>(tiles) * (round_up(width, 128 / bytes) / (128 / bytes) * c.step + c.rest);
+    const long long last = Shape::Quartered ? tiles % kUnits : 0;
+    const double rounds = last && last <= kUnits / 4 ? static_cast<double>(tiles / kUnits) + kQuarter : rounds_of<Shape>(tiles);
+    return rounds * (round_up(width, 128 / bytes) / (128 / bytes) * c.step + c.rest);
 }
 
 // dw and dx of a piece: their tiles follow each other, so only the last round is not full
