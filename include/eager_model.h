@@ -96,6 +96,8 @@ int eager_qk_norm_rope_backward(int dtype, const eager_packed *shape, const eage
  * Rows that belong to no sequence get out = 0 and lse = -infinity.
  * Non-finite keys, values or queries reach no other sequence; inside their sequence they may
  * reach every row of it.
+ * fp32 products are formed from three bf16 pieces of every operand, whose sum is the operand: within two
+ * roundings of an fp32 product; an infinite operand gives NaN.
  * Errors: EINVAL (NULL, alignment, strides, sizes, scale not positive and finite), EDEVICE.
  *
  * Backward: dq, dk, dv from the forward pass's inputs and results and dout.  Gradients of a key
@@ -133,8 +135,7 @@ typedef struct {
  * negative target or a dloss of zero are left out from the start: they cost nothing, whatever x
  * holds there reaches no gradient, and their dx is zero.  dx or dw may be NULL (not wanted).  In bf16
  * the dl of a piece are held in bf16 between the products.
- * fp32 products are formed from three bf16 pieces of every operand, whose sum is the operand: within two
- * roundings of an fp32 product; an infinite operand gives NaN.
+ * fp32 products as in eager_attention().
  * workspace_bytes: what the forward (backward = 0) or the backward pass (1) needs.
  */
 int eager_cross_entropy(int dtype, const eager_projection *shape, const void *x, const void *w,

@@ -6,7 +6,7 @@
 // transposed, S^T = K Q^T and O^T = V^T P^T: a lane then holds scores of one row only, so maximum
 // and sum are taken in registers (one exchange between the halves of a wavefront), the rescaling
 // of O is one factor a lane, and P^T is the second product's operand as it stands.  P is rounded to
-// the inputs' type for that product (a matrix instruction takes both sides in one type); its sum l is taken
+// bf16 for that product where the inputs are (a matrix instruction takes both sides in one type); its sum l is taken
 // in fp32 before the rounding.
 //
 // Tiles of keys come by loads that write shared memory directly, one tile ahead, and tiles of queries
@@ -18,7 +18,7 @@
 // instructions busy 44 %, vector instructions 50 % of the time.
 // Measured: bf16, 16 heads (4 of keys) of 64: 113 tokens 6.2 us, 16 sequences of 8192 tokens 31 us; 25 heads of 64, 8
 // sequences of 1024: 50 us (532 TFLOP/s, masked pairs not counted); 8 heads (2) of 128, one sequence of 16384: 587 us
-// (937 TFLOP/s); fp32, 16 heads (8) of 64, 9 sequences, 4099 tokens: 110 us.
+// (937 TFLOP/s); fp32, 16 heads (8) of 64, 9 sequences, 4099 tokens: 87 us.
 //
 // Slower, 16 sequences and 8 x 1024 of the above: two groups of wavefronts that share a row's keys and join their
 // statistics (39 and 62 us against 31 and 52), two tiles of queries a workgroup (43 and 61).
@@ -54,9 +54,9 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attention_
     const int kv_head = head / (a.q_heads / a.kv_heads);
     const int wave_row = t.first + 32 * wave, row = wave_row + (lane & 31);
     const T *q_row = static_cast<const T *>(a.q.data) + static_cast<long long>(row) * a.q.row + head * a.q.head;
-    typename Operand<T>::frag q[Steps];
+    decltype(operand(typename Operand<T>::frag())) q[Steps];
 #pragma unroll
-    for (int s = 0; s < Steps; ++s) q[s] = row_operand(q_row, s, lane, a.dim, row < t.end);
+    for (int s = 0; s < Steps; ++s) q[s] = operand(row_operand(q_row, s, lane, a.dim, row < t.end));
 
     const char *k_base = reinterpret_cast<const char *>(static_cast<const T *>(a.k.data) + kv_head * a.k.head);
     const char *v_base = reinterpret_cast<const char *>(static_cast<const T *>(a.v.data) + kv_head * a.v.head);
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attention_
 #pragma unroll
         for (int i = 0; i < Steps; ++i)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) s[b] = mma(read_rows<Chunks>(k_tile, 32 * b, i, lane, type), q[i], s[b]);
+            for (int b = 0; b < 2; ++b) s[b] = mma(operand(read_rows<Chunks>(k_tile, 32 * b, i, lane, type)), q[i], s[b]);
         if (key0 + kKeys - 1 > wave_row) {
             const int seen = row - key0 - 4 * (lane >> 5);
 #pragma unroll
@@ -117,10 +117,10 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attention_
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const typename Operand<T>::frag p = as_operand<T>(s[b], h);
+                const auto p = operand(as_operand<T>(s[b], h));
 #pragma unroll
                 for (int d = 0; d < DP / 32; ++d)
-                    o[d] = mma(read_columns<Chunks>(v_tile, 32 * d, 32 * b + 16 * h, 4, 8, lane, type), p, o[d]);
+                    o[d] = mma(operand(read_columns<Chunks>(v_tile, 32 * d, 32 * b + 16 * h, 4, 8, lane, type)), p, o[d]);
             }
     };
     stage(t.begin, k_tile0, v_tile0);

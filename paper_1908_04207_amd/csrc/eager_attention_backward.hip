@@ -11,8 +11,8 @@
 // summed by `parts` workgroups in fp32 and joined in the parts' order.  Batches of little work have
 // both in one launch (gradients_kernel), the rows' delta then from a launch before it.
 //
-// P and dS are rounded to the inputs' type for the second products: in bf16 those run at 16 times
-// the fp32 rate, and the error is that of the formula's own operands.  Sums are fp32.
+// With bf16 inputs P and dS are rounded to bf16 for the second products, whose other sides are bf16:
+// the error is that of the formula's own operands.  Sums are fp32, and so are P and dS with fp32 inputs.
 //
 // Bound, heads of 64: the vector instructions beside the matrix ones (an exponential, two products
 // and two conversions an element, on the same SIMD; about 1000 clocks beside 512 in a tile of 64 x 32)
@@ -22,7 +22,7 @@
 // Measured: bf16, 16 heads (4 of keys) of 64, 16 sequences, 8192 tokens: 43 us dq, 49 us dk and dv, 12 us
 // parts; 25 heads of 64, 8 sequences of 1024: 68 and 90 us (589 and 597 TFLOP/s, masked pairs not counted); 8
 // heads (2) of 128, one of 16384: 833 and 1364 us (990 and 806 TFLOP/s); fp32, 16 heads (8) of 64, 9 sequences,
-// 4099 tokens: 164 and 171 us.
+// 4099 tokens: 124 and 156 us.
 //
 // Slower, same sizes: both halves of a tile side by side with heads of 128 (registers spill: 4.8 ms), two tiles of queries
 // a workgroup (dq 84 us instead of 52 in the first).
@@ -64,15 +64,15 @@ __device__ __forceinline__ void queries(const AttentionArgs &a, int id, bool wri
     const T *q_row = static_cast<const T *>(a.q.data) + static_cast<long long>(row) * a.q.row + head * a.q.head;
     const T *do_row = static_cast<const T *>(a.dout.data) + static_cast<long long>(row) * a.dout.row + head * a.dout.head;
     const T *o_row = static_cast<const T *>(a.out.data) + static_cast<long long>(row) * a.out.row + head * a.out.head;
-    typename Operand<T>::frag q[Steps], g[Steps];
+    decltype(operand(typename Operand<T>::frag())) q[Steps], g[Steps];
     float delta = 0.0f;
 #pragma unroll
     for (int s = 0; s < Steps; ++s) {
-        q[s] = row_operand(q_row, s, lane, a.dim, there);
-        g[s] = row_operand(do_row, s, lane, a.dim, there);
-        const typename Operand<T>::frag o = row_operand(o_row, s, lane, a.dim, there);
+        const typename Operand<T>::frag x = row_operand(do_row, s, lane, a.dim, there), o = row_operand(o_row, s, lane, a.dim, there);
+        q[s] = operand(row_operand(q_row, s, lane, a.dim, there));
+        g[s] = operand(x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) delta = fmaf(static_cast<float>(g[s][j]), static_cast<float>(o[j]), delta);
+        for (int j = 0; j < 8; ++j) delta = fmaf(static_cast<float>(x[j]), static_cast<float>(o[j]), delta);
     }
     delta = both_sum(delta);
     float lse = 0.0f;
@@ -107,8 +107,8 @@ __device__ __forceinline__ void queries(const AttentionArgs &a, int id, bool wri
             f32x16 s = {}, dp = {};
 #pragma unroll
             for (int i = 0; i < Steps; ++i) {
-                s = mma(read_rows<Chunks>(k_tile, 32 * b, i, lane, type), q[i], s);
-                dp = mma(read_rows<Chunks>(v_tile, 32 * b, i, lane, type), g[i], dp);
+                s = mma(operand(read_rows<Chunks>(k_tile, 32 * b, i, lane, type)), q[i], s);
+                dp = mma(operand(read_rows<Chunks>(v_tile, 32 * b, i, lane, type)), g[i], dp);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = exp2_fast(fmaf(s[i], c, -lse));
@@ -122,10 +122,10 @@ __device__ __forceinline__ void queries(const AttentionArgs &a, int id, bool wri
             for (int i = 0; i < 16; ++i) s[i] *= dp[i] - delta;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const typename Operand<T>::frag ds = as_operand<T>(s, h);
+                const auto ds = operand(as_operand<T>(s, h));
 #pragma unroll
                 for (int d = 0; d < DP / 32; ++d)
-                    dq[d] = mma(read_columns<Chunks>(k_tile, 32 * d, 32 * b + 16 * h, 4, 8, lane, type), ds, dq[d]);
+                    dq[d] = mma(operand(read_columns<Chunks>(k_tile, 32 * d, 32 * b + 16 * h, 4, 8, lane, type)), ds, dq[d]);
             }
         }
     };
@@ -174,11 +174,11 @@ __device__ __forceinline__ void keys(const AttentionArgs &a, int id, char *q_til
     const bool there = key < t.end;
     const T *k_row = static_cast<const T *>(a.k.data) + static_cast<long long>(key) * a.k.row + kv_head * a.k.head;
     const T *v_row = static_cast<const T *>(a.v.data) + static_cast<long long>(key) * a.v.row + kv_head * a.v.head;
-    typename Operand<T>::frag k[Steps], v[Steps];
+    decltype(operand(typename Operand<T>::frag())) k[Steps], v[Steps];
 #pragma unroll
     for (int s = 0; s < Steps; ++s) {
-        k[s] = row_operand(k_row, s, lane, a.dim, there);
-        v[s] = row_operand(v_row, s, lane, a.dim, there);
+        k[s] = operand(row_operand(k_row, s, lane, a.dim, there));
+        v[s] = operand(row_operand(v_row, s, lane, a.dim, there));
     }
     const long long q_stride = a.q.row * sizeof(T), g_stride = a.dout.row * sizeof(T);
     const int chunks = a.dim * sizeof(T) / 16;
@@ -227,8 +227,8 @@ __device__ __forceinline__ void keys(const AttentionArgs &a, int id, char *q_til
             }
 #pragma unroll
             for (int i = 0; i < Steps; ++i) {
-                s = mma(read_rows<Chunks>(q_tile, 32 * b, i, lane, type), k[i], s);
-                dp = mma(read_rows<Chunks>(g_tile, 32 * b, i, lane, type), v[i], dp);
+                s = mma(operand(read_rows<Chunks>(q_tile, 32 * b, i, lane, type)), k[i], s);
+                dp = mma(operand(read_rows<Chunks>(g_tile, 32 * b, i, lane, type)), v[i], dp);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = exp2_fast(s[i] * c);
@@ -242,11 +242,11 @@ __device__ __forceinline__ void keys(const AttentionArgs &a, int id, char *q_til
             for (int i = 0; i < 16; ++i) dp[i] *= s[i];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const typename Operand<T>::frag p = as_operand<T>(s, h), ds = as_operand<T>(dp, h);
+                const auto p = operand(as_operand<T>(s, h)), ds = operand(as_operand<T>(dp, h));
 #pragma unroll
                 for (int d = 0; d < DP / 32; ++d) {
-                    dv[d] = mma(read_columns<Chunks>(g_tile, 32 * d, 32 * b + 16 * h, 4, 8, lane, type), p, dv[d]);
-                    dk[d] = mma(read_columns<Chunks>(q_tile, 32 * d, 32 * b + 16 * h, 4, 8, lane, type), ds, dk[d]);
+                    dv[d] = mma(operand(read_columns<Chunks>(g_tile, 32 * d, 32 * b + 16 * h, 4, 8, lane, type)), p, dv[d]);
+                    dk[d] = mma(operand(read_columns<Chunks>(q_tile, 32 * d, 32 * b + 16 * h, 4, 8, lane, type)), ds, dk[d]);
                 }
             }
         }

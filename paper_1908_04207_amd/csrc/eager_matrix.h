@@ -2,9 +2,9 @@
 //
 // One 32x32x16 step is the unit: a lane holds 8 elements of each operand, of row (column)
 // lane % 32, at k = 8 * (lane / 32) + 0..7; of the result it holds column lane % 32 and rows
-// 8 * (i / 4) + 4 * (lane / 32) + i % 4, i = 0..15.  bf16 takes one instruction for it.  fp32
-// takes eight of 32x32x2, each with one element of every lane: the order of k inside a step is
-// free as long as both operands agree, so both types share every layout below.
+// 8 * (i / 4) + 4 * (lane / 32) + i % 4, i = 0..15.  bf16 takes one instruction for it, fp32 six, on
+// operands cut into bf16 pieces in registers.  The order of k inside a step is free as long as both
+// operands agree, and both types share every layout below.
 //
 // Tiles come from global memory straight into shared memory, 16 bytes a lane, through buffer
 // descriptors whose length makes reads beyond an operand's end return zeros.  The shared-memory
@@ -42,13 +42,6 @@ __device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c)
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
-__device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c)
-{
-#pragma unroll
-    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
-    return c;
-}
-
 // fp32 operands as three bf16 pieces, each what rounding left of the one before: their sum is the
 // operand exactly.  (Magnitudes from 2^128 (1 - 2^-9) on count as infinite.)
 struct Pieces {
@@ -68,7 +61,9 @@ __device__ __forceinline__ Pieces cut(f32x8 x)
 
 // The product of such operands without the three smallest of the nine products of pieces, together at
 // most 2^-23 of the operands' product (two roundings of an fp32 product).  Six instructions of
-// 32 clocks, where the fp32 ones take eight of 64.
+// 32 clocks, where the fp32 ones take eight of 64; cutting costs 44 vector instructions an operand, which run beside them.
+// Measured against the fp32 instructions: attention over 8192 tokens, 16 heads of 64, 1 sequence: forward 1153 us -> 924,
+// backward 4091 -> 3382; 16 sequences 95 -> 78 and 365 -> 318; 8 heads of 128, 16 sequences 109 -> 96 and 371 -> 366.
 __device__ __forceinline__ f32x16 mma(const Pieces &a, const Pieces &b, f32x16 c)
 {
     c = mma(a.low, b.high, c);
