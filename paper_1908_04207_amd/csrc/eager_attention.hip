@@ -18,7 +18,7 @@
 // instructions busy 44 %, vector instructions 50 % of the time.
 // Measured: bf16, 16 heads (4 of keys) of 64: 113 tokens 6.2 us, 16 sequences of 8192 tokens 31 us; 25 heads of 64, 8
 // sequences of 1024: 50 us (532 TFLOP/s, masked pairs not counted); 8 heads (2) of 128, one sequence of 16384: 587 us
-// (937 TFLOP/s); fp32, 16 heads (8) of 64, 9 sequences, 4099 tokens: 87 us.
+// (937 TFLOP/s); fp32, 16 heads (8) of 64, 9 sequences, 4099 tokens: 77 us.
 //
 // Slower, 16 sequences and 8 x 1024 of the above: two groups of wavefronts that share a row's keys and join their
 // statistics (39 and 62 us against 31 and 52), two tiles of queries a workgroup (43 and 61).

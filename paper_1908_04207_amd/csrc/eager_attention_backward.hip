@@ -22,7 +22,7 @@
 // Measured: bf16, 16 heads (4 of keys) of 64, 16 sequences, 8192 tokens: 43 us dq, 49 us dk and dv, 12 us
 // parts; 25 heads of 64, 8 sequences of 1024: 68 and 90 us (589 and 597 TFLOP/s, masked pairs not counted); 8
 // heads (2) of 128, one of 16384: 833 and 1364 us (990 and 806 TFLOP/s); fp32, 16 heads (8) of 64, 9 sequences,
-// 4099 tokens: 124 and 156 us.
+// 4099 tokens: 108 and 125 us.
 //
 // Slower, same sizes: both halves of a tile side by side with heads of 128 (registers spill: 4.8 ms), two tiles of queries
 // a workgroup (dq 84 us instead of 52 in the first).

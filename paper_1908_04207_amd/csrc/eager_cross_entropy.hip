@@ -20,7 +20,7 @@
 // tiles and, in the last round, tiles that do not fill the card.  Measured (rows x width x vocabulary): 4096 x 1024 x 50257
 // bf16 forward 453 us (930 TFLOP/s), backward with a tenth of the rows masked: dl 434 us, dx and dw 822 us (923 TFLOP/s of the
 // rows that count); 8191 x 1600 x 50257 forward 1157 us (1139 TFLOP/s), two pieces of dl 602 and of dx and dw 1306 us
-// (957 with 5 % masked); fp32 1019 x 1024 x 50257: 677, 666, 1258 us (155 TFLOP/s forward, 150 backward); 61 x 1024 x 50257
+// (957 with 5 % masked); fp32 1019 x 1024 x 50257: 659, 655, 1196 us (159 TFLOP/s forward, 158 backward); 61 x 1024 x 50257
 // forward 19.4 us, 5.3 TB/s of the projection.
 //
 // Slower: the compiler's own order of matrix instructions and reads (10 to 15 %, see spread()), 4 wavefronts of 256 x 256

@@ -48,22 +48,40 @@ struct Pieces {
     bf16x8 high, middle, low;
 };
 
+// x less its piece: a product of two pairs with an addend, so the pieces need not be unpacked (exact: the
+// difference has no more digits than x, and the pair's other element counts nothing); with unpacked pieces 44
+// instructions instead of 28 for both cuts, and 15 % more time in attention
+__device__ __forceinline__ f32x8 less(f32x8 x, bf16x8 piece)
+{
+    // (-1, 0) and (0, -1), from registers: as a constant in the instruction the first one is taken for the second
+    unsigned low = 0x0000bf80u, high = 0xbf800000u;
+    asm("" : "+s"(low), "+s"(high));
+    const bf16x2 first = __builtin_bit_cast(bf16x2, low), second = __builtin_bit_cast(bf16x2, high);
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+        const bf16x2 pair = {piece[j], piece[j + 1]};
+        x[j] = __builtin_amdgcn_fdot2_f32_bf16(pair, first, x[j], false);
+        x[j + 1] = __builtin_amdgcn_fdot2_f32_bf16(pair, second, x[j + 1], false);
+    }
+    return x;
+}
+
 __device__ __forceinline__ Pieces cut(f32x8 x)
 {
     Pieces p;
     p.high = __builtin_convertvector(x, bf16x8);
-    x -= __builtin_convertvector(p.high, f32x8);
+    x = less(x, p.high);
     p.middle = __builtin_convertvector(x, bf16x8);
-    x -= __builtin_convertvector(p.middle, f32x8);
+    x = less(x, p.middle);
     p.low = __builtin_convertvector(x, bf16x8);
     return p;
 }
 
 // The product of such operands without the three smallest of the nine products of pieces, together at
 // most 2^-23 of the operands' product (two roundings of an fp32 product).  Six instructions of
-// 32 clocks, where the fp32 ones take eight of 64; cutting costs 44 vector instructions an operand, which run beside them.
-// Measured against the fp32 instructions: attention over 8192 tokens, 16 heads of 64, 1 sequence: forward 1153 us -> 924,
-// backward 4091 -> 3382; 16 sequences 95 -> 78 and 365 -> 318; 8 heads of 128, 16 sequences 109 -> 96 and 371 -> 366.
+// 32 clocks, where the fp32 ones take eight of 64; cutting costs 28 vector instructions an operand, which run beside them.
+// Measured against the fp32 instructions: attention over 8192 tokens, 16 heads of 64, 1 sequence: forward 1153 us -> 823,
+// backward 4091 -> 2853; 16 sequences 95 -> 71 and 365 -> 269; 8 heads of 128, 16 sequences 109 -> 87 and 371 -> 308.
 __device__ __forceinline__ f32x16 mma(const Pieces &a, const Pieces &b, f32x16 c)
 {
     c = mma(a.low, b.high, c);

@@ -189,8 +189,7 @@ inline int attention_parts(long long tokens, int q_heads, int kv_heads, int sequ
 // The backward pass: both its kernels in one launch (true), or dq's and then the keys'. One launch has both tails at once
 // and runs one kernel's long rows beside the other's; two leave dq's kernel its own registers and so more wavefronts a
 // SIMD. Measured, apart and in one launch, us, by dq's workgroups * dim (bf16 unless said): 1000 tokens as 1 sequence, 8
-// heads of 128 (9216) 83 and 55; 4000 as 1, 16 of 64 (33792) 181 and 152; the same as 4 (36864) 65 and 60, in fp32 299 and
-// 301; 4000 as 4, 8 of 128 (36864) 90 and 68, in fp32 483 and 328; 6000 as 2, 16 of 64 (49152) 160 and 164; 6000 as 12,
+// heads of 128 (9216) 83 and 55; 4000 as 1, 16 of 64 (33792) 181 and 152; the same as 4 (36864) 65 and 60; 4000 as 4, 8 of 128 (36864) 90 and 68; 6000 as 2, 16 of 64 (49152) 160 and 164; 6000 as 12,
 // 8 of 128 (59392) 73 and 76; 8192 as 16, 16 of 64 (81920) 80 and 85.
 inline bool attention_together(long long workgroups, int dim) { return workgroups * dim <= 40960; }
 
