@@ -16,11 +16,11 @@
 // two products whose other side has that type.  fp32 products are six bf16 ones of operands cut into three bf16
 // pieces of 8 bits each: a bf16 instruction has 16 times the rate of the fp32 one, so six cost less than one.
 //
-// Bound by the matrix instructions, busy 45 to 60 % of the time at about 2.1 GHz; what they wait for is the barrier between
+// Bound by the matrix instructions, busy 54 to 58 % of the time; what they wait for is the barrier between
 // tiles and, in the last round, tiles that do not fill the card.  Measured (rows x width x vocabulary): 4096 x 1024 x 50257
 // bf16 forward 453 us (930 TFLOP/s), backward with a tenth of the rows masked: dl 434 us, dx and dw 822 us (923 TFLOP/s of the
 // rows that count); 8191 x 1600 x 50257 forward 1157 us (1139 TFLOP/s), two pieces of dl 602 and of dx and dw 1306 us
-// (957 with 5 % masked); fp32 1019 x 1024 x 50257: 659, 655, 1196 us (159 TFLOP/s forward, 158 backward); 61 x 1024 x 50257
+// (957 with 5 % masked); fp32 1019 x 1024 x 50257: 651, 637, 1166 us (161 TFLOP/s forward, 162 backward); 61 x 1024 x 50257
 // forward 19.4 us, 5.3 TB/s of the projection.
 //
 // Slower: the compiler's own order of matrix instructions and reads (10 to 15 %, see spread()), 4 wavefronts of 256 x 256
