@@ -224,11 +224,13 @@ __device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b
         body(tile1, tile0, t + 1);
     }
     if (t < count) body(tile0, tile1, t);
+    // the last step has asked for zeros beyond the product, in either tile: every wavefront's are there
+    // before an epilogue writes into the tiles
     wait_loads();
+    __syncthreads();
 
     const int half = lane >> 5;
     if (Epi == kStats) {
-        __syncthreads();
         float2 *parts = reinterpret_cast<float2 *>(tile0);             // [WM][BN]
         const int live = static_cast<int>(min(p.live - a0, static_cast<long long>(BM))) - wave_a - 4 * half;
 #pragma unroll
@@ -293,7 +295,6 @@ __device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b
     constexpr bool Across = sizeof(T) == 2 && Epi != kSums;
     constexpr int RowChunks = BM / 8, RowsOfTile0 = (BM + BN) * 128 / (BM * 2);
     static_assert(!Across || BN <= 2 * RowsOfTile0, "results fit the tiles");
-    if (Across) __syncthreads();
     auto place_of = [&](int row, int chunk) {
         char *tile = row < RowsOfTile0 ? tile0 + row * BM * 2 : tile1 + (row - RowsOfTile0) * BM * 2;
         return tile + (chunk ^ (row & (RowChunks - 1) & 31)) * 16;

@@ -1,0 +1,45 @@
+"""The model operators where kernels share memory between steps, where statistics are joined over many tiles,
+and where calls come in forms that torch makes by itself; against the definitions in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from oracle import model_oracle as mo
+from test_gpu_model_ops import _check, _normal
+
+pytestmark = pytest.mark.gpu
+DTYPES = [torch.bfloat16, torch.float32]
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_1908_04207_amd import model_ops
+    return model_ops
+
+
+def _on_gpu(pairs):
+    return {n: tuple(t.cpu() for t in p) for n, p in pairs.items()}
+
+
+# widths of an odd number of 128-byte steps (32 values in fp32, 64 in bf16), so that the loads under way after the
+# last step go to the tile in shared memory that the epilogue uses next
+@pytest.mark.parametrize("dtype,rows,width,vocab", [(torch.float32, 300, 96, 100), (torch.float32, 500, 800, 100),
+                                                    (torch.float32, 2000, 96, 64), (torch.float32, 200, 32, 100),
+                                                    (torch.float32, 3656, 160, 3), (torch.float32, 130, 72, 128),
+                                                    (torch.bfloat16, 300, 192, 100), (torch.bfloat16, 500, 64, 100),
+                                                    (torch.bfloat16, 3656, 320, 3), (torch.bfloat16, 130, 136, 128)])
+def test_cross_entropy_one_tile_of_vocabulary_odd_steps(ops, dtype, rows, width, vocab):
+    gen = torch.Generator().manual_seed(rows + width)
+    x, w = _normal(gen, rows, width, dtype=dtype).cuda(), _normal(gen, vocab, width, dtype=dtype, sigma=1 / math.sqrt(width)).cuda()
+    target = torch.randint(0, vocab, (rows,), generator=gen)
+    target[torch.rand(rows, generator=gen) < 0.1] = -1
+    target, dloss = target.cuda(), _normal(gen, rows, sigma=0.1).cuda()
+    loss, lse = ops.cross_entropy(x, w, target)
+    dx, dw = ops.cross_entropy_backward(dloss, x, w, target, lse)
+    want = _on_gpu(mo.cross_entropy(x, w, target, dloss))
+    for name, t in (("loss", loss), ("lse", lse), ("dx", dx), ("dw", dw)):
+        _check(name, t, *want[name])
+    for _ in range(5):
+        for a, b in zip((dx, dw), ops.cross_entropy_backward(dloss, x, w, target, lse)):
+            assert torch.equal(a, b)
