@@ -14,7 +14,8 @@ take comes back as NotImplemented and is checked and refused, or called, here.
     out, lse = attention(q, k, v, cu_seqlens)
     loss, lse = cross_entropy(x, w, target)
 
-each with its `_backward`, and `QKNormRope`, `Attention`, `CrossEntropy` for torch's autograd.
+each with its `_backward`, and `QKNormRope`, `Attention`, `CrossEntropy` for torch's autograd (first
+derivatives; asked for the derivatives of gradients they raise).
 """
 from __future__ import annotations
 
@@ -84,6 +85,29 @@ class _Nothing:
 
 
 _NOTHING = _Nothing()
+
+
+class _Once(torch.autograd.Function):
+    """Gradients as they are, in a graph that wants to go on from them: it ends here with an error."""
+
+    @staticmethod
+    def forward(ctx, what, count, *tensors):
+        ctx.what = what
+        return tuple(t.view_as(t) for t in tensors[:count])
+
+    @staticmethod
+    def backward(ctx, *_):
+        _refuse(f"{ctx.what}: second derivatives are not formed")
+
+
+def _once(what: str, grads, *depends):
+    """The gradients that a backward pass returns.  In one that is recorded (create_graph) they depend on
+    `depends`, through a node that refuses: without it they would count as constants there."""
+    if not torch.is_grad_enabled():
+        return tuple(grads)
+    given = [g for g in grads if g is not None]
+    marked = iter(_Once.apply(what, len(given), *given, *depends))
+    return tuple(None if g is None else next(marked) for g in grads)
 
 
 # ------------------------------------------------------------------------------ heads
@@ -162,8 +186,9 @@ class QKNormRope(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dq_out, dk_out):
         q, k, wq, wk, cos, sin, positions = ctx.saved_tensors
-        return (*qk_norm_rope_backward(dq_out.contiguous(), dk_out.contiguous(), q, k, wq, wk, cos, sin, positions,
-                                       ctx.eps), None, None, None, None)
+        grads = qk_norm_rope_backward(dq_out.contiguous(), dk_out.contiguous(), q, k, wq, wk, cos, sin, positions,
+                                      ctx.eps)
+        return (*_once("QKNormRope", grads, dq_out, dk_out, q, k, wq, wk), None, None, None, None)
 
 
 # ------------------------------------------------------------------------------ attention
@@ -231,7 +256,8 @@ class Attention(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dout):
         q, k, v, out, lse, cu_seqlens = ctx.saved_tensors
-        return (*attention_backward(dout.contiguous(), q, k, v, out, lse, cu_seqlens, ctx.scale), None, None)
+        grads = attention_backward(dout.contiguous(), q, k, v, out, lse, cu_seqlens, ctx.scale)
+        return (*_once("Attention", grads, dout, q, k, v), None, None)
 
 
 # ------------------------------------------------------------------------------ loss
@@ -300,4 +326,5 @@ class CrossEntropy(torch.autograd.Function):
         x, w, target, lse = ctx.saved_tensors
         if not any(ctx.needs_input_grad[:2]):
             return None, None, None
-        return (*cross_entropy_backward(dloss.contiguous(), x, w, target, lse, want=ctx.needs_input_grad[:2]), None)
+        grads = cross_entropy_backward(dloss.contiguous(), x, w, target, lse, want=ctx.needs_input_grad[:2])
+        return (*_once("CrossEntropy", grads, dloss, x, w), None)

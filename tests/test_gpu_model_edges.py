@@ -43,3 +43,15 @@ def test_cross_entropy_one_tile_of_vocabulary_odd_steps(ops, dtype, rows, width,
     for _ in range(5):
         for a, b in zip((dx, dw), ops.cross_entropy_backward(dloss, x, w, target, lse)):
             assert torch.equal(a, b)
+
+
+def test_second_derivatives_of_the_library_s_own_are_refused(ops):
+    from paper_1908_04207_amd import binding as eb
+    gen = torch.Generator().manual_seed(2)
+    x, w = (_normal(gen, n, 64).cuda().requires_grad_() for n in (20, 30))
+    loss = ops.CrossEntropy.apply(x, w, torch.arange(20, device="cuda")).sum()
+    grads = torch.autograd.grad(loss, (x, w), create_graph=True)
+    with pytest.raises(eb.EagerError, match="second derivatives"):
+        (loss + sum(g.square().sum() for g in grads)).backward(retain_graph=True)
+    loss.backward()                                      # the graph of the loss itself is still there
+    assert torch.equal(x.grad, grads[0]) and torch.equal(w.grad, grads[1])
