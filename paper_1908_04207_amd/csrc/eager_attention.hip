@@ -96,7 +96,8 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attention_
         best = both_max(best);
         const float base = best == -__builtin_inff() ? 0.0f : best * c;
         if (__any(best != top)) {                       // a new maximum: rare after the first tiles
-            const float keep = exp2_fast(fmaf(top, c, -base));
+            // from the rounded reference that the sums have: exactly 1 for the rows whose maximum stays
+            const float keep = exp2_fast(top * c - base);
             top = best;
             sum *= keep;
 #pragma unroll
@@ -133,7 +134,9 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attention_
     if (row < t.end) {
         T *out = static_cast<T *>(a.out.data) + static_cast<long long>(row) * a.out.row + head * a.out.head;
         store_row<T, DP>(out, o, 1.0f / sum, lane, a.dim);
-        if (lane < 32) a.lse[head * a.tokens + row] = fmaf(log2_fast(sum), kLn2, top * a.scale);
+        // what rounding the reference top * c has left is in the sum, and taken out of its logarithm
+        const float left = top == -__builtin_inff() ? 0.0f : fmaf(top, c, -(top * c));
+        if (lane < 32) a.lse[head * a.tokens + row] = fmaf(top, a.scale, (log2_fast(sum) - left) * kLn2);
     }
 }
 

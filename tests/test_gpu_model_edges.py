@@ -55,3 +55,32 @@ def test_second_derivatives_of_the_library_s_own_are_refused(ops):
         (loss + sum(g.square().sum() for g in grads)).backward(retain_graph=True)
     loss.backward()                                      # the graph of the loss itself is still there
     assert torch.equal(x.grad, grads[0]) and torch.equal(w.grad, grads[1])
+
+
+@pytest.mark.parametrize("n,centre", [(2048, 50), (16384, 50), (16384, 200), (16384, -120)])
+def test_attention_statistics_over_many_tiles(ops, n, centre):
+    """Rows whose scores lie around `centre` beside rows whose maximum moves in every tile of keys, fp32.  Inputs
+    are multiples of 1/16, so the scores (up to 2^11) are exact; what is left is rounding of the result and of the
+    logarithm (a unit of each, relative to it), of exponentials, and of a sum whose roundings have random
+    signs: 64 E covers 4096 tiles of it.  A factor per tile that is not exactly 1 would add up beyond."""
+    gen = torch.Generator().manual_seed(centre)
+    D, scale = 64, 0.125
+    grid = lambda *s: (torch.randint(-24, 25, s, generator=gen) / 16).float()      # noqa: E731
+    q, k, v = grid(n, 1, D) / 2, grid(n, 1, D) / 2, _normal(gen, n, 1, D)
+    q = (q * 16).round() / 16
+    k = (k * 16).round() / 16
+    q[..., 0], k[..., 0] = centre / scale, 1.0
+    k[:, 0, 1] = torch.arange(n) * 64 // n / 8                     # a ramp from 0 to 8 that every 32nd row looks at
+    q[..., 1] = 0.0
+    q[7::32, :, 1] = 16.0
+    q, k, v = q.cuda(), k.cuda(), v.cuda()
+    out, lse = ops.attention(q, k, v, torch.tensor([0, n], dtype=torch.int32, device="cuda"), scale)
+    first = n - 256
+    later = torch.arange(n, device="cuda") > torch.arange(first, n, device="cuda")[:, None]
+    s = (scale * (q[first:, 0].double() @ k[:, 0].double().t())).masked_fill(later, -math.inf)
+    want = torch.logsumexp(s, 1)
+    off = (lse[0, first:].double() - want).abs()
+    assert (off <= 2 * mo.E * want.abs() + 64 * mo.E).all(), float(off.max())
+    p = torch.exp(s - want[:, None])
+    off = (out[first:, 0].double() - p @ v[:, 0].double()).abs()
+    assert (off <= 64 * mo.E * (p @ v[:, 0].double().abs())).all(), float(off.max())
