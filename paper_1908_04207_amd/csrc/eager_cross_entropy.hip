@@ -60,6 +60,7 @@ struct Product {
     int live;                // rows of a that are vocabulary (the rest is padding)
     int vocab;
     int whole;               // one tile of a holds the vocabulary
+    float *others;           // [a tile][b row]: sums of p without the target's, or NULL
     const int *counted;      // device: rows of x that count (gather_kernel), or NULL: all of them
     int counted_k;           // they are k, not the rows of b
 };
@@ -327,9 +328,38 @@ __device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b
                         if (wave_a + 32 * i + 8 * (r >> 2) + 4 * half + (r & 3) >= live) c[i][j][r] = 0.0f;
             }
         }
-        // With the whole vocabulary in one tile p is normalised anew and 1 - p of the target is the sum of the others:
-        // lse in fp32 is up to 2^-24 of itself off, too much for rows whose p is close to 1.
-        if (p.whole) {
+        // 1 - p of the target is the sum of the others: lse in fp32 is up to 2^-24 of itself off, too much for rows
+        // whose p is close to 1.  With the whole vocabulary in one tile p is normalised anew as well; with more tiles
+        // each leaves its sum and targets_kernel puts the target's entry in.
+        if (p.others) {
+            float *parts = reinterpret_cast<float *>(tile0);           // [WM][BN]
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                float sum = 0.0f;
+                if (__any(target[j] >= 0)) {
+#pragma unroll
+                    for (int i = 0; i < MI; ++i)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            sum += wave_a + 32 * i + 8 * (r >> 2) + 4 * half + (r & 3) == target[j] ? 0.0f : c[i][j][r];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < MI; ++i)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) sum += c[i][j][r];
+                }
+                sum += __shfl_xor(sum, 32, 64);
+                if (half == 0) parts[wave % WM * BN + wave_b + 32 * j + lane] = sum;
+            }
+            __syncthreads();
+            for (int n = threadIdx.x; n < BN && b0 + n < rows; n += 64 * Waves) {
+                float all = 0.0f;
+#pragma unroll
+                for (int i = 0; i < WM; ++i) all += parts[i * BN + n];
+                p.others[tile_a * p.b.rows + b0 + n] = all;
+            }
+            __syncthreads();
+        } else if (p.whole) {
             float2 *parts = reinterpret_cast<float2 *>(tile0);         // [WM][BN]: others, target
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
@@ -606,6 +636,30 @@ __global__ __launch_bounds__(1024) void before_kernel(const Gather g, int *befor
     }
 }
 
+// The targets' entries of dl, 16 rows a workgroup: minus the others' sum, 64 threads a row.  Bound by the latency of
+// the loads and the launch.
+template <typename T>
+__global__ __launch_bounds__(1024) void targets_kernel(const Product p, T *dl)
+{
+    __shared__ float part[16][kJoined];
+    const int in = threadIdx.x % kJoined, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = *p.counted;
+    const long long row = static_cast<long long>(blockIdx.x) * kJoined + in;
+    float sum = 0.0f;
+    if (row < rows)
+#pragma unroll 4
+        for (int t = threadIdx.x / kJoined; t < p.tiles_a; t += 1024 / kJoined) sum += p.others[t * p.b.rows + row];
+#pragma unroll
+    for (int other = kJoined; other < 64; other *= 2) sum += __shfl_xor(sum, other, 64);
+    if (lane < kJoined) part[wave][in] = sum;
+    __syncthreads();
+    if (threadIdx.x >= kJoined || row >= rows) return;
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += part[i][in];
+    const long long v = p.target[row];
+    if (v < p.vocab) dl[row * p.out_stride + v] = static_cast<T>(-sum * p.dloss[row]);
+}
+
 // dx (and dw) from the slices' sums, four values a thread
 struct Sums {
     const float *sums;       // [slices][rows_padded][width]
@@ -711,7 +765,11 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
             p.counted = counted;
             p.out = dl;
             p.out_stride = padded;
+            p.others = c.pieces == 1 && !p.whole ? reinterpret_cast<float *>(a.workspace + l.others) : nullptr;
             launch_logits<T, kDlogits>(p, c.logits, stream);
+            if (p.others)
+                hipLaunchKernelGGL((targets_kernel<T>), dim3(static_cast<unsigned>((a.rows + kJoined - 1) / kJoined)), dim3(1024), 0,
+                                   stream, p, dl);
         }
         Product dx = {}, dw = {};
         int dx_tiles = 0, dw_tiles = 0;

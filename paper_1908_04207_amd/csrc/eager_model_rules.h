@@ -72,6 +72,7 @@ enum { kLarge, kMedium, kNarrow };
 struct Cut {
     long long rows_padded, piece;
     int dx_slices, dw_slices, logits, gradients;
+    long long pieces;
 };
 
 inline int logits_shape(long long rows, int width, long long vocab, int bytes)
@@ -88,7 +89,7 @@ inline Cut cut_of(long long rows, int width, int vocab, int bytes)
     const long long padded = round_up(std::max(rows, 1ll), 256);
     const long long fit = std::max(4096ll, (1ll << 29) / bytes / padded / 256 * 256);
     const long long fewest = (vocab + fit - 1) / fit;
-    Cut best = {padded, 0, 1, 1, 0, 0};
+    Cut best = {padded, 0, 1, 1, 0, 0, 0};
     double least = 0;
     for (long long n = fewest; n < fewest + 6; ++n) {
         const long long piece = round_up((vocab + n - 1) / n, 256), pieces = (vocab + piece - 1) / piece;
@@ -104,7 +105,7 @@ inline Cut cut_of(long long rows, int width, int vocab, int bytes)
                     const double cost = (logits + one) * (pieces > 1 ? pieces - 1 + last : 1);
                     if (!best.piece || cost < least) {
                         least = cost;
-                        best = {padded, piece, dx, dw, shape, g};
+                        best = {padded, piece, dx, dw, shape, g, pieces};
                     }
                 }
         if (piece == 256) break;
@@ -119,7 +120,7 @@ constexpr long long kCountedByEach = 16384;
 
 // Where things are in the backward pass's workspace (bytes from its start).
 struct Layout {
-    long long dl, dx_sums, dw_sums, x, target, lse, dloss, place, before, counted, end;
+    long long dl, others, dx_sums, dw_sums, x, target, lse, dloss, place, before, counted, end;
 };
 
 inline Layout layout_of(const Cut &c, long long rows, int width, int bytes)
@@ -132,6 +133,7 @@ inline Layout layout_of(const Cut &c, long long rows, int width, int bytes)
     };
     Layout l;
     l.dl = take(c.rows_padded * c.piece * bytes);
+    l.others = take(c.pieces == 1 ? c.piece / 128 * rows * 4 : 0);       // a number a row and tile, of 128 at least
     l.dx_sums = take(c.dx_slices * rows * width * 4);
     l.dw_sums = take(c.dw_slices > 1 ? c.dw_slices * c.piece * width * 4 : 0);
     l.x = take(rows * width * bytes);

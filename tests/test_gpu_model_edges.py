@@ -84,3 +84,26 @@ def test_attention_statistics_over_many_tiles(ops, n, centre):
     p = torch.exp(s - want[:, None])
     off = (out[first:, 0].double() - p @ v[:, 0].double()).abs()
     assert (off <= 64 * mo.E * (p @ v[:, 0].double().abs())).all(), float(off.max())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,vocab", [(100, 100), (300, 129), (130, 300), (700, 1000), (257, 5003), (300, 40003), (2500, 3001)])
+def test_cross_entropy_gradients_of_confident_rows_any_vocabulary(ops, dtype, rows, vocab):
+    """Targets that lead by so much that 1 - p is about 1e-4, whatever the number of tiles.  Entries of dl are sums and
+    exponentials of their own, good to the logits' error: of width 64 at most 66 E of products that add up to
+    about the lead (up to 20), 8e-5 of the entry, in fp32; an entry 1 - p formed from a log-sum-exp in fp32
+    would be 5e-3 off.  bf16 inputs: 2^-8 of dl and of the result."""
+    gen = torch.Generator().manual_seed(vocab)
+    width, lead = 64, math.log(vocab) + 9
+    w = _normal(gen, vocab, width, dtype=dtype, sigma=0.02).double()
+    target = torch.randint(0, vocab, (rows,), generator=gen)
+    x = w[target] * (lead / w[target].square().sum(1, keepdim=True)) + 0.3 * _normal(gen, rows, width).double()
+    x, w = x.to(dtype).cuda(), w.to(dtype).cuda()
+    target[5], target = -1, target.cuda()
+    g = torch.rand(rows, generator=gen).cuda() + 0.1
+    lse = ops.cross_entropy(x, w, target)[1]
+    dx, dw = ops.cross_entropy_backward(g, x, w, target, lse)
+    want = mo.cross_entropy(x, w, target, g)
+    for name, t in (("dx", dx), ("dw", dw)):
+        off = float((t.double() - want[name][0]).norm() / want[name][0].norm())
+        assert off < (1e-4 if dtype == torch.float32 else 2.0 ** -8 + 1e-4), (name, off)
