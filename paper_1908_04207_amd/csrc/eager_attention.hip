@@ -22,6 +22,7 @@
 //
 // Slower, 16 sequences and 8 x 1024 of the above: two groups of wavefronts that share a row's keys and join their
 // statistics (39 and 62 us against 31 and 52), two tiles of queries a workgroup (43 and 61).
+#include "eager_launch.h"
 #include "eager_packed.h"
 
 namespace eager {
@@ -141,20 +142,17 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attention_
 }
 
 template <typename T>
-void enqueue(const AttentionArgs &a, hipStream_t stream)
+hipError_t enqueue(const AttentionArgs &a, hipStream_t stream)
 {
     const dim3 grid(static_cast<unsigned>(tile_numbers(a.tokens, a.sequences, kRows) * a.q_heads));
-    if (a.dim <= 64) hipLaunchKernelGGL((attention_kernel<T, 64>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((attention_kernel<T, 128>), grid, dim3(256), 0, stream, a);
+    return launch(a.dim <= 64 ? attention_kernel<T, 64> : attention_kernel<T, 128>, grid, dim3(256), 0, stream, a);
 }
 
 }  // namespace
 
 hipError_t launch_attention(const AttentionArgs &a, bool bf16, hipStream_t stream)
 {
-    if (bf16) enqueue<__bf16>(a, stream);
-    else enqueue<float>(a, stream);
-    return hipGetLastError();
+    return bf16 ? enqueue<__bf16>(a, stream) : enqueue<float>(a, stream);
 }
 
 }  // namespace eager

@@ -26,6 +26,7 @@
 //
 // Slower, same sizes: both halves of a tile side by side with heads of 128 (registers spill: 4.8 ms), two tiles of queries
 // a workgroup (dq 84 us instead of 52 in the first).
+#include "eager_launch.h"
 #include "eager_packed.h"
 
 namespace eager {
@@ -340,33 +341,31 @@ __global__ __launch_bounds__(256) void parts_kernel(const AttentionArgs a)
 }
 
 template <typename T, int DP>
-void enqueue(const AttentionArgs &a, hipStream_t stream)
+hipError_t enqueue(const AttentionArgs &a, hipStream_t stream)
 {
+    hipError_t e;
     const long long tiles = tile_numbers(a.tokens, a.sequences, kRows);
     const unsigned of_queries = static_cast<unsigned>(tiles * a.q_heads), of_keys = static_cast<unsigned>(tiles * a.kv_heads * a.parts);
     if (attention_together(tiles * a.q_heads, DP)) {
         const long long blocks = (a.tokens + kRows - 1) / kRows * a.q_heads;
-        hipLaunchKernelGGL((rows_kernel<T, DP>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
-        hipLaunchKernelGGL((gradients_kernel<T, DP>), dim3(of_keys + of_queries), dim3(256), 0, stream, a, static_cast<int>(of_keys));
+        e = launch(rows_kernel<T, DP>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
+        if (e == hipSuccess)
+            e = launch(gradients_kernel<T, DP>, dim3(of_keys + of_queries), dim3(256), 0, stream, a, static_cast<int>(of_keys));
     } else {
-        hipLaunchKernelGGL((queries_kernel<T, DP>), dim3(of_queries), dim3(256), 0, stream, a);
-        hipLaunchKernelGGL((keys_kernel<T, DP>), dim3(of_keys), dim3(256), 0, stream, a);
+        e = launch(queries_kernel<T, DP>, dim3(of_queries), dim3(256), 0, stream, a);
+        if (e == hipSuccess) e = launch(keys_kernel<T, DP>, dim3(of_keys), dim3(256), 0, stream, a);
     }
-    if (a.parts > 1) {
-        const long long quads = a.tokens * a.kv_heads * (a.dim / 4);
-        hipLaunchKernelGGL((parts_kernel<T>), dim3(static_cast<unsigned>((quads + 255) / 256), 2), dim3(256), 0, stream, a);
-    }
+    if (e != hipSuccess || a.parts == 1) return e;
+    const long long quads = a.tokens * a.kv_heads * (a.dim / 4);
+    return launch(parts_kernel<T>, dim3(static_cast<unsigned>((quads + 255) / 256), 2), dim3(256), 0, stream, a);
 }
 
 }  // namespace
 
 hipError_t launch_attention_backward(const AttentionArgs &a, bool bf16, hipStream_t stream)
 {
-    if (bf16 && a.dim <= 64) enqueue<__bf16, 64>(a, stream);
-    else if (bf16) enqueue<__bf16, 128>(a, stream);
-    else if (a.dim <= 64) enqueue<float, 64>(a, stream);
-    else enqueue<float, 128>(a, stream);
-    return hipGetLastError();
+    if (bf16) return a.dim <= 64 ? enqueue<__bf16, 64>(a, stream) : enqueue<__bf16, 128>(a, stream);
+    return a.dim <= 64 ? enqueue<float, 64>(a, stream) : enqueue<float, 128>(a, stream);
 }
 
 }  // namespace eager

@@ -25,6 +25,7 @@
 //
 // Slower: the compiler's own order of matrix instructions and reads (10 to 15 %, see spread()), 4 wavefronts of 256 x 256
 // (8 %), wavefronts of raised priority (no effect).
+#include "eager_launch.h"
 #include "eager_matrix.h"
 #include "eager_model.h"
 #include "eager_model_rules.h"
@@ -698,13 +699,13 @@ int lay_out(Product &p, int shape)
 }
 
 template <typename T, int Epi>
-void launch_logits(Product &p, int shape, hipStream_t stream)
+hipError_t launch_logits(Product &p, int shape, hipStream_t stream)
 {
     const int tiles = lay_out<T>(p, shape);
     const dim3 grid(shape == kLarge ? std::min(4 * tiles, tiles + 3 * (kUnits / 4)) : tiles);
-    if (shape == kLarge) hipLaunchKernelGGL((logits_kernel<T, Large, Epi>), grid, dim3(Large::Threads), 0, stream, p);
-    else if (shape == kMedium) hipLaunchKernelGGL((logits_kernel<T, Medium, Epi>), grid, dim3(Medium::Threads), 0, stream, p);
-    else hipLaunchKernelGGL((logits_kernel<T, Narrow, Epi>), grid, dim3(Narrow::Threads), 0, stream, p);
+    if (shape == kLarge) return launch(logits_kernel<T, Large, Epi>, grid, dim3(Large::Threads), 0, stream, p);
+    if (shape == kMedium) return launch(logits_kernel<T, Medium, Epi>, grid, dim3(Medium::Threads), 0, stream, p);
+    return launch(logits_kernel<T, Narrow, Epi>, grid, dim3(Narrow::Threads), 0, stream, p);
 }
 
 template <typename T>
@@ -720,15 +721,18 @@ hipError_t forward(const CrossEntropyArgs &a, hipStream_t stream)
     p.target = a.target;
     p.stats = reinterpret_cast<float2 *>(a.workspace);
     p.right = reinterpret_cast<float *>(p.stats + tiles * a.rows);
-    launch_logits<T, kStats>(p, shape, stream);
-    hipLaunchKernelGGL(rows_kernel, dim3(static_cast<unsigned>((a.rows + kJoined - 1) / kJoined)), dim3(1024), 0, stream, p.stats, p.right,
-                       a.target, a.loss, a.lse, a.rows, static_cast<int>(tiles), a.vocab);
-    return hipGetLastError();
+    const hipError_t e = launch_logits<T, kStats>(p, shape, stream);
+    if (e != hipSuccess) return e;
+    const float2 *stats = p.stats;
+    const float *right = p.right;
+    return launch(rows_kernel, dim3(static_cast<unsigned>((a.rows + kJoined - 1) / kJoined)), dim3(1024), 0, stream, stats, right,
+                  a.target, a.loss, a.lse, a.rows, static_cast<int>(tiles), a.vocab);
 }
 
 template <typename T>
 hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
 {
+    hipError_t e = hipSuccess;
     const Cut c = cut_of(a.rows, a.width, a.vocab, sizeof(T));
     const Layout l = layout_of(c, a.rows, a.width, sizeof(T));
     const T *w = static_cast<const T *>(a.w);
@@ -741,13 +745,14 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
                 reinterpret_cast<float *>(a.workspace + l.dloss), place, counted};
     if (a.rows > kCountedByEach) {
         int *before = reinterpret_cast<int *>(a.workspace + l.before);
-        hipLaunchKernelGGL(before_kernel, dim3(1), dim3(1024), 0, stream, g, before);
+        e = launch(before_kernel, dim3(1), dim3(1024), 0, stream, g, before);
         g.before = before;
     }
     // (without rows one workgroup says that none count)
-    hipLaunchKernelGGL((gather_kernel<T>), dim3(static_cast<unsigned>(std::max((a.rows + kGathered - 1) / kGathered, 1ll))),
-                       dim3(1024), 0, stream, g);
-    for (long long first = 0; first < a.vocab; first += c.piece) {
+    if (e == hipSuccess)
+        e = launch(gather_kernel<T>, dim3(static_cast<unsigned>(std::max((a.rows + kGathered - 1) / kGathered, 1ll))), dim3(1024), 0,
+                   stream, g);
+    for (long long first = 0; e == hipSuccess && first < a.vocab; first += c.piece) {
         const int live = static_cast<int>(std::min<long long>(a.vocab - first, c.piece));
         const long long padded = round_up(live, kSides[c.logits][0]);
         if (a.rows) {
@@ -766,10 +771,10 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
             p.out = dl;
             p.out_stride = padded;
             p.others = c.pieces == 1 && !p.whole ? reinterpret_cast<float *>(a.workspace + l.others) : nullptr;
-            launch_logits<T, kDlogits>(p, c.logits, stream);
-            if (p.others)
-                hipLaunchKernelGGL((targets_kernel<T>), dim3(static_cast<unsigned>((a.rows + kJoined - 1) / kJoined)), dim3(1024), 0,
-                                   stream, p, dl);
+            e = launch_logits<T, kDlogits>(p, c.logits, stream);
+            if (e == hipSuccess && p.others)
+                e = launch(targets_kernel<T>, dim3(static_cast<unsigned>((a.rows + kJoined - 1) / kJoined)), dim3(1024), 0, stream, p, dl);
+            if (e != hipSuccess) return e;
         }
         Product dx = {}, dw = {};
         int dx_tiles = 0, dw_tiles = 0;
@@ -799,19 +804,18 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
         const dim3 grid(dx_tiles + dw_tiles);
         if (!(dx_tiles + dw_tiles)) continue;
         if (c.gradients == kLarge)
-            hipLaunchKernelGGL((gradients_kernel<T, Large, false>), grid, dim3(Large::Threads), 0, stream, dw, dx, dw_tiles);
-        else if (c.dw_slices > 1)
-            hipLaunchKernelGGL((gradients_kernel<T, Medium, true>), grid, dim3(Medium::Threads), 0, stream, dw, dx, dw_tiles);
+            e = launch(gradients_kernel<T, Large, false>, grid, dim3(Large::Threads), 0, stream, dw, dx, dw_tiles);
         else
-            hipLaunchKernelGGL((gradients_kernel<T, Medium, false>), grid, dim3(Medium::Threads), 0, stream, dw, dx, dw_tiles);
+            e = launch(c.dw_slices > 1 ? gradients_kernel<T, Medium, true> : gradients_kernel<T, Medium, false>, grid,
+                       dim3(Medium::Threads), 0, stream, dw, dx, dw_tiles);
     }
+    if (e != hipSuccess) return e;
     if (a.dx && a.rows) of_dx = {sums, place, a.dx, a.x_stride, a.rows, a.rows, c.dx_slices};
     if (a.dw && c.dw_slices > 1) of_dw = {dw_sums, nullptr, a.dw, a.w_stride, a.vocab, of_dw.rows_padded, c.dw_slices};
     const long long quads = std::max(of_dx.rows, of_dw.rows) * (a.width / 4);
-    if (quads)
-        hipLaunchKernelGGL((sums_kernel<T>), dim3(static_cast<unsigned>((quads + 255) / 256), of_dw.rows ? 2 : 1), dim3(256), 0,
-                           stream, of_dx, of_dw, a.width);
-    return hipGetLastError();
+    if (!quads) return hipSuccess;
+    return launch(sums_kernel<T>, dim3(static_cast<unsigned>((quads + 255) / 256), of_dw.rows ? 2 : 1), dim3(256), 0, stream, of_dx,
+                  of_dw, a.width);
 }
 
 }  // namespace

@@ -12,6 +12,7 @@
 // x, which is read anyway.  Means, norms and gains' sums are fp32.  Measured: fp32, 20011 tokens of 50 heads of 64
 // (256 MB an array): forward 93 us (5.5 TB/s), backward 165 us (4.7 TB/s of three arrays) and 7 us for the gains' sums;
 // bf16, 8192 tokens of 20 heads of 64 (21 MB, which the last cache holds): 11.4, 16.5 and 4.1 us; 37 tokens: 4.8 us, a launch.
+#include "eager_launch.h"
 #include "eager_matrix.h"
 #include "eager_model.h"
 
@@ -212,15 +213,15 @@ __global__ __launch_bounds__(1024) void norm_rope_gains_kernel(const NormRopeArg
 }
 
 template <typename T, int V, int G>
-void enqueue(const NormRopeArgs &a, bool backward, hipStream_t stream)
+hipError_t enqueue(const NormRopeArgs &a, bool backward, hipStream_t stream)
 {
-    if (backward) {
-        if (a.blocks) hipLaunchKernelGGL((norm_rope_backward_kernel<T, V, G>), dim3(a.blocks), dim3(256), 0, stream, a);
-        hipLaunchKernelGGL((norm_rope_gains_kernel<T>), dim3((a.dim + 15) / 16, 2), dim3(1024), 0, stream, a);
-    } else {
+    if (!backward) {
         const long long blocks = (a.tokens + a.per_block - 1) / a.per_block;
-        hipLaunchKernelGGL((norm_rope_kernel<T, V, G>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
+        return launch(norm_rope_kernel<T, V, G>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
     }
+    hipError_t e = hipSuccess;
+    if (a.blocks) e = launch(norm_rope_backward_kernel<T, V, G>, dim3(a.blocks), dim3(256), 0, stream, a);
+    return e != hipSuccess ? e : launch(norm_rope_gains_kernel<T>, dim3((a.dim + 15) / 16, 2), dim3(1024), 0, stream, a);
 }
 
 // Lanes of 8 values need halves of a multiple of 8 (16-byte accesses in bf16); other head sizes take 4.
@@ -228,19 +229,18 @@ hipError_t dispatch(const NormRopeArgs &a, bool bf16, bool backward, hipStream_t
 {
     const int half = a.dim / 2;
     if (bf16 && half % 8 == 0) {
-        if (half <= 8) enqueue<__bf16, 8, 1>(a, backward, stream);
-        else if (half <= 16) enqueue<__bf16, 8, 2>(a, backward, stream);
-        else if (half <= 32) enqueue<__bf16, 8, 4>(a, backward, stream);
-        else enqueue<__bf16, 8, 8>(a, backward, stream);
-    } else if (bf16) {
-        if (half <= 16) enqueue<__bf16, 4, 4>(a, backward, stream);
-        else enqueue<__bf16, 4, 16>(a, backward, stream);
-    } else {
-        if (half <= 16) enqueue<float, 4, 4>(a, backward, stream);
-        else if (half <= 32) enqueue<float, 4, 8>(a, backward, stream);
-        else enqueue<float, 4, 16>(a, backward, stream);
+        if (half <= 8) return enqueue<__bf16, 8, 1>(a, backward, stream);
+        if (half <= 16) return enqueue<__bf16, 8, 2>(a, backward, stream);
+        if (half <= 32) return enqueue<__bf16, 8, 4>(a, backward, stream);
+        return enqueue<__bf16, 8, 8>(a, backward, stream);
     }
-    return hipGetLastError();
+    if (bf16) {
+        if (half <= 16) return enqueue<__bf16, 4, 4>(a, backward, stream);
+        return enqueue<__bf16, 4, 16>(a, backward, stream);
+    }
+    if (half <= 16) return enqueue<float, 4, 4>(a, backward, stream);
+    if (half <= 32) return enqueue<float, 4, 8>(a, backward, stream);
+    return enqueue<float, 4, 16>(a, backward, stream);
 }
 
 }  // namespace

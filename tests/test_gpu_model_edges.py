@@ -107,3 +107,45 @@ def test_cross_entropy_gradients_of_confident_rows_any_vocabulary(ops, dtype, ro
     for name, t in (("dx", dx), ("dw", dw)):
         off = float((t.double() - want[name][0]).norm() / want[name][0].norm())
         assert off < (1e-4 if dtype == torch.float32 else 2.0 ** -8 + 1e-4), (name, off)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_an_error_of_another_call_is_not_an_operator_s(ops, dtype):
+    """The runtime keeps the last error of a thread until somebody asks.  One that an unrelated call has left there
+    (a device that does not exist) is not reported by any operator as its own, nor taken away."""
+    import ctypes
+    from paper_1908_04207_amd import binding as eb
+    gen = torch.Generator().manual_seed(1)
+    T, D = 40, 64
+    q, k, v = (_normal(gen, T, h, D, dtype=dtype).cuda() for h in (4, 2, 2))
+    w, table, pos = torch.ones(D, dtype=dtype, device="cuda"), torch.ones(T, D // 2, device="cuda"), torch.arange(T, device="cuda").int()
+    cu = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    out, lse = ops.attention(q, k, v, cu)
+    x, target, g = q.flatten(1), torch.arange(T, device="cuda"), torch.ones(T, device="cuda")
+    of_loss = {n: ops.cross_entropy(x[:, :64], head, target)[1] for n, head in (("one", k[:, 0]), ("many", torch.cat([x[:, :64]] * 10)))}
+    heads = {"one": k[:, 0], "many": torch.cat([x[:, :64]] * 10)}
+    many_q, many_k = q.repeat(200, 1, 1), k.repeat(200, 1, 1)
+    many_cu = torch.arange(0, 200 * T + 1, T, device="cuda").int()
+    many_out, many_lse = ops.attention(many_q, many_k, many_k, many_cu)
+    torch.cuda.synchronize()
+    hip = ctypes.CDLL(eb.LIB_PATH)                  # the runtime that the library is linked with
+    calls = {
+        "norm": lambda: ops.qk_norm_rope(q, k, w, w, table, table, pos),
+        "norm, gradients": lambda: ops.qk_norm_rope_backward(q, k, q, k, w, w, table, table, pos),
+        "attention": lambda: ops.attention(q, k, v, cu),
+        "attention, gradients": lambda: ops.attention_backward(q, q, k, v, out, lse, cu),
+        "attention, gradients of many": lambda: ops.attention_backward(many_q, many_q, many_k, many_k, many_out, many_lse, many_cu),
+        "loss": lambda: ops.cross_entropy(x[:, :64], heads["one"], target)}
+    for n, head in heads.items():
+        calls["loss, gradients, " + n] = lambda n=n, head=head: ops.cross_entropy_backward(g, x[:, :64], head, target, of_loss[n])
+    for call in calls.values():
+        call()                                      # what torch allocates is there from here on
+    for name, call in calls.items():
+        left = hip.hipSetDevice(1 << 20)
+        assert left != 0
+        try:
+            call()
+        finally:
+            assert hip.hipGetLastError() == left, name
+            assert hip.hipGetLastError() == 0
+    torch.cuda.synchronize()
