@@ -28,6 +28,7 @@ import torch
 from . import binding as eb
 
 _DTYPES = {torch.float32: eb.F32, torch.bfloat16: eb.BF16}
+_MAX_STRIDE = 1 << 21            # elements from row to row
 
 
 def _refuse(text: str):
@@ -98,6 +99,16 @@ class _Once(torch.autograd.Function):
     @staticmethod
     def backward(ctx, *_):
         _refuse(f"{ctx.what}: second derivatives are not formed")
+
+
+def _upstream(t):
+    """A gradient [tokens, heads, head_dim] that autograd hands over, copied only if the kernels do not take its
+    strides (a broadcast or transposed one) or its place in memory."""
+    each = 16 // t.element_size()
+    row, head, one = t.stride()
+    taken = (one == 1 and row >= t.shape[2] and head >= t.shape[2] and row % each == 0 and head % each == 0 and
+             row <= _MAX_STRIDE and t.data_ptr() % 16 == 0)
+    return t if taken else t.clone(memory_format=torch.contiguous_format)
 
 
 def _once(what: str, grads, *depends):
@@ -186,8 +197,7 @@ class QKNormRope(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dq_out, dk_out):
         q, k, wq, wk, cos, sin, positions = ctx.saved_tensors
-        grads = qk_norm_rope_backward(dq_out.contiguous(), dk_out.contiguous(), q, k, wq, wk, cos, sin, positions,
-                                      ctx.eps)
+        grads = qk_norm_rope_backward(_upstream(dq_out), _upstream(dk_out), q, k, wq, wk, cos, sin, positions, ctx.eps)
         return (*_once("QKNormRope", grads, dq_out, dk_out, q, k, wq, wk), None, None, None, None)
 
 
@@ -256,7 +266,7 @@ class Attention(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dout):
         q, k, v, out, lse, cu_seqlens = ctx.saved_tensors
-        grads = attention_backward(dout.contiguous(), q, k, v, out, lse, cu_seqlens, ctx.scale)
+        grads = attention_backward(_upstream(dout), q, k, v, out, lse, cu_seqlens, ctx.scale)
         return (*_once("Attention", grads, dout, q, k, v), None, None)
 
 

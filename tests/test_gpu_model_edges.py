@@ -149,3 +149,21 @@ def test_an_error_of_another_call_is_not_an_operator_s(ops, dtype):
             assert hip.hipGetLastError() == left, name
             assert hip.hipGetLastError() == 0
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_upstream_gradients_off_a_boundary(ops, dtype):
+    """Contiguous, but not on 16 bytes: as a part of a flat buffer that other gradients share may be."""
+    gen = torch.Generator().manual_seed(5)
+    T, D = 50, 64
+    q, k, v = (_normal(gen, T, h, D, dtype=dtype).cuda().requires_grad_() for h in (4, 2, 2))
+    w, table, pos = torch.ones(D, dtype=dtype, device="cuda"), torch.ones(T, D // 2, device="cuda"), torch.arange(T, device="cuda").int()
+    flat = _normal(gen, T * 4 * D + 1, dtype=dtype).cuda()
+    up = flat[1:].view(T, 4, D)
+    out = ops.Attention.apply(q, k, v, torch.tensor([0, T], dtype=torch.int32, device="cuda"), None)
+    for a, b in zip(torch.autograd.grad(out, (q, k, v), up, retain_graph=True), torch.autograd.grad(out, (q, k, v), up.clone())):
+        assert torch.equal(a, b)
+    out = ops.QKNormRope.apply(q, k, w, w, table, table, pos, 1e-6)
+    for a, b in zip(torch.autograd.grad(out, (q, k), (up, up[:, :2]), retain_graph=True),
+                    torch.autograd.grad(out, (q, k), (up.clone(), up[:, :2].clone()))):
+        assert torch.equal(a, b)

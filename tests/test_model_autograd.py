@@ -92,3 +92,61 @@ def test_second_derivatives_are_refused(plain, name, linear):
     penalty = sum(g.square().sum() for g in grads if g is not None)
     with pytest.raises(eb.EagerError, match="second derivatives"):
         (value + penalty).backward()
+
+
+def _views():
+    """Upstream gradients [T, heads, D] as torch may hand them over, and whether the kernels take them as they are."""
+    def contiguous(h):
+        return torch.randn(T, h, D)
+
+    def part_of_a_row(h):
+        return torch.randn(T, h * D + 24)[:, 8:8 + h * D].view(T, h, D)
+
+    def heads_first(h):
+        return torch.randn(h, T, D).transpose(0, 1)
+
+    def off_a_boundary(h):
+        return torch.randn(T * h * D + 1)[1:].view(T, h, D)
+
+    def odd_rows(h):
+        return torch.randn(T, h * D + 1)[:, :h * D].view(T, h, D)
+
+    def broadcast(h):
+        return torch.randn(1, 1, D).expand(T, h, D)
+
+    def one_number(h):
+        return torch.ones(()).expand(T, h, D)
+
+    def dims_first(h):
+        return torch.randn(T, D, h).transpose(1, 2)
+
+    return [(contiguous, True), (part_of_a_row, True), (heads_first, True), (off_a_boundary, False), (odd_rows, False),
+            (broadcast, False), (one_number, False), (dims_first, False)]
+
+
+@pytest.mark.parametrize("view,taken", _views(), ids=lambda x: getattr(x, "__name__", None))
+@pytest.mark.parametrize("name", ["attention", "norm"])
+def test_upstream_gradients_reach_the_kernels_in_a_form_they_take(plain, monkeypatch, name, view, taken):
+    handed = []
+    for fn in ("attention_backward", "qk_norm_rope_backward"):
+        call = getattr(ops, fn)
+
+        def spy(*a, call=call, n=1 if fn[0] == "a" else 2, **kw):
+            handed.extend(a[:n])
+            return call(*a, **kw)
+        monkeypatch.setattr(ops, fn, spy)
+    if name == "norm":
+        q, k, w = (torch.randn(*s).requires_grad_() for s in ((T, Hq, D), (T, Hk, D), (D,)))
+        table, pos = torch.ones(T, D // 2), torch.arange(T, dtype=torch.int32)
+        outs, leaves = ops.QKNormRope.apply(q, k, w, w, table, table, pos, 1e-6), (q, k)
+        ups = [view(Hq), view(Hk)]
+    else:
+        q, k, v = (torch.randn(T, h, D).requires_grad_() for h in (Hq, Hk, Hk))
+        outs, leaves = (ops.Attention.apply(q, k, v, torch.tensor([0, T], dtype=torch.int32), None),), (q, k, v)
+        ups = [view(Hq)]
+    torch.autograd.grad(outs, leaves, ups)
+    assert len(handed) == len(ups)
+    for up, got in zip(ups, handed):
+        assert torch.equal(up, got)
+        assert got.data_ptr() % 16 == 0 and got.stride(2) == 1 and all(s % 4 == 0 and s >= D for s in got.stride()[:2])
+        assert (got.data_ptr() == up.data_ptr()) == taken
