@@ -557,7 +557,8 @@ def heads(x) -> Heads:
     if x.dim() != 3 or (x.shape[2] > 1 and x.stride(2) != 1):
         raise EagerError(EINVAL, f"expected [tokens, heads, head_dim] with contiguous heads, got {tuple(x.shape)} "
                                  f"with strides {x.stride()}")
-    return Heads(x.data_ptr(), x.stride(0), x.stride(1))
+    # a lone token or head may have any stride
+    return Heads(x.data_ptr(), x.stride(0) if x.shape[0] > 1 else x.shape[2], x.stride(1) if x.shape[1] > 1 else x.shape[2])
 
 
 def packed(tokens: int, q_heads: int, kv_heads: int, head_dim: int, cu_seqlens=None) -> Packed:

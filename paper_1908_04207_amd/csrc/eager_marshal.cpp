@@ -407,7 +407,8 @@ bool heads_like(const Tensor &t, const Tensor &like, int64_t heads, eager_heads 
     if (t.dims != 3 || t.type != like.type || t.device != like.device || t.size[0] != like.size[0] ||
         t.size[1] != heads || t.size[2] != like.size[2] || (t.size[2] > 1 && t.stride[2] != 1))
         return false;
-    *h = {t.data, t.stride[0], t.stride[1]};
+    // a lone token or head may have any stride
+    *h = {t.data, t.size[0] > 1 ? t.stride[0] : t.size[2], t.size[1] > 1 ? t.stride[1] : t.size[2]};
     return true;
 }
 

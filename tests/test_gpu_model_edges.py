@@ -167,3 +167,32 @@ def test_upstream_gradients_off_a_boundary(ops, dtype):
     for a, b in zip(torch.autograd.grad(out, (q, k), (up, up[:, :2]), retain_graph=True),
                     torch.autograd.grad(out, (q, k), (up.clone(), up[:, :2].clone()))):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("through", ["module", "ctypes"])
+def test_a_lone_token_or_head_of_any_stride(ops, dtype, through, monkeypatch):
+    from paper_1908_04207_amd import binding as eb
+    gen = torch.Generator().manual_seed(7)
+    D = 64
+    w, table, pos = torch.ones(D, dtype=dtype, device="cuda"), torch.ones(9, D // 2, device="cuda"), torch.arange(9, device="cuda").int()
+    base = _normal(gen, 9, 2, D, dtype=dtype).cuda()
+    odd = _normal(gen, 3, 2 * D + 3, dtype=dtype).cuda()
+    views = [base[0].expand(1, 2, D),                              # a token out of a row: stride 0
+             odd[:1, :2 * D].view(1, 2, D),                        # the first of rows of an odd length
+             base[:, 0].as_strided((9, 1, D), (2 * D, 1, 1))]      # a head whose stride is a leftover
+    if through == "ctypes":
+        monkeypatch.setattr(eb, "_marshal", eb._CtypesOnly)
+    for q in views:
+        T, H, near = q.shape[0], q.shape[1], q.contiguous().clone()
+        cu = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+        out, lse = ops.attention(q, q, q, cu)
+        want, lse_n = ops.attention(near, near, near, cu)
+        assert torch.equal(out, want) and torch.equal(lse, lse_n)
+        for a, b in zip(ops.attention_backward(q, q, q, q, out, lse, cu), ops.attention_backward(near, near, near, near, out, lse, cu)):
+            assert torch.equal(a, b)
+        rest = w, w, table, table, pos[:T]
+        for a, b in zip(ops.qk_norm_rope_backward(q, q, q, q, *rest), ops.qk_norm_rope_backward(near, near, near, near, *rest)):
+            assert torch.equal(a, b)
+        for a, b in zip(ops.qk_norm_rope(q, q, *rest), ops.qk_norm_rope(near, near, *rest)):
+            assert torch.equal(a, b)

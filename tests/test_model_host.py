@@ -169,3 +169,15 @@ def test_tensors_off_the_gpu_are_refused():
     _refused(lambda: ops.qk_norm_rope(q, k, w, w, table, table, pos))
     _refused(lambda: ops.cross_entropy(torch.zeros(3, 64), torch.zeros(5, 64), torch.zeros(3, dtype=torch.int64)))
     _refused(lambda: ops.attention(q.double(), k.double(), k.double(), cu))
+
+
+def test_the_stride_of_a_lone_token_or_head_counts_nothing():
+    """Nothing is stepped over there, and torch may give it any stride."""
+    import torch
+    for t in (torch.zeros(2, 64).expand(1, 2, 64), torch.zeros(5, 64)[:, None], torch.zeros(64).expand(1, 1, 64),
+              torch.zeros(1, 2, 3 << 21)[:, :, :64], torch.zeros(3, 1, 64).as_strided((3, 1, 64), (64, 1, 1))):
+        h = eb.heads(t)
+        assert h.data == t.data_ptr()
+        assert h.row_stride == (t.stride(0) if t.shape[0] > 1 else 64)
+        assert h.head_stride == (t.stride(1) if t.shape[1] > 1 else 64)
+    assert eb.heads(torch.zeros(3, 64)[:, None].expand(3, 2, 64)).head_stride == 0       # a broadcast view: refused later
