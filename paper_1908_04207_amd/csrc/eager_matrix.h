@@ -12,6 +12,8 @@
 // keeps reads free of bank conflicts is applied to the global address.
 #pragma once
 
+#include "eager_tiles.h"
+
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -127,14 +129,6 @@ __device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t r, char *lds, 
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
 
 // ---- tiles whose rows are operand rows and hold consecutive k: `Chunks` 16-byte chunks a row.
-// Reads take the same chunk of 32 rows; the exchange spreads 16 consecutive rows over the 256 bytes
-// of banks, and the four rows of a transposing read over different pairs of chunks.
-template <int Chunks>
-__device__ __forceinline__ int exchange(int row)
-{
-    if (Chunks >= 16) return ((row & 3) << 2) | ((row >> 2) & 3);
-    return ((row & 2) << 1) | ((row >> 1) & 2) | ((row >> 3) & 1);
-}
 
 // Rows of a matrix from `base` on into a tile; rows from rows_left on and chunks from chunks_left on
 // are zeros (rows_left may be negative).  stride: bytes.
@@ -175,10 +169,7 @@ __device__ __forceinline__ f32x8 read_rows(const char *tile, int row0, int step,
 // The transposed operand from such a tile: rows are columns col0 .. col0 + 31 of the tile, k runs
 // over tile rows: j = 0..3 of the lane's half from k0 + k_half * (lane / 32) on, j = 4..7 from
 // k_quad later.  bf16 has a read for it: 16 lanes get 16 columns of 4 rows.
-template <int Chunks, int Shift>
-__device__ __forceinline__ int exchange_of(int row) { return Shift < 0 ? exchange<Chunks>(row) : (row & 3) << Shift; }
-
-template <int Chunks, int Shift = -1>
+template <int Chunks, int Shift = kOfRows>
 __device__ __forceinline__ bf16x8 read_columns(const char *tile, int col0, int k0, int k_half, int k_quad, int lane,
                                                __bf16 *)
 {
@@ -193,7 +184,7 @@ __device__ __forceinline__ bf16x8 read_columns(const char *tile, int col0, int k
     const i16x8 z = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
     return __builtin_bit_cast(bf16x8, z);
 }
-template <int Chunks, int Shift = -1>
+template <int Chunks, int Shift = kOfRows>
 __device__ __forceinline__ f32x8 read_columns(const char *tile, int col0, int k0, int k_half, int k_quad, int lane,
                                               float *)
 {

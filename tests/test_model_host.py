@@ -181,3 +181,14 @@ def test_the_stride_of_a_lone_token_or_head_counts_nothing():
         assert h.row_stride == (t.stride(0) if t.shape[0] > 1 else 64)
         assert h.head_stride == (t.stride(1) if t.shape[1] > 1 else 64)
     assert eb.heads(torch.zeros(3, 64)[:, None].expand(3, 2, 64)).head_stride == 0       # a broadcast view: refused later
+
+
+def test_places_in_tiles_on_the_cpu(tmp_path):
+    """The chunks of a tile's rows have places of their own, by arithmetic that stays in its types (under
+    UndefinedBehaviorSanitizer)."""
+    exe = tmp_path / "model_tiles"
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+                           "-static-libasan", "-Wall", "-Wextra", "-Werror",
+                           os.path.join(ROOT, "tests", "c", "model_tiles_host.cpp"), "-o", str(exe)])
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", (r.stdout[-500:], r.stderr[-2000:])
