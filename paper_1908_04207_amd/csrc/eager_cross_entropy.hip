@@ -121,8 +121,8 @@ struct Source {
 template <typename T, int Rows, bool Columns>
 __device__ __forceinline__ typename Operand<T>::frag read_side(const char *tile, int row0, int step, int lane)
 {
-    if (!Columns) return read_rows<8>(tile, row0, step, lane, static_cast<T *>(nullptr));
-    return read_columns<Rows * sizeof(T) / 16, sizeof(T) == 2 ? 2 : kNoExchange>(tile, row0, 16 * step, 8, 4, lane, static_cast<T *>(nullptr));
+    if constexpr (!Columns) return read_rows<8>(tile, row0, step, lane, static_cast<T *>(nullptr));
+    else return read_columns<Rows * sizeof(T) / 16, sizeof(T) == 2 ? 2 : kNoExchange>(tile, row0, 16 * step, 8, 4, lane, static_cast<T *>(nullptr));
 }
 
 // Workgroups id, id + 8, ... run on the same chiplet (one second-level cache): which of `all` pieces of work
