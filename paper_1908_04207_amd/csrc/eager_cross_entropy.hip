@@ -107,8 +107,7 @@ struct Source {
     // the next tile; zeros instead where !live
     __device__ __forceinline__ void load(char *tile, bool live)
     {
-        const long long n = min(max(live ? bytes : 0ll, 0ll), 0x7fffffffll);
-        const __amdgpu_buffer_rsrc_t r = buffer(base, static_cast<unsigned>(n));
+        const __amdgpu_buffer_rsrc_t r = buffer(base, covered(live ? bytes : 0));
         const unsigned at = Columns || chunk < chunks_left ? offset : kOutside;
 #pragma unroll
         for (int i = 0; i < Loads; ++i) load_lds16(r, tile + (i * Waves + wave) * 1024, at + i * row_step);

@@ -112,8 +112,6 @@ __device__ __forceinline__ typename Operand<T>::frag as_operand(const f32x16 &c,
     return f;
 }
 
-constexpr unsigned kOutside = 0x80000000u;     // an offset no descriptor covers
-
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *base, unsigned bytes)
 {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, bytes, 0x00020000);

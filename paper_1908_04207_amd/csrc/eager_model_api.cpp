@@ -15,7 +15,7 @@ int64_t chunk(int dtype) { return dtype == EAGER_BF16 ? 8 : 4; }     // elements
 
 // Tokens stay this far from 2^31, so that no tile's end passes it.
 constexpr int64_t kMaxTokens = (1ll << 31) - (1ll << 16);
-// Tiles are at most 128 rows, addressed within 2^31 bytes.
+// Tiles are at most 256 rows, so the last byte of one lies within 2^31 bytes of its first (fp32: exactly).
 constexpr int64_t kMaxStride = 1ll << 21;
 constexpr int64_t kMaxGrid = (1ll << 31) - 1;
 

@@ -23,4 +23,10 @@ constexpr int exchange_of(int row)
     return Shift == kOfRows ? exchange<Chunks>(row) : Shift == kNoExchange ? 0 : (row & 3) << (Shift < 0 ? 0 : Shift);
 }
 
+constexpr unsigned kOutside = 0x80000000u;     // an offset no descriptor covers
+
+// The length of a descriptor that covers `bytes` from a tile's first row on; a tile's own are at most kOutside: 256 rows, 2^23
+// bytes apart.
+constexpr unsigned covered(long long bytes) { return bytes <= 0 ? 0 : bytes < kOutside ? static_cast<unsigned>(bytes) : kOutside; }
+
 }  // namespace eager

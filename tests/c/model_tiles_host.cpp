@@ -33,6 +33,13 @@ int main()
     places<16, 2>(64);
     places<64, kNoExchange>(32);         // fp32 columns
     places<32, kNoExchange>(32);
+    // a tile of 256 rows at the largest stride, as wide as the stride, fp32: its last bytes are covered, and the
+    // offset that stands for none is not
+    const long long stride = (1ll << 21) * 4, bytes = 255 * stride + stride;
+    CHECK(covered(bytes) == static_cast<unsigned long long>(bytes));
+    CHECK(covered(2 * bytes) <= kOutside && covered(1ll << 40) <= kOutside);
+    CHECK(kOutside + 255ull * stride < (1ull << 32));                      // nor after the steps between its rows
+    CHECK(covered(0) == 0 && covered(-1) == 0 && covered(-(1ll << 40)) == 0 && covered(16) == 16);
     for (int row = 0; row < 256; ++row) CHECK((exchange_of<32, kNoExchange>(row)) == 0);
     std::puts("ok");
     return 0;
