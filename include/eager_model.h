@@ -98,7 +98,7 @@ int eager_qk_norm_rope_backward(int dtype, const eager_packed *shape, const eage
  * reach every row of it.
  * fp32 products are formed from three bf16 pieces of every operand, whose sum is the operand: within two
  * roundings of an fp32 product; an infinite operand gives NaN.
- * Errors: EINVAL (NULL, alignment, strides, sizes, scale not positive and finite), EDEVICE.
+ * Errors: EINVAL (NULL, alignment, strides, sizes, scale not in 2^-120 .. 2^120), EDEVICE.
  *
  * Backward: dq, dk, dv from the forward pass's inputs and results and dout.  Gradients of a key
  * and value head are summed over the query heads that share it.  Rows that belong to no sequence

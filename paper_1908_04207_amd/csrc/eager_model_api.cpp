@@ -18,6 +18,8 @@ constexpr int64_t kMaxTokens = (1ll << 31) - (1ll << 16);
 // Tiles are at most 256 rows, so the last byte of one lies within 2^31 bytes of its first (fp32: exactly).
 constexpr int64_t kMaxStride = 1ll << 21;
 constexpr int64_t kMaxGrid = (1ll << 31) - 1;
+// With scales from here to its inverse lse / scale and scale * log2(e) are numbers in fp32.
+constexpr float kLeastScale = 0x1p-120f;
 
 bool valid_shape(const eager_packed *s)
 {
@@ -77,7 +79,7 @@ bool fill(eager::NormRopeArgs &a, int dtype, const eager_packed *s, const eager_
 bool fill(eager::AttentionArgs &a, int dtype, const eager_packed *s, const eager_heads *q, const eager_heads *k,
           const eager_heads *v, const eager_heads *out, const float *lse, float scale)
 {
-    if (!valid_dtype(dtype) || !valid_sequences(s) || !(scale > 0.0f) || !std::isfinite(scale) ||
+    if (!valid_dtype(dtype) || !valid_sequences(s) || !(scale >= kLeastScale && scale <= 1.0f / kLeastScale) ||
         !(aligned(lse, 4) || s->tokens == 0))
         return false;
     for (const eager_heads *h : {q, k, v, out})

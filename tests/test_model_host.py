@@ -192,3 +192,22 @@ def test_places_in_tiles_on_the_cpu(tmp_path):
                            os.path.join(ROOT, "tests", "c", "model_tiles_host.cpp"), "-o", str(exe)])
     r = subprocess.run([str(exe)], capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout.strip() == "ok", (r.stdout[-500:], r.stderr[-2000:])
+
+
+@pytest.mark.parametrize("dtype", [eb.F32, eb.BF16])
+def test_scales_that_leave_the_range_of_fp32_are_refused(dtype):
+    """lse / scale and scale * log2(e) have to be numbers: log-sum-exps of 2^31 equal scores reach 21.5, and 21.5 / 6e-38 is
+    none (keys' gradients would be zeros)."""
+    none = _heads(data=None)
+
+    def forward(scale):
+        eb.eager_attention(dtype, _shape(tokens=0), none, none, none, scale, none, None, stream=0)
+
+    def backward(scale):
+        eb.eager_attention_backward(dtype, _shape(tokens=0), none, none, none, none, None, none, scale, none, none, none, A, 1 << 30, stream=0)
+
+    for call in (forward, backward):
+        for scale in (1e-38, 1e-45, 2.0 ** -121, 2.0 ** 121, 3e38):
+            _refused(lambda: call(scale))
+        for scale in (2.0 ** -120, 1e-6, 1.0, 2.0 ** 120):
+            call(scale)
