@@ -212,20 +212,6 @@ __device__ __forceinline__ void spread()
     }
 }
 
-// The same for Products matrix instructions with, between each two of them, Reads reads of shared
-// memory, Vector vector instructions and Exponentials of them.
-template <int Products, int Reads, int Vector, int Exponentials, int I = 0>
-__device__ __forceinline__ void overlap()
-{
-    if constexpr (I < Products) {
-        if constexpr (Reads > 0) __builtin_amdgcn_sched_group_barrier(0x100, Reads, 0);
-        if constexpr (Vector > 0) __builtin_amdgcn_sched_group_barrier(0x2, Vector, 0);
-        if constexpr (Exponentials > 0) __builtin_amdgcn_sched_group_barrier(0x400, Exponentials, 0);
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        overlap<Products, Reads, Vector, Exponentials, I + 1>();
-    }
-}
-
 // base-2 exponential and logarithm of the hardware: one unit in the last place for normal results
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
