@@ -1,5 +1,7 @@
-// Where things lie in the tiles of the model operators' products (eager_tiles.h), on the CPU with sanitizers.
+// Where things lie in the tiles of the model operators' products (eager_tiles.h) and in a backward pass's workspace, and
+// what the rules say of sizes that tests stand on (eager_model_rules.h), on the CPU with sanitizers.
 // Run by tests/test_model_host.py.
+#include "../../paper_1908_04207_amd/csrc/eager_model_rules.h"
 #include "../../paper_1908_04207_amd/csrc/eager_tiles.h"
 
 #include <cstdio>
@@ -41,6 +43,23 @@ int main()
     CHECK(kOutside + 255ull * stride < (1ull << 32));                      // nor after the steps between its rows
     CHECK(covered(0) == 0 && covered(-1) == 0 && covered(-(1ll << 40)) == 0 && covered(16) == 16);
     for (int row = 0; row < 256; ++row) CHECK((exchange_of<32, kNoExchange>(row)) == 0);
+    // heads that share keys: in parts, or summed by one workgroup (tests/test_gpu_model_edges.py)
+    CHECK(attention_parts(70000, 8, 2, 700) == 1 && attention_parts(66000, 6, 2, 660) == 1);
+    CHECK(attention_parts(70000, 4, 1, 700) == 2 && attention_parts(300, 4, 1, 3) == 4);
+    // sums of p without the target's: a number a row and tile, while one piece holds the vocabulary
+    const long long rows[] = {0, 1, 61, 300, 4096, 8191, 70000};
+    const int vocabs[] = {1, 64, 128, 129, 300, 5003, 50257, 250000};
+    for (long long n : rows)
+        for (int v : vocabs)
+            for (int width = 8; width <= 1600; width += 199 * 8)
+                for (int size = 2; size <= 4; size += 2) {
+                    const Cut c = cut_of(n, width, v, size);
+                    const Layout l = layout_of(c, n, width, size);
+                    CHECK(c.pieces == (v + c.piece - 1) / c.piece);
+                    const long long tiles = (v + kSides[c.logits][0] - 1) / kSides[c.logits][0];
+                    CHECK(l.dl + c.rows_padded * c.piece * size <= l.others && l.others <= l.dx_sums);
+                    CHECK(c.pieces > 1 || l.others + tiles * n * 4 <= l.dx_sums);
+                }
     std::puts("ok");
     return 0;
 }

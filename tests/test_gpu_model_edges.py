@@ -196,3 +196,26 @@ def test_a_lone_token_or_head_of_any_stride(ops, dtype, through, monkeypatch):
             assert torch.equal(a, b)
         for a, b in zip(ops.qk_norm_rope(q, q, *rest), ops.qk_norm_rope(near, near, *rest)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,group", [(70000, 4), (66000, 3)])
+def test_attention_shared_keys_summed_by_one_workgroup(ops, dtype, T, group):
+    """Enough tiles that the heads that share keys are not split into parts (checked with the launch rules on the
+    CPU): as with the keys repeated for every head and the gradients added up."""
+    gen = torch.Generator().manual_seed(3)
+    kv, D = 2, 16
+    cu = torch.tensor([0] + [100] * (T // 100), dtype=torch.int32).cumsum(0, dtype=torch.int32).cuda()
+    q, dout = (_normal(gen, T, kv * group, D, dtype=dtype).cuda() for _ in range(2))
+    k, v = (_normal(gen, T, kv, D, dtype=dtype).cuda() for _ in range(2))
+    out, lse = ops.attention(q, k, v, cu)
+    dq, dk, dv = ops.attention_backward(dout, q, k, v, out, lse, cu)
+    kr, vr = (t.repeat_interleave(group, 1) for t in (k, v))
+    out_r, lse_r = ops.attention(q, kr, vr, cu)
+    dq_r, dk_r, dv_r = ops.attention_backward(dout, q, kr, vr, out_r, lse_r, cu)
+    assert torch.equal(out, out_r) and torch.equal(lse, lse_r) and torch.equal(dq, dq_r)
+    for got, each in ((dk, dk_r), (dv, dv_r)):
+        each = each.double().view(T, kv, group, D)
+        # one rounding of the result and one of each of those that are added here
+        bound = mo.U[dtype] * (each.abs().sum(2) * 2.01) + 64 * mo.E * each.abs().sum(2) + 1e-6 * each.abs().amax()
+        assert ((got.double() - each.sum(2)).abs() <= bound).all()
