@@ -7,18 +7,20 @@
 // and sum are taken in registers (one exchange between the halves of a wavefront), the rescaling
 // of O is one factor a lane, and P^T is the second product's operand as it stands.  P is rounded to
 // bf16 for that product where the inputs are (a matrix instruction takes both sides in one type); its sum l is taken
-// in fp32 before the rounding.
+// in fp32 before the rounding, so that lse is that of the scores, and the weights that are applied add up to one
+// within P's roundings.
 //
 // Tiles of keys come by loads that write shared memory directly, one tile ahead, and tiles of queries
 // with the most keys first: a workgroup's time is its number of key tiles.
 //
 // Bound, heads of 64: the vector instructions of the softmax (an exponential of 16 clocks per 64 scores and about 4 more
-// instructions each, ~1000 clocks a tile of 64 x 32 beside 512 of matrix instructions on the same SIMD), and with short
-// sequences the longest row's chain: 0.87 us a tile of keys and 3.2 us of start and end.  Heads of 128: matrix
-// instructions busy 56 % of the time.
+// instructions each), 75 % of a unit's clocks with 25 heads beside 32 % of matrix instructions, and what is open between a tile's
+// steps, which wait for each other (barrier, scores, maximum, exponentials, second product); with short
+// sequences the longest row's chain of them: 0.87 us a tile of keys and 3.2 us of start and end (16 sequences: 68 and
+// 26 %).  Heads of 128: matrix instructions 56 %, vector instructions 56 %.
 // Measured: bf16, 16 heads (4 of keys) of 64: 113 tokens 6.2 us, 16 sequences of 8192 tokens 31 us; 25 heads of 64, 8
-// sequences of 1024: 50 us (532 TFLOP/s, masked pairs not counted); 8 heads (2) of 128, one sequence of 16384: 587 us
-// (937 TFLOP/s); fp32, 16 heads (8) of 64, 9 sequences, 4099 tokens: 77 us.
+// sequences of 1024: 50 us (532 TFLOP/s, masked pairs not counted); 8 heads (2) of 128, one sequence of 16384: 588 us
+// (935 TFLOP/s); fp32, 16 heads (8) of 64, 9 sequences, 4099 tokens: 78 us.
 //
 // Slower, 16 sequences and 8 x 1024 of the above: two groups of wavefronts that share a row's keys and join their
 // statistics (39 and 62 us against 31 and 52), two tiles of queries a workgroup (43 and 61).

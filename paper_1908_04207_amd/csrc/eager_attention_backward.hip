@@ -14,11 +14,12 @@
 // With bf16 inputs P and dS are rounded to bf16 for the second products, whose other sides are bf16:
 // the error is that of the formula's own operands.  Sums are fp32, and so are P and dS with fp32 inputs.
 //
-// Bound, heads of 64: the vector instructions beside the matrix ones (an exponential, two products
-// and two conversions an element, on the same SIMD; about 1000 clocks beside 512 in a tile of 64 x 32)
-// and, in short sequences, the last key tile's chain of all its queries.  Heads of 128: one
-// wavefront a SIMD in the keys' kernel (316 registers: two accumulators of 128 x 32), so waits of a
-// tile's loads and of the chain S -> P -> dP -> dS are not covered by another wavefront.
+// Bound, heads of 64: what is open in the chain S -> P -> dP -> dS of a tile, with three wavefronts a SIMD in the queries' kernel and
+// two in the keys' (vector instructions take 53 and 37 % of a unit's clocks, matrix instructions 35 and 33 %, 25 heads of
+// 64) and, in short sequences, the last key tile's chain of all its queries.  Heads of 128 and fp32: one
+// wavefront a SIMD in the keys' kernel (bf16 316 registers: two accumulators of 128 x 32), so waits of a
+// tile's loads and of that chain are not covered by another wavefront; in fp32 with heads of 128 it keeps 132 bytes a
+// lane in scratch memory.
 // Measured: bf16, 16 heads (4 of keys) of 64, 16 sequences, 8192 tokens: 43 us dq, 49 us dk and dv, 12 us
 // parts; 25 heads of 64, 8 sequences of 1024: 68 and 90 us (589 and 597 TFLOP/s, masked pairs not counted); 8
 // heads (2) of 128, one of 16384: 833 and 1364 us (990 and 806 TFLOP/s); fp32, 16 heads (8) of 64, 9 sequences,

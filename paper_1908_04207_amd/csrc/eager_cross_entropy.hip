@@ -18,9 +18,10 @@
 //
 // Bound by the matrix instructions, busy 54 to 58 % of the time; what they wait for is the barrier between
 // tiles and, in the last round, tiles that do not fill the card.  Measured (rows x width x vocabulary): 4096 x 1024 x 50257
-// bf16 forward 453 us (930 TFLOP/s), backward with a tenth of the rows masked: dl 434 us, dx and dw 822 us (923 TFLOP/s of the
-// rows that count); 8191 x 1600 x 50257 forward 1157 us (1139 TFLOP/s), two pieces of dl 602 and of dx and dw 1306 us
-// (957 with 5 % masked); fp32 1019 x 1024 x 50257: 651, 637, 1166 us (161 TFLOP/s forward, 162 backward); 61 x 1024 x 50257
+// bf16 forward 457 us (923 TFLOP/s), backward with a tenth of the rows masked: dl 439 us and 6 for the targets' entries, dx and dw
+// 815 us (931 TFLOP/s of the rows that count); 8191 x 1600 x 50257 forward 1157 us (1139 TFLOP/s), two pieces of dl 602 and of dx and dw 1306 us
+// (957 with 5 % masked); fp32 1019 x 1024 x 50257: 639, 652, 1176 us (164 TFLOP/s forward, 160 dx and dw; 36 to 56 bytes a
+// lane in scratch memory with tiles of 256 x 256); 61 x 1024 x 50257
 // forward 19.4 us, 5.3 TB/s of the projection.
 //
 // Slower: the compiler's own order of matrix instructions and reads (10 to 15 %, see spread()), 4 wavefronts of 256 x 256
@@ -637,7 +638,7 @@ __global__ __launch_bounds__(1024) void before_kernel(const Gather g, int *befor
 }
 
 // The targets' entries of dl, 16 rows a workgroup: minus the others' sum, 64 threads a row.  Bound by the latency of
-// the loads and the launch.
+// the loads and the launch: 4096 rows of 197 tiles 6.0 us, 1019 5.2 us.
 template <typename T>
 __global__ __launch_bounds__(1024) void targets_kernel(const Product p, T *dl)
 {

@@ -67,7 +67,7 @@ double gradients_time(long long rows, int width, long long live, int dw_slices, 
 
 // How the backward pass is cut: vocabulary rows of a piece; slices that are summed apart, of a
 // piece for dx and, where there is one piece, of the rows for dw; the shapes of tiles.  The fastest cut by
-// the above is taken among those whose dl fit 512 MiB (4096 columns of many rows).
+// the above is taken among those whose dl fit 512 MiB; 4096 columns are taken of however many rows (1 GiB in fp32 for 65536).
 enum { kLarge, kMedium, kNarrow };
 struct Cut {
     long long rows_padded, piece;
@@ -175,8 +175,8 @@ inline int norm_rope_blocks(long long tokens, int q_heads, int kv_heads)
 constexpr int kAttentionRows = 128;
 inline long long tile_numbers(long long tokens, int sequences, int rows) { return tokens / rows + sequences + 2; }
 
-// Two workgroups have a compute unit: 512 run at once, and about four rounds of them even out what a
-// causal mask leaves to each.  Measured (16 heads of 64, 4 of keys, 16 sequences of 8192 tokens, bf16): 4 parts 50 us and
+// Of the keys' kernel in bf16 with heads of up to 64 two workgroups have a compute unit, 512 run at once (of its other forms one
+// and 256), and about four rounds of them even out what a causal mask leaves to each.  Measured (16 heads of 64, 4 of keys, 16 sequences of 8192 tokens, bf16): 4 parts 50 us and
 // 12 for their sums, 2 parts (of a limit of 600) 62 and 8.
 inline int attention_parts(long long tokens, int q_heads, int kv_heads, int sequences)
 {
