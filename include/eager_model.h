@@ -139,8 +139,8 @@ typedef struct {
  * negative target or a dloss of zero are left out from the start: they cost nothing, whatever x
  * holds there reaches no gradient, and their dx is zero.  dx or dw may be NULL (not wanted).  In bf16
  * the dl of a piece are held in bf16 between the products.
- * p - 1 of a target is formed as minus the sum of the others, so that it keeps its digits where p is
- * close to 1, as long as one piece holds the vocabulary (dl of up to 512 MiB, or 4096 columns of them);
+ * p - 1 of a target is formed as minus the sum of the others where p is beyond a half, so that it keeps its
+ * digits where p is close to 1, as long as one piece holds the vocabulary (dl of up to 512 MiB, or 4096 columns of them);
  * with more pieces it is exp(l - lse) - 1 and as far off as lse in fp32 is (2^-24 |lse|).
  * fp32 products as in eager_attention().
  * workspace_bytes: what the forward (backward = 0) or the backward pass (1) needs.

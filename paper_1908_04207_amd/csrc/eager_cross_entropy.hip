@@ -329,7 +329,7 @@ __device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b
                         if (wave_a + 32 * i + 8 * (r >> 2) + 4 * half + (r & 3) >= live) c[i][j][r] = 0.0f;
             }
         }
-        // 1 - p of the target is the sum of the others: lse in fp32 is up to 2^-24 of itself off, too much for rows
+        // 1 - p of the target as the sum of the others: lse in fp32 is up to 2^-24 of itself off, too much for rows
         // whose p is close to 1.  With the whole vocabulary in one tile p is normalised anew as well; with more tiles
         // each leaves its sum and targets_kernel puts the target's entry in.
         if (p.others) {
@@ -637,7 +637,8 @@ __global__ __launch_bounds__(1024) void before_kernel(const Gather g, int *befor
     }
 }
 
-// The targets' entries of dl, 16 rows a workgroup: minus the others' sum, 64 threads a row.  Bound by the latency of
+// The targets' entries of dl, 16 rows a workgroup: minus the others' sum, 64 threads a row.  Only where that is the smaller of
+// the two: all p are off by lse's rounding relative to themselves, so p - 1 is the better one for a small p.  Bound by the latency of
 // the loads and the launch: 4096 rows of 197 tiles 6.0 us, 1019 5.2 us.
 template <typename T>
 __global__ __launch_bounds__(1024) void targets_kernel(const Product p, T *dl)
@@ -658,7 +659,7 @@ __global__ __launch_bounds__(1024) void targets_kernel(const Product p, T *dl)
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum += part[i][in];
     const long long v = p.target[row];
-    if (v < p.vocab) dl[row * p.out_stride + v] = static_cast<T>(-sum * p.dloss[row]);
+    if (v < p.vocab && sum < 0.5f) dl[row * p.out_stride + v] = static_cast<T>(-sum * p.dloss[row]);
 }
 
 // dx (and dw) from the slices' sums, four values a thread

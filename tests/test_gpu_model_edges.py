@@ -219,3 +219,18 @@ def test_attention_shared_keys_summed_by_one_workgroup(ops, dtype, T, group):
         # one rounding of the result and one of each of those that are added here
         bound = mo.U[dtype] * (each.abs().sum(2) * 2.01) + 64 * mo.E * each.abs().sum(2) + 1e-6 * each.abs().amax()
         assert ((got.double() - each.sum(2)).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("rows,width,vocab,sigma", [(1, 24, 2715, 0.2), (5, 24, 1077, 0.2), (3, 8, 300, 1.0), (2, 40, 4000, 0.02)])
+def test_cross_entropy_gradients_of_few_rows_without_favourites(ops, rows, width, vocab, sigma):
+    """Rows whose targets have next to no weight, one by one: there p - 1 is as good as a rounding of one, and the sum of the
+    others, as far off as their common log-sum-exp, is not."""
+    for seed in range(60):
+        gen = torch.Generator().manual_seed(seed)
+        x, w = _normal(gen, rows, width), _normal(gen, vocab, width, sigma=sigma)
+        target, g = torch.randint(0, vocab, (rows,), generator=gen), _normal(gen, rows)
+        xd, wd, td, gd = (t.cuda() for t in (x, w, target, g))
+        lse = ops.cross_entropy(xd, wd, td)[1]
+        want = mo.cross_entropy(x, w, target, g)
+        for name, t in zip(("dx", "dw"), ops.cross_entropy_backward(gd, xd, wd, td, lse)):
+            _check(f"{name} {seed}", t, *want[name])
