@@ -639,7 +639,8 @@ __global__ __launch_bounds__(1024) void before_kernel(const Gather g, int *befor
 
 // The targets' entries of dl, 16 rows a workgroup: minus the others' sum, 64 threads a row.  Only where that is the smaller of
 // the two: all p are off by lse's rounding relative to themselves, so p - 1 is the better one for a small p.  Bound by the latency of
-// the loads and the launch: 4096 rows of 197 tiles 6.0 us, 1019 5.2 us.
+// the loads and the launch: 4096 rows of 197 tiles 6.0 us, 1019 5.2 us; of a small
+// backward pass (64 x 256 x 1009 in bf16 23.6 us, 500 x 512 x 3000 35.8) the sums and this launch are 2 and 3.5 us.
 template <typename T>
 __global__ __launch_bounds__(1024) void targets_kernel(const Product p, T *dl)
 {
