@@ -5,8 +5,12 @@
  *   eager_qk_norm_rope      RMS norm of every query and key head, then the rotation by position
  *   eager_attention         causal attention over packed sequences of different lengths
  *   eager_cross_entropy     output projection and softmax cross entropy over the vocabulary
+ *   eager_layer_norm        residual sum and layer norm of the hidden states
+ *   eager_rotary            the rotation by position alone, of whole heads or a part, in both layouts of pairs;
+ *                           eager_rotary_table makes its table, also for contexts longer than those of training
+ *   eager_distillation      output projection and the divergence from a teacher's top logits
  *
- * each with its backward pass.  Gradients of weights are written to where the caller says, for
+ * each (but for the table) with its backward pass.  Gradients of weights are written to where the caller says, for
  * example into a bucket of a process's gradient arena, which a round then reads.
  *
  * Conventions, in addition to those of eager.h
@@ -17,8 +21,8 @@
  *     Both sides of a product have dtype: in bf16 the factors that are formed in between (P of attention
  *     and the gradients of its scores, the gradients of logits) are rounded to it, a result is then about
  *     0.0025 of its norm off, 0.0017 of which is its own rounding.
- *   - Device pointers are 16-byte aligned (lse, loss, dloss, dwq, dwk, positions, cu_seqlens: 4 bytes;
- *     target: 8); strides are in elements, multiples of 16 bytes, at least the length of what they
+ *   - Device pointers are 16-byte aligned (lse, loss, dloss, dwq, dwk, positions, cu_seqlens, stats, dw and db of
+ *     a layer norm, a teacher's logits and picked: 4 bytes; target and a teacher's index: 8); strides are in elements, multiples of 16 bytes, at least the length of what they
  *     step over (no broadcast views) and, but for a head_stride, at most 2^21.  Arrays of no
  *     elements may be NULL.
  *   - Outputs and workspaces must not overlap each other or any input, except where said.
@@ -153,6 +157,124 @@ int eager_cross_entropy_workspace_bytes(int dtype, const eager_projection *shape
 int eager_cross_entropy_backward(int dtype, const eager_projection *shape, const void *x, const void *w,
                                  const int64_t *target, const float *lse, const float *dloss, void *dx,
                                  void *dw, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Rows of hidden states: element i of row r is data[r * stride + i]. */
+typedef struct {
+    void   *data;
+    int64_t stride;
+} eager_rows;
+
+#define EAGER_MAX_NORM_WIDTH 16384
+
+/*
+ * Residual sum and layer norm of every row (width: a multiple of 8 up to EAGER_MAX_NORM_WIDTH):
+ *     s = x + residual, rounded to dtype,   m = mean(s),  r = (mean((s - m)^2) + eps)^(-1/2),
+ *     y = (s - m) r w + b
+ * and stats[row] = m, stats[rows + row] = r, for the backward pass.  The norm is that of the s that is stored.
+ * residual and sum may be NULL, both or none: s is x.  b may be NULL: none is added.  sum and y may each be x or
+ * residual, but not the same one.  A row of equal values has r = eps^(-1/2), with eps = 0 NaN in y.  Non-finite
+ * values stay in their row.
+ * Errors: EINVAL (NULL, alignment, strides, sizes, eps negative or not finite), EDEVICE.
+ *
+ * Backward, from the gradients dy of y and ds of s (NULL: s is used nowhere else):
+ *     dn = dy w,  n = (s - m) r,  dx = ds + r (dn - mean(dn) - n mean(dn n)),  dw = sum dy n,  db = sum dy
+ * dx is the gradient of x and of residual; it may be dy or ds.  dw and db (width values of dtype, the sums over all
+ * rows rounded once) may be NULL: not wanted.  w and stats as in the forward pass.
+ */
+int eager_layer_norm(int dtype, int64_t rows, int32_t width, const eager_rows *x, const eager_rows *residual,
+                     const void *w, const void *b, float eps, const eager_rows *sum, const eager_rows *y,
+                     float *stats, void *stream);
+int eager_layer_norm_workspace_bytes(int dtype, int64_t rows, int32_t width, int64_t *bytes);
+int eager_layer_norm_backward(int dtype, int64_t rows, int32_t width, const eager_rows *dy, const eager_rows *ds,
+                              const eager_rows *s, const void *w, const float *stats, const eager_rows *dx,
+                              void *dw, void *db, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* How the angles of a rotation's table follow from the position: angle = position * f_i of pair i < part / 2. */
+typedef enum {
+    EAGER_ANGLES_PLAIN = 0,    /* f_i = base^(-2 i / part) */
+    EAGER_ANGLES_LINEAR = 1,   /* f_i / factor: positions squeezed into the original context */
+    EAGER_ANGLES_BASE = 2,     /* base * factor^(part / (part - 2)): the slowest pair squeezed, the fastest kept */
+    EAGER_ANGLES_PARTS = 3     /* f_i (keep + (1 - keep) / factor), keep = (t - low) / (high - low) held to 0 .. 1 with
+                                  t = original f_i / (2 pi) turns over the original context: pairs of `high` turns and
+                                  more are kept, of `low` and fewer squeezed */
+} eager_angle_scaling;
+
+typedef struct {
+    int64_t positions;         /* rows of the table: 0 .. 2^31 - 2^16 */
+    int32_t part;              /* elements of a head that are rotated: a multiple of 8 up to EAGER_MAX_HEAD_DIM */
+    int32_t scaling;           /* eager_angle_scaling */
+    double  base;              /* >= 1 */
+    double  factor;            /* >= 1 (not used by PLAIN) */
+    double  original;          /* > 0 (PARTS alone) */
+    double  low, high;         /* 0 <= low < high (PARTS alone) */
+    double  magnitude;         /* cosines and sines are multiplied by it (1: a rotation) */
+} eager_angles;
+
+/*
+ * cos_table[p * part / 2 + i] = magnitude cos(p f_i), sin_table[...] likewise: angles and functions in 64 bits,
+ * rounded once.  Errors: EINVAL (NULL, alignment, sizes, values out of range or not finite), EDEVICE.
+ */
+int eager_rotary_table(const eager_angles *angles, float *cos_table, float *sin_table, void *stream);
+
+/* Which elements of a head make pair i < part / 2. */
+typedef enum {
+    EAGER_ROTARY_HALVES = 0,         /* i and i + part / 2 */
+    EAGER_ROTARY_INTERLEAVED = 1     /* 2 i and 2 i + 1 */
+} eager_rotary_layout;
+
+/*
+ * The first `part` elements (a multiple of 8, up to head_dim) of every head of q and k turned by the position's
+ * angles, the others as they are: of a pair (a, b),
+ *     a' = a cos - b sin,  b' = b cos + a sin.
+ * rotation: tables of part / 2 columns.  q_out and k_out may be q and k themselves; nothing behind `part` is moved
+ * then.  A token whose position is outside the table gets NaN in the first `part` elements of its output heads.
+ * Errors: EINVAL (NULL, alignment, strides, sizes, layout), EDEVICE.
+ *
+ * Backward: the same with the sines' sign turned, from the gradients of the outputs; dq, dk may be dq_out, dk_out.
+ */
+int eager_rotary(int dtype, const eager_packed *shape, const eager_heads *q, const eager_heads *k,
+                 const eager_rotation *rotation, int32_t part, int layout, const eager_heads *q_out,
+                 const eager_heads *k_out, void *stream);
+int eager_rotary_backward(int dtype, const eager_packed *shape, const eager_heads *dq_out, const eager_heads *dk_out,
+                          const eager_rotation *rotation, int32_t part, int layout, const eager_heads *dq,
+                          const eager_heads *dk, void *stream);
+
+#define EAGER_MAX_ENTRIES 256
+
+/* A teacher's top logits: of row r, entry k < entries is the logit logits[r * entries + k] of the word
+ * index[r * entries + k] (device).  An entry with a negative index, or a logit of -infinity, counts nothing, whatever
+ * else stands there; a row without an entry that counts is masked.  A word may stand in several entries. */
+typedef struct {
+    const int64_t *index;
+    const float   *logits;
+    int32_t        entries;       /* 1 .. EAGER_MAX_ENTRIES */
+    float          temperature;   /* 2^-20 .. 2^20 */
+} eager_teacher;
+
+/*
+ * With t the teacher's logits of a row, l_v = <x_r, w_v>, q = softmax(t / temperature) over the entries that count
+ * and p = softmax(l / temperature) over the vocabulary:
+ *     loss[r] = sum_k q_k (log q_k - log p_{index_k}),  lse[r] = log sum_v exp(l_v / temperature),
+ *     picked[r * entries + k] = l_{index_k}  (0 where the entry counts nothing)
+ * A masked row has loss 0.  An index beyond the vocabulary gives loss and picked NaN.  The student's logits are
+ * not stored.  The loss is not multiplied by the temperature's square; dloss may be.
+ * Errors: EINVAL (NULL, alignment, strides, sizes, temperature, workspace too small), EDEVICE.
+ *
+ * Backward, for the upstream gradients dloss[r] (device, fp32), from lse and picked of the forward pass:
+ *     dl_v = dloss[r] / temperature (p_v - sum of the q_k with index_k = v),  dx_r = sum_v dl_v w_v,
+ *     dw_v = sum_r dl_v x_r
+ * in pieces of the vocabulary, as eager_cross_entropy_backward.  Masked rows and rows with a dloss of zero are left
+ * out from the start.  The dl of the word that the teacher favours most is formed from the others' p and q where its
+ * p is beyond a half, as long as one piece holds the vocabulary.  dx or dw may be NULL (not wanted).
+ */
+int eager_distillation(int dtype, const eager_projection *shape, const void *x, const void *w,
+                       const eager_teacher *teacher, float *loss, float *lse, float *picked, void *workspace,
+                       int64_t workspace_bytes, void *stream);
+int eager_distillation_workspace_bytes(int dtype, const eager_projection *shape, int backward, int64_t *bytes);
+int eager_distillation_backward(int dtype, const eager_projection *shape, const void *x, const void *w,
+                                const eager_teacher *teacher, const float *lse, const float *picked,
+                                const float *dloss, void *dx, void *dw, void *workspace, int64_t workspace_bytes,
+                                void *stream);
 
 #ifdef __cplusplus
 }

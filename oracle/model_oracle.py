@@ -140,3 +140,123 @@ def cross_entropy(x, w, target, dloss=None):
     result["dx"] = (dx, (dl_err @ w.abs() + (V + 8) * E * (dl.abs() @ w.abs())) * 1.01 + u * dx.abs())
     result["dw"] = (dw, (dl_err.t() @ x.abs() + (rows + 8) * E * (dl.abs().t() @ x.abs())) * 1.01 + u * dw.abs())
     return result
+
+
+# additions one after the other in a sum over a row: 16 values a lane, 6 steps inside a wavefront, 16 wavefronts
+ROW = 38
+
+
+def layer_norm(s, w, b, eps, dy=None, ds=None):
+    """The norm of the stored rows s: dict of y, mean, r and, with dy, dx, dw, db: (value, bound)."""
+    u = U[s.dtype]
+    s, w = s.to(F), w.to(F)
+    rows, d = s.shape
+    depth = min(d, ROW) + 2
+    m = s.mean(1, keepdim=True)
+    m_err = depth * E * s.abs().mean(1, keepdim=True) + E * m.abs()
+    c = s - m
+    var = c.square().mean(1, keepdim=True)
+    r = (var + eps) ** -0.5
+    # squares around a mean that is off by m_err are larger by its square; the root halves, and rounds itself
+    rel_r = ((depth + 4) * E * var + m_err.square() + 2 * E * m_err * c.abs().mean(1, keepdim=True)) * r.square() / 2 + 4 * E
+    n = c * r
+    n_err = (m_err + E * c.abs()) * r + n.abs() * (rel_r + 2 * E)
+    y = n * w + (0 if b is None else b.to(F))
+    size = (n * w).abs() + (0 if b is None else b.to(F).abs())
+    out = {"y": (y, (w.abs() * n_err + 3 * E * size) * 1.01 + u * y.abs()), "mean": (m[:, 0], m_err[:, 0]),
+           "r": (r[:, 0], (rel_r * r)[:, 0])}
+    if dy is None:
+        return out
+    dy = dy.to(F)
+    dn = dy * w
+    even, even_err = dn.mean(1, keepdim=True), (depth + 2) * E * dn.abs().mean(1, keepdim=True)
+    along = (dn * n).mean(1, keepdim=True)
+    along_err = (depth + 3) * E * (dn * n).abs().mean(1, keepdim=True) + (dn.abs() * n_err).mean(1, keepdim=True)
+    inner = dn - even - n * along
+    size = dn.abs() + even.abs() + (n * along).abs()
+    dx = r * inner
+    err = r * (even_err + n_err * along.abs() + n.abs() * along_err + 4 * E * size) + dx.abs() * rel_r
+    if ds is not None:
+        dx = dx + ds.to(F)
+        err = err + 2 * E * ds.to(F).abs()
+    out["dx"] = (dx, err * 1.01 + u * dx.abs())
+    # rows one after the other: those of a group of lanes, of a workgroup's groups, of 64 slices of up to 512 workgroups
+    deep = min(rows, rows // 512 + 16 + 8 + 64) + 4
+    dw, db = (dy * n).sum(0), dy.sum(0)
+    out["dw"] = (dw, (deep * E * (dy * n).abs().sum(0) + (dy.abs() * n_err).sum(0)) * 1.01 + u * dw.abs())
+    out["db"] = (db, deep * E * dy.abs().sum(0) * 1.01 + u * db.abs())
+    return out
+
+
+def frequencies(part, base, scaling="none", factor=1.0, original=0.0, low=1.0, high=32.0):
+    """Angles of one position, pair by pair."""
+    out = []
+    for i in range(part // 2):
+        f = base ** (-2 * i / part)
+        if scaling == "linear":
+            f = f / factor
+        if scaling == "base":
+            f = (base * factor ** (part / (part - 2))) ** (-2 * i / part)
+        if scaling == "parts":
+            turns = original * f / (2 * math.pi)
+            keep = 1.0 if turns >= high else 0.0 if turns <= low else (turns - low) / (high - low)
+            f = keep * f + (1 - keep) * f / factor
+        out.append(f)
+    return torch.tensor(out, dtype=F)
+
+
+def rotary(x, cos, sin, positions, interleaved, back=False):
+    """One of q, k: (y, bound); back: turned the other way, as its gradient is."""
+    u = U[x.dtype]
+    x = x.to(F)
+    half = cos.shape[1]
+    c, s = cos.to(F)[positions.long()][:, None, :], sin.to(F)[positions.long()][:, None, :]
+    s = -s if back else s
+    y, size = x.clone(), torch.zeros_like(x)
+    at = (slice(0, 2 * half, 2), slice(1, 2 * half, 2)) if interleaved else (slice(0, half), slice(half, 2 * half))
+    a, b = x[..., at[0]], x[..., at[1]]
+    y[..., at[0]], y[..., at[1]] = a * c - b * s, b * c + a * s
+    size[..., at[0]], size[..., at[1]] = (a * c).abs() + (b * s).abs(), (b * c).abs() + (a * s).abs()
+    moved = size.abs() > 0
+    return y, torch.where(moved, u * y.abs() + 2 * E * size, 0.0) * 1.01
+
+
+def distillation(x, w, index, logits, tau, dloss=None):
+    """dict of loss, lse, picked and, with dloss, dx, dw: (value, bound).  Words lie in the vocabulary or are negative."""
+    u = U[x.dtype]
+    x, w = x.to(F), w.to(F)
+    rows, d = x.shape
+    V, K = w.shape[0], index.shape[1]
+    l = x @ w.t()
+    l_err = ((d + 2) * E * (x.abs() @ w.abs().t())).amax(1, keepdim=True)
+    lse = torch.logsumexp(l / tau, 1, keepdim=True)
+    s_err = l_err / tau + (V + 16) * E + 10 * E * l.abs().amax(1, keepdim=True) / tau + 4 * E * lse.abs()
+    used = (index >= 0) & (logits != -math.inf)
+    counted = used.any(1, keepdim=True)
+    at = torch.where(used, index, 0)
+    picked = torch.where(used, l.gather(1, at), 0.0)
+    t = torch.where(used, logits.to(F) / tau, -math.inf)
+    t_top = torch.where(counted, t.amax(1, keepdim=True), 0.0)
+    log_q = torch.where(used, t - torch.where(counted, torch.logsumexp(t, 1, keepdim=True), 0.0), 0.0)
+    q = torch.where(used, log_q.exp(), 0.0)
+    far = torch.where(used, t_top - t, 0.0)
+    # distances in the exponent, exponentials and their sum
+    q_err = 6 * E * far + 6 * E * (q * far).sum(1, keepdim=True) + (16 + 8) * E
+    log_p = torch.where(used, picked / tau - lse, 0.0)
+    term = torch.where(used, log_q - log_p, 0.0)
+    term_err = q_err + l_err / tau + s_err + 6 * E * (log_q.abs() + log_p.abs())
+    result = {"loss": ((q * term).sum(1), (q * (term_err + q_err * term.abs() + 16 * E * term.abs())).sum(1) * 1.01),
+              "lse": (lse[:, 0], s_err[:, 0]), "picked": (picked, torch.where(used, l_err, 0.0))}
+    if dloss is None:
+        return result
+    p = torch.exp(l / tau - lse)
+    share, share_err = torch.zeros_like(p), torch.zeros_like(p)
+    share.scatter_add_(1, at, q)
+    share_err.scatter_add_(1, at, q * q_err)
+    g = torch.where(counted[:, 0], dloss.to(F), 0.0)[:, None] / tau
+    dl = g * (p - share)
+    dl_err = u * dl.abs() + g.abs() * (p * (s_err + l_err / tau) + share_err + 4 * E * (p + share))
+    dx, dw = dl @ w, dl.t() @ x
+    result["dx"] = (dx, (dl_err @ w.abs() + (V + 8) * E * (dl.abs() @ w.abs())) * 1.01 + u * dx.abs())
+    result["dw"] = (dw, (dl_err.t() @ x.abs() + (rows + 8) * E * (dl.abs().t() @ x.abs())) * 1.01 + u * dw.abs())
+    return result

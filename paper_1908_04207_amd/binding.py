@@ -44,6 +44,9 @@ EXPORTS = (
     "eager_qk_norm_rope", "eager_qk_norm_rope_workspace_bytes", "eager_qk_norm_rope_backward",
     "eager_attention", "eager_attention_workspace_bytes", "eager_attention_backward",
     "eager_cross_entropy", "eager_cross_entropy_workspace_bytes", "eager_cross_entropy_backward",
+    "eager_layer_norm", "eager_layer_norm_workspace_bytes", "eager_layer_norm_backward",
+    "eager_rotary_table", "eager_rotary", "eager_rotary_backward",
+    "eager_distillation", "eager_distillation_workspace_bytes", "eager_distillation_backward",
 )
 
 
@@ -85,6 +88,28 @@ class Rotation(ctypes.Structure):
 class Projection(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int32), ("vocab", ctypes.c_int32),
                 ("x_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64)]
+
+
+class Rows(ctypes.Structure):
+    """eager_rows: rows of hidden states as a strided view (strides in elements)."""
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+
+
+class Angles(ctypes.Structure):
+    """eager_angles: how a rotation's angles follow from the position."""
+    _fields_ = [("positions", ctypes.c_int64), ("part", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double), ("original", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class Teacher(ctypes.Structure):
+    """eager_teacher: the top logits of a teacher's rows."""
+    _fields_ = [("index", ctypes.c_void_p), ("logits", ctypes.c_void_p), ("entries", ctypes.c_int32),
+                ("temperature", ctypes.c_float)]
+
+
+ANGLES_PLAIN, ANGLES_LINEAR, ANGLES_BASE, ANGLES_PARTS = 0, 1, 2, 3
+ROTARY_HALVES, ROTARY_INTERLEAVED = 0, 1
 
 
 def _load() -> ctypes.CDLL:
@@ -155,6 +180,16 @@ def _load() -> ctypes.CDLL:
     lib.eager_cross_entropy.argtypes = [i32, Pj, vp, vp, vp, vp, vp, vp, i64, vp]
     lib.eager_cross_entropy_workspace_bytes.argtypes = [i32, Pj, i32, ctypes.POINTER(i64)]
     lib.eager_cross_entropy_backward.argtypes = [i32, Pj, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    Rw, An, Te = (ctypes.POINTER(t) for t in (Rows, Angles, Teacher))
+    lib.eager_layer_norm.argtypes = [i32, i64, i32, Rw, Rw, vp, vp, f32, Rw, Rw, vp, vp]
+    lib.eager_layer_norm_workspace_bytes.argtypes = [i32, i64, i32, ctypes.POINTER(i64)]
+    lib.eager_layer_norm_backward.argtypes = [i32, i64, i32, Rw, Rw, Rw, vp, vp, Rw, vp, vp, vp, i64, vp]
+    lib.eager_rotary_table.argtypes = [An, vp, vp, vp]
+    lib.eager_rotary.argtypes = [i32, Pk, H, H, Rt, i32, i32, H, H, vp]
+    lib.eager_rotary_backward.argtypes = [i32, Pk, H, H, Rt, i32, i32, H, H, vp]
+    lib.eager_distillation.argtypes = [i32, Pj, vp, vp, Te, vp, vp, vp, vp, i64, vp]
+    lib.eager_distillation_workspace_bytes.argtypes = [i32, Pj, i32, ctypes.POINTER(i64)]
+    lib.eager_distillation_backward.argtypes = [i32, Pj, vp, vp, Te, vp, vp, vp, vp, vp, vp, i64, vp]
     return lib
 
 
@@ -170,6 +205,7 @@ class _CtypesOnly:
 
     plan_participation = plan_quorum = round = step = stash = views = _unknown
     qk_norm_rope = attention = cross_entropy = _unknown
+    layer_norm = layer_norm_backward = rotary = distillation = _unknown
 
     @staticmethod
     def streams(*_):
@@ -624,3 +660,60 @@ def eager_cross_entropy_backward(dtype: int, shape: Projection, x, w, target, ls
     _status(lib.eager_cross_entropy_backward(dtype, shape, _ptr(x), _ptr(w), _ptr(target), _ptr(lse), _ptr(dloss),
                                              _ptr(dx), _ptr(dw), _ptr(workspace), workspace_bytes, _stream(stream)),
             "eager_cross_entropy_backward")
+
+
+def rows(x) -> Rows:
+    """The view of a tensor [rows, width] whose last axis is contiguous."""
+    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise EagerError(EINVAL, f"expected [rows, width] with contiguous rows, got {tuple(x.shape)} with strides {x.stride()}")
+    # a lone row may have any stride
+    return Rows(x.data_ptr(), x.stride(0) if x.shape[0] > 1 else x.shape[1])
+
+
+def eager_layer_norm(dtype: int, count: int, width: int, x: Rows, residual: Optional[Rows], w, b, eps: float,
+                     sum: Optional[Rows], y: Rows, stats, stream=None) -> None:
+    _status(lib.eager_layer_norm(dtype, count, width, x, residual, _ptr(w), _ptr(b), eps, sum, y, _ptr(stats),
+                                 _stream(stream)), "eager_layer_norm")
+
+
+def eager_layer_norm_workspace_bytes(dtype: int, count: int, width: int) -> int:
+    return _workspace_bytes(lib.eager_layer_norm_workspace_bytes, "eager_layer_norm_workspace_bytes", dtype, count, width)
+
+
+def eager_layer_norm_backward(dtype: int, count: int, width: int, dy: Rows, ds: Optional[Rows], s: Rows, w, stats, dx: Rows,
+                              dw, db, workspace, workspace_bytes: int, stream=None) -> None:
+    _status(lib.eager_layer_norm_backward(dtype, count, width, dy, ds, s, _ptr(w), _ptr(stats), dx, _ptr(dw), _ptr(db),
+                                          _ptr(workspace), workspace_bytes, _stream(stream)), "eager_layer_norm_backward")
+
+
+def eager_rotary_table(angles: Angles, cos_table, sin_table, stream=None) -> None:
+    _status(lib.eager_rotary_table(angles, _ptr(cos_table), _ptr(sin_table), _stream(stream)), "eager_rotary_table")
+
+
+def eager_rotary(dtype: int, shape: Packed, q: Heads, k: Heads, rotation: Rotation, part: int, layout: int, q_out: Heads,
+                 k_out: Heads, stream=None) -> None:
+    _status(lib.eager_rotary(dtype, shape, q, k, rotation, part, layout, q_out, k_out, _stream(stream)), "eager_rotary")
+
+
+def eager_rotary_backward(dtype: int, shape: Packed, dq_out: Heads, dk_out: Heads, rotation: Rotation, part: int, layout: int,
+                          dq: Heads, dk: Heads, stream=None) -> None:
+    _status(lib.eager_rotary_backward(dtype, shape, dq_out, dk_out, rotation, part, layout, dq, dk, _stream(stream)),
+            "eager_rotary_backward")
+
+
+def eager_distillation(dtype: int, shape: Projection, x, w, teacher: Teacher, loss, lse, picked, workspace,
+                       workspace_bytes: int, stream=None) -> None:
+    _status(lib.eager_distillation(dtype, shape, _ptr(x), _ptr(w), teacher, _ptr(loss), _ptr(lse), _ptr(picked),
+                                   _ptr(workspace), workspace_bytes, _stream(stream)), "eager_distillation")
+
+
+def eager_distillation_workspace_bytes(dtype: int, shape: Projection, backward: bool) -> int:
+    return _workspace_bytes(lib.eager_distillation_workspace_bytes, "eager_distillation_workspace_bytes", dtype, shape,
+                            int(backward))
+
+
+def eager_distillation_backward(dtype: int, shape: Projection, x, w, teacher: Teacher, lse, picked, dloss, dx, dw, workspace,
+                                workspace_bytes: int, stream=None) -> None:
+    _status(lib.eager_distillation_backward(dtype, shape, _ptr(x), _ptr(w), teacher, _ptr(lse), _ptr(picked), _ptr(dloss),
+                                            _ptr(dx), _ptr(dw), _ptr(workspace), workspace_bytes, _stream(stream)),
+            "eager_distillation_backward")

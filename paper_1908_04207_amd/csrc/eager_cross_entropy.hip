@@ -26,6 +26,8 @@
 //
 // Slower: the compiler's own order of matrix instructions and reads (10 to 15 %, see spread()), 4 wavefronts of 256 x 256
 // (8 %), wavefronts of raised priority (no effect).
+#include "eager_distillation.h"
+#include "eager_joined.h"
 #include "eager_launch.h"
 #include "eager_matrix.h"
 #include "eager_model.h"
@@ -58,6 +60,7 @@ struct Product {
     float *right;            // logit of the target
     const long long *target;
     const float *lse, *dloss;
+    float scale;             // of the logits in exponents of two: log2(e) / temperature
     long long first;         // vocabulary index of a row 0
     int live;                // rows of a that are vocabulary (the rest is padding)
     int vocab;
@@ -258,14 +261,14 @@ __device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
                         if (whole || 32 * i + 8 * (r >> 2) + (r & 3) < live) top = fmaxf(top, c[i][j][r]);
-                // in powers of two from here on: what rounding leaves of top * kLog2e stays in the exponents
-                top *= kLog2e;
+                // in powers of two from here on: what rounding leaves of top * scale stays in the exponents
+                top *= p.scale;
                 const float base = top == -__builtin_inff() ? 0.0f : top;
 #pragma unroll
                 for (int i = 0; i < MI; ++i)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        const float e = exp2_fast(fmaf(c[i][j][r], kLog2e, -base));
+                        const float e = exp2_fast(fmaf(c[i][j][r], p.scale, -base));
                         if (whole || 32 * i + 8 * (r >> 2) + (r & 3) < live) sum += e;
                     }
             };
@@ -320,7 +323,7 @@ __device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b
 #pragma unroll
             for (int i = 0; i < MI; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) c[i][j][r] = exp2_fast(fmaf(c[i][j][r], kLog2e, -lse));
+                for (int r = 0; r < 16; ++r) c[i][j][r] = exp2_fast(fmaf(c[i][j][r], p.scale, -lse));
             if (__any(live < wave_a + 32 * MI)) {
 #pragma unroll
                 for (int i = 0; i < MI; ++i)
@@ -502,43 +505,16 @@ __global__ __launch_bounds__(Shape::Threads) void gradients_kernel(const Product
     else gradient<T, Shape, false, kSums>(dx, id - dw_tiles, tile0, tile1);
 }
 
-__device__ __forceinline__ void join(float &top, float &sum, float2 q)
-{
-    const float both = fmaxf(top, q.x), zero = both == -__builtin_inff() ? 0.0f : both;
-    sum = sum * exp2_fast(top - zero) + q.y * exp2_fast(q.x - zero);
-    top = both;
-}
-
 // loss and lse of 16 rows from the tiles' statistics: 64 threads a row share the tiles, four loads of each under way at
 // a time.  Bound by the latency of the loads and the launch: 61 rows of 393 tiles 4.1 us, 4096 of 197 4.9 (64 rows a workgroup: 6.0 and 5.5)
-constexpr int kJoined = 16;
 __global__ __launch_bounds__(1024) void rows_kernel(const float2 *stats, const float *right, const long long *target,
                                                     float *loss, float *lse, long long rows, int tiles, int vocab)
 {
-    constexpr int Threads = 1024 / kJoined;                 // of a row
     __shared__ float2 part[16][kJoined];
-    const int in = threadIdx.x % kJoined, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long row = static_cast<long long>(blockIdx.x) * kJoined + in;
-    float top = -__builtin_inff(), sum = 0.0f;
-    if (row < rows)
-        for (int t = threadIdx.x / kJoined; t < tiles; t += 4 * Threads) {
-            float2 q[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                q[i] = t + Threads * i < tiles ? stats[(t + Threads * i) * rows + row] : make_float2(-__builtin_inff(), 0.0f);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) join(top, sum, q[i]);
-        }
-#pragma unroll
-    for (int other = kJoined; other < 64; other *= 2) {
-        const float2 q = make_float2(__shfl_xor(top, other, 64), __shfl_xor(sum, other, 64));
-        join(top, sum, q);
-    }
-    if (lane < kJoined) part[wave][in] = make_float2(top, sum);
-    __syncthreads();
+    const float2 all = joined_statistics(stats, rows, tiles, part);
+    const float top = all.x, sum = all.y;
+    const long long row = static_cast<long long>(blockIdx.x) * kJoined + threadIdx.x;
     if (threadIdx.x >= kJoined || row >= rows) return;
-#pragma unroll
-    for (int i = 1; i < 16; ++i) join(top, sum, part[i][in]);
     // the largest logit is not added to the logarithm where the loss takes one away again
     const float log_sum = log1pf(sum - 1.0f);
     const long long t = target[row];
@@ -555,6 +531,7 @@ struct Gather {
     const float *lse, *dloss;
     long long rows, stride;
     int width;
+    float by;                // of dloss
     const int *before;       // per workgroup: counted rows in front of them, or NULL: each counts them
     void *x_out;             // [counted][width]
     long long *target_out;
@@ -593,7 +570,7 @@ __global__ __launch_bounds__(1024) void gather_kernel(const Gather g)
         if (in) {
             g.target_out[to] = g.target[row];
             g.lse_out[to] = g.lse[row];
-            g.dloss_out[to] = g.dloss[row];
+            g.dloss_out[to] = g.dloss[row] * g.by;
         }
         if (lane == 0 && first + kGathered >= g.rows) *g.counted = before + __popcll(mask);
     }
@@ -645,20 +622,10 @@ template <typename T>
 __global__ __launch_bounds__(1024) void targets_kernel(const Product p, T *dl)
 {
     __shared__ float part[16][kJoined];
-    const int in = threadIdx.x % kJoined, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = *p.counted;
-    const long long row = static_cast<long long>(blockIdx.x) * kJoined + in;
-    float sum = 0.0f;
-    if (row < rows)
-#pragma unroll 4
-        for (int t = threadIdx.x / kJoined; t < p.tiles_a; t += 1024 / kJoined) sum += p.others[t * p.b.rows + row];
-#pragma unroll
-    for (int other = kJoined; other < 64; other *= 2) sum += __shfl_xor(sum, other, 64);
-    if (lane < kJoined) part[wave][in] = sum;
-    __syncthreads();
+    const int rows = *p.counted;
+    const long long row = static_cast<long long>(blockIdx.x) * kJoined + threadIdx.x % kJoined;
+    const float sum = joined_sums(p.others, row < rows ? row : -1, p.b.rows, p.tiles_a, part);
     if (threadIdx.x >= kJoined || row >= rows) return;
-    sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) sum += part[i][in];
     const long long v = p.target[row];
     if (v < p.vocab && sum < 0.5f) dl[row * p.out_stride + v] = static_cast<T>(-sum * p.dloss[row]);
 }
@@ -714,17 +681,26 @@ template <typename T>
 hipError_t forward(const CrossEntropyArgs &a, hipStream_t stream)
 {
     const int shape = logits_shape(a.rows, a.width, a.vocab, sizeof(T));
+    const bool taught = a.teacher.index;
+    // a teacher's favourite takes the target's place
+    long long *const favourite = reinterpret_cast<long long *>(a.workspace);
+    if (taught) {
+        const hipError_t e = launch_picked(a, favourite, sizeof(T) == 2, stream);
+        if (e != hipSuccess) return e;
+    }
     const long long tiles = round_up(a.vocab, kSides[shape][0]) / kSides[shape][0];
     Product p = {};
     p.a = {a.w, a.w_stride, a.vocab, a.width};
     p.b = {a.x, a.x_stride, a.rows, a.width};
     p.slices = 1;
     p.live = a.vocab;
-    p.target = a.target;
-    p.stats = reinterpret_cast<float2 *>(a.workspace);
+    p.scale = taught ? kLog2e / a.teacher.temperature : kLog2e;
+    p.target = taught ? favourite : a.target;
+    p.stats = reinterpret_cast<float2 *>(a.workspace + (taught ? teacher_target_bytes(a.rows) : 0));
     p.right = reinterpret_cast<float *>(p.stats + tiles * a.rows);
     const hipError_t e = launch_logits<T, kStats>(p, shape, stream);
     if (e != hipSuccess) return e;
+    if (taught) return launch_divergence(a, p.stats, p.right, favourite, static_cast<int>(tiles), p.scale, stream);
     const float2 *stats = p.stats;
     const float *right = p.right;
     return launch(rows_kernel, dim3(static_cast<unsigned>((a.rows + kJoined - 1) / kJoined)), dim3(1024), 0, stream, stats, right,
@@ -742,10 +718,18 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
     float *sums = reinterpret_cast<float *>(a.workspace + l.dx_sums), *dw_sums = reinterpret_cast<float *>(a.workspace + l.dw_sums);
     int *counted = reinterpret_cast<int *>(a.workspace + l.counted), *place = reinterpret_cast<int *>(a.workspace + l.place);
     Sums of_dx = {}, of_dw = {};
-    Gather g = {a.x, a.target, a.lse, a.dloss, a.rows, a.x_stride, a.width, nullptr, x,
+    const bool taught = a.teacher.index;
+    const float scale = taught ? kLog2e / a.teacher.temperature : kLog2e;
+    const long long *target = a.target;
+    if (taught) {
+        long long *const favourite = reinterpret_cast<long long *>(a.workspace + l.end);
+        if (a.rows) e = launch_favourites(a, favourite, stream);
+        target = favourite;
+    }
+    Gather g = {a.x, target, a.lse, a.dloss, a.rows, a.x_stride, a.width, taught ? 1.0f / a.teacher.temperature : 1.0f, nullptr, x,
                 reinterpret_cast<long long *>(a.workspace + l.target), reinterpret_cast<float *>(a.workspace + l.lse),
                 reinterpret_cast<float *>(a.workspace + l.dloss), place, counted};
-    if (a.rows > kCountedByEach) {
+    if (e == hipSuccess && a.rows > kCountedByEach) {
         int *before = reinterpret_cast<int *>(a.workspace + l.before);
         e = launch(before_kernel, dim3(1), dim3(1024), 0, stream, g, before);
         g.before = before;
@@ -765,7 +749,8 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
             p.first = first;
             p.live = live;
             p.vocab = a.vocab;
-            p.whole = a.vocab <= kSides[c.logits][0];
+            p.scale = scale;
+            p.whole = !taught && a.vocab <= kSides[c.logits][0];
             p.target = g.target_out;
             p.lse = g.lse_out;
             p.dloss = g.dloss_out;
@@ -774,7 +759,10 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
             p.out_stride = padded;
             p.others = c.pieces == 1 && !p.whole ? reinterpret_cast<float *>(a.workspace + l.others) : nullptr;
             e = launch_logits<T, kDlogits>(p, c.logits, stream);
-            if (e == hipSuccess && p.others)
+            if (e == hipSuccess && taught) {
+                const Entries n = {place, g.target_out, g.lse_out, g.dloss_out, p.others, p.tiles_a, dl, padded, first, live, scale};
+                e = launch_entries(a, n, sizeof(T) == 2, stream);
+            } else if (e == hipSuccess && p.others)
                 e = launch(targets_kernel<T>, dim3(static_cast<unsigned>((a.rows + kJoined - 1) / kJoined)), dim3(1024), 0, stream, p, dl);
             if (e != hipSuccess) return e;
         }

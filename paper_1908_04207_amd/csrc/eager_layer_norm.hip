@@ -1,0 +1,270 @@
+// Residual sum and layer norm of rows of hidden states, and their gradients.
+//
+//   s = x + residual (as stored),  m = mean(s),  r = (mean((s - m)^2) + eps)^(-1/2),  n = (s - m) r,  y = n w + b
+//   dn = dy w,  dx = ds + r (dn - mean(dn) - n mean(dn n)),  dw = sum over rows of dy n,  db = sum of dy
+//
+// A row is held by a group of lanes, 16 values each, from its first read to its last write: the mean, then the
+// squares around it, both in fp32, so a row far from zero loses nothing to a difference of squares.  The backward
+// pass takes m and r from the forward pass; its workgroups go through rows at equal steps and keep the sums of dw
+// and db in registers; the groups of a workgroup are added in shared memory in order, the workgroups by a second
+// kernel.
+#include "eager_launch.h"
+#include "eager_model.h"
+#include "eager_model_rules.h"
+#include "eager_vector.h"
+
+namespace eager {
+namespace {
+
+// The sums of two numbers over a group, in each of its lanes.  Groups of more than a wavefront meet in `part`, of which
+// there are two for calls in turn, so one barrier a call is enough.
+template <int Threads>
+__device__ __forceinline__ float2 group_sums(float2 x, float2 *part)
+{
+    constexpr int Waves = Threads / 64;
+    x.x = lanes_sum<(Threads < 64 ? Threads : 64)>(x.x);
+    x.y = lanes_sum<(Threads < 64 ? Threads : 64)>(x.y);
+    if (Waves <= 1) return x;
+    const int wave = threadIdx.x >> 6, first = wave / (Waves > 0 ? Waves : 1) * Waves;
+    if ((threadIdx.x & 63) == 0) part[wave] = x;
+    __syncthreads();
+    x = part[first];
+#pragma unroll
+    for (int i = 1; i < Waves; ++i) {
+        const float2 q = part[first + i];
+        x.x += q.x, x.y += q.y;
+    }
+    return x;
+}
+
+template <int Threads> constexpr int kBlock = Threads < 256 ? 256 : Threads;
+
+template <typename T, int Threads, int C>
+__global__ __launch_bounds__(kBlock<Threads>) void layer_norm_kernel(const LayerNormArgs a)
+{
+    constexpr int E = kVector<T>, Groups = kBlock<Threads> / Threads;
+    __shared__ float2 part[2][16];
+    const int lane = threadIdx.x % Threads;
+    // as many turns for every group of the workgroup
+    for (long long first = static_cast<long long>(blockIdx.x) * Groups; first < a.rows; first += static_cast<long long>(gridDim.x) * Groups) {
+        const long long row = first + threadIdx.x / Threads;
+        const bool live = row < a.rows;
+        float x[C][E], sum = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int at = (c * Threads + lane) * E;
+#pragma unroll
+            for (int i = 0; i < E; ++i) x[c][i] = 0.0f;
+            if (!live || at >= a.width) continue;
+            const auto v = load16(static_cast<const T *>(a.x.data) + row * a.x.stride + at);
+#pragma unroll
+            for (int i = 0; i < E; ++i) x[c][i] = static_cast<float>(v[i]);
+            if (a.residual.data) {
+                const auto u = load16(static_cast<const T *>(a.residual.data) + row * a.residual.stride + at);
+#pragma unroll
+                for (int i = 0; i < E; ++i) x[c][i] = static_cast<float>(static_cast<T>(x[c][i] + static_cast<float>(u[i])));
+                store16(static_cast<T *>(a.sum.data) + row * a.sum.stride + at, x[c]);
+            }
+#pragma unroll
+            for (int i = 0; i < E; ++i) sum += x[c][i];
+        }
+        const float mean = group_sums<Threads>(make_float2(sum, 0.0f), part[0]).x * a.inv_width;
+        float squares = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if ((c * Threads + lane) * E >= a.width) continue;
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                x[c][i] -= mean;
+                squares = fmaf(x[c][i], x[c][i], squares);
+            }
+        }
+        squares = group_sums<Threads>(make_float2(squares, 0.0f), part[1]).x;
+        if (!live) continue;
+        const float r = rsqrtf(fmaf(squares, a.inv_width, a.eps));
+        if (lane == 0) a.stats[row] = mean, a.stats[a.rows + row] = r;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int at = (c * Threads + lane) * E;
+            if (at >= a.width) continue;
+            const auto w = load16(static_cast<const T *>(a.w) + at);
+            if (a.b) {
+                const auto b = load16(static_cast<const T *>(a.b) + at);
+#pragma unroll
+                for (int i = 0; i < E; ++i) x[c][i] = fmaf(x[c][i] * r, static_cast<float>(w[i]), static_cast<float>(b[i]));
+            } else {
+#pragma unroll
+                for (int i = 0; i < E; ++i) x[c][i] = x[c][i] * r * static_cast<float>(w[i]);
+            }
+            store16(static_cast<T *>(a.y.data) + row * a.y.stride + at, x[c]);
+        }
+    }
+}
+
+// a.x: s, a.y: dy, a.residual: ds, a.sum: dx
+template <typename T, int Threads, int C>
+__global__ __launch_bounds__(kBlock<Threads>) void layer_norm_backward_kernel(const LayerNormArgs a)
+{
+    constexpr int E = kVector<T>, Groups = kBlock<Threads> / Threads;
+    typedef typename Vector<T>::type vec;
+    __shared__ float2 part[2][16];
+    __shared__ float sums[Groups > 1 ? 2 * Threads * C * E : 1];
+    const int lane = threadIdx.x % Threads, group = threadIdx.x / Threads;
+    vec w[C] = {}, s[C], g[C], d[C];
+    float gain[C][E], bias[C][E];
+    auto fetch = [&](long long row) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int at = (c * Threads + lane) * E;
+            s[c] = g[c] = d[c] = vec{};
+            if (row >= a.rows || at >= a.width) continue;
+            s[c] = load16(static_cast<const T *>(a.x.data) + row * a.x.stride + at);
+            g[c] = load16(static_cast<const T *>(a.y.data) + row * a.y.stride + at);
+            if (a.residual.data) d[c] = load16(static_cast<const T *>(a.residual.data) + row * a.residual.stride + at);
+        }
+    };
+    const long long step = static_cast<long long>(gridDim.x) * Groups;
+    long long row = static_cast<long long>(blockIdx.x) * Groups + group;
+    fetch(row);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int at = (c * Threads + lane) * E;
+        if (at < a.width) w[c] = load16(static_cast<const T *>(a.w) + at);
+#pragma unroll
+        for (int i = 0; i < E; ++i) gain[c][i] = bias[c][i] = 0.0f;
+    }
+    int turn = 0;
+    // as many turns for every group of the workgroup
+    for (long long first = static_cast<long long>(blockIdx.x) * Groups; first < a.rows; first += step, row += step, turn ^= 1) {
+        const bool live = row < a.rows;
+        const float mean = live ? a.stats[row] : 0.0f, r = live ? a.stats[a.rows + row] : 0.0f;
+        float n[C][E], dn[C][E];
+        vec rest[C];
+        float2 both = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            rest[c] = d[c];
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float dy = static_cast<float>(g[c][i]);
+                n[c][i] = (static_cast<float>(s[c][i]) - mean) * r;
+                dn[c][i] = dy * static_cast<float>(w[c][i]);
+                both.x += dn[c][i];
+                both.y = fmaf(dn[c][i], n[c][i], both.y);
+                gain[c][i] = fmaf(dy, n[c][i], gain[c][i]);
+                bias[c][i] += dy;
+            }
+        }
+        fetch(row + step);
+        both = group_sums<Threads>(both, part[turn]);
+        if (!live) continue;
+        const float even = both.x * a.inv_width, along = both.y * a.inv_width;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int at = (c * Threads + lane) * E;
+            if (at >= a.width) continue;
+#pragma unroll
+            for (int i = 0; i < E; ++i) n[c][i] = fmaf(r, fmaf(-n[c][i], along, dn[c][i] - even), static_cast<float>(rest[c][i]));
+            store16(static_cast<T *>(a.sum.data) + row * a.sum.stride + at, n[c]);
+        }
+    }
+    if (!a.partials) return;
+    float *out = a.partials + static_cast<long long>(blockIdx.x) * 2 * a.width;
+    if (Groups > 1) {
+        constexpr int Columns = Threads * C * E;
+        for (int turns = 0; turns < Groups; ++turns) {
+            if (group == turns) {
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int i = 0; i < E; ++i) {
+                        const int at = (c * Threads + lane) * E + i;
+                        sums[at] = turns ? sums[at] + gain[c][i] : gain[c][i];
+                        sums[Columns + at] = turns ? sums[Columns + at] + bias[c][i] : bias[c][i];
+                    }
+            }
+            __syncthreads();
+        }
+        for (int at = threadIdx.x; at < a.width; at += kBlock<Threads>) {
+            out[at] = sums[at];
+            out[a.width + at] = sums[Columns + at];
+        }
+        return;
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int at = (c * Threads + lane) * E;
+        if (at >= a.width) continue;
+#pragma unroll
+        for (int i = 0; i < E; i += 4) {
+            *reinterpret_cast<f32x4 *>(out + at + i) = f32x4{gain[c][i], gain[c][i + 1], gain[c][i + 2], gain[c][i + 3]};
+            *reinterpret_cast<f32x4 *>(out + a.width + at + i) = f32x4{bias[c][i], bias[c][i + 1], bias[c][i + 2], bias[c][i + 3]};
+        }
+    }
+}
+
+// The workgroups' records of 16 columns of dw (blockIdx.y = 0) or db: 64 sums over every 64th record, then these in
+// order.
+template <typename T>
+__global__ __launch_bounds__(1024) void layer_norm_columns_kernel(const LayerNormArgs a)
+{
+    __shared__ float part[64][17];
+    T *const to = static_cast<T *>(blockIdx.y ? a.db : a.dw);
+    if (!to) return;
+    const int in = threadIdx.x % 16, col = blockIdx.x * 16 + in, slice = threadIdx.x / 16;
+    float sum = 0.0f;
+    if (col < a.width) {
+        const float *p = a.partials + blockIdx.y * a.width + col;
+#pragma unroll 8
+        for (int b = slice; b < a.blocks; b += 64) sum += p[static_cast<long long>(b) * 2 * a.width];
+    }
+    part[slice][in] = sum;
+    __syncthreads();
+    if (threadIdx.x < 16 && col < a.width) {
+#pragma unroll 8
+        for (int i = 1; i < 64; ++i) sum += part[i][in];
+        to[col] = static_cast<T>(sum);
+    }
+}
+
+template <typename T, int Threads, int C>
+hipError_t enqueue(const LayerNormArgs &a, bool backward, hipStream_t stream)
+{
+    constexpr int Groups = kBlock<Threads> / Threads;
+    if (!backward)
+        return launch(layer_norm_kernel<T, Threads, C>, dim3(static_cast<unsigned>(std::min((a.rows + Groups - 1) / Groups, kMostBlocks))),
+                      dim3(kBlock<Threads>), 0, stream, a);
+    hipError_t e = hipSuccess;
+    if (a.blocks) e = launch(layer_norm_backward_kernel<T, Threads, C>, dim3(a.blocks), dim3(kBlock<Threads>), 0, stream, a);
+    if (e != hipSuccess || !a.partials) return e;
+    return launch(layer_norm_columns_kernel<T>, dim3((a.width + 15) / 16, a.db ? 2 : 1), dim3(1024), 0, stream, a);
+}
+
+template <typename T>
+hipError_t dispatch(const LayerNormArgs &a, bool backward, hipStream_t stream)
+{
+    constexpr int C = 16 / kVector<T>;                      // 16 values a lane
+    const int threads = layer_norm_threads(a.width);
+    if (threads == 16)
+        return a.width <= 128 ? enqueue<T, 16, C / 2>(a, backward, stream) : enqueue<T, 16, C>(a, backward, stream);
+    if (threads == 64)
+        return a.width <= 512 ? enqueue<T, 64, C / 2>(a, backward, stream) : enqueue<T, 64, C>(a, backward, stream);
+    if (threads == 128) return enqueue<T, 128, C>(a, backward, stream);
+    if (threads == 256) return enqueue<T, 256, C>(a, backward, stream);
+    if (threads == 512) return enqueue<T, 512, C>(a, backward, stream);
+    return enqueue<T, 1024, C>(a, backward, stream);
+}
+
+}  // namespace
+
+hipError_t launch_layer_norm(const LayerNormArgs &a, bool bf16, hipStream_t stream)
+{
+    return bf16 ? dispatch<__bf16>(a, false, stream) : dispatch<float>(a, false, stream);
+}
+
+hipError_t launch_layer_norm_backward(const LayerNormArgs &a, bool bf16, hipStream_t stream)
+{
+    return bf16 ? dispatch<__bf16>(a, true, stream) : dispatch<float>(a, true, stream);
+}
+
+}  // namespace eager

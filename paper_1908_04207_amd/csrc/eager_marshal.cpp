@@ -345,6 +345,14 @@ struct ModelEntry {
     decltype(&eager_cross_entropy) loss;
     decltype(&eager_cross_entropy_workspace_bytes) loss_bytes;
     decltype(&eager_cross_entropy_backward) loss_backward;
+    decltype(&eager_layer_norm) layer;
+    decltype(&eager_layer_norm_workspace_bytes) layer_bytes;
+    decltype(&eager_layer_norm_backward) layer_backward;
+    decltype(&eager_rotary) rotary;
+    decltype(&eager_rotary_backward) rotary_backward;
+    decltype(&eager_distillation) taught;
+    decltype(&eager_distillation_workspace_bytes) taught_bytes;
+    decltype(&eager_distillation_backward) taught_backward;
 };
 ModelEntry model;
 PyObject *t_f32, *t_bf16, *t_i32, *t_i64, *new_workspace;
@@ -578,6 +586,150 @@ PyObject *py_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
     return st == EAGER_EINVAL ? other_form() : PyLong_FromLong(st);
 }
 
+// [rows, width] of the same type and size on the same device, rows contiguous; None: no such array, `at` NULL
+bool view_like(PyObject *o, const Tensor &like, eager_rows *r, const eager_rows **at)
+{
+    *at = nullptr;
+    if (o == Py_None) return true;
+    Tensor t;
+    if (!as_tensor(o, &t) || t.dims != 2 || t.type != like.type || t.device != like.device || t.size[0] != like.size[0] ||
+        t.size[1] != like.size[1] || (t.size[1] > 1 && t.stride[1] != 1))
+        return false;
+    // a lone row may have any stride
+    *r = {t.data, t.size[0] > 1 ? t.stride[0] : t.size[1]};
+    *at = r;
+    return true;
+}
+
+// a vector of the rows' type and width, or None
+bool gain_of(PyObject *o, const Tensor &like, void **data)
+{
+    *data = nullptr;
+    if (o == Py_None) return true;
+    Tensor t;
+    if (!as_tensor(o, &t) || !vector_of(t, like.type, like.device, like.size[1])) return false;
+    *data = t.data;
+    return true;
+}
+
+// layer_norm(x, residual, w, b, eps, s, y, stats); residual and s, and b, or None
+PyObject *py_layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Tensor x, stats;
+    eager_rows r[4];
+    const eager_rows *at[4];
+    void *w, *b, *stream;
+    int dtype;
+    float eps;
+    if (n != 8 || !t_f32 || !as_tensor(a[0], &x) || x.dims != 2 || !as_dtype(x, &dtype) || !view_like(a[0], x, &r[0], &at[0]) ||
+        !view_like(a[1], x, &r[1], &at[1]) || !gain_of(a[2], x, &w) || !gain_of(a[3], x, &b) || !as_float(a[4], &eps) ||
+        !view_like(a[5], x, &r[2], &at[2]) || !view_like(a[6], x, &r[3], &at[3]) || !as_tensor(a[7], &stats) ||
+        !table_of(stats, x.device, 2, x.size[0]) || !fits_int(x.size[1]) || !stream_of(x, &stream))
+        return other_form();
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = model.layer(dtype, x.size[0], static_cast<int32_t>(x.size[1]), at[0], at[1], w, b, eps, at[2], at[3],
+                     static_cast<float *>(stats.data), stream);
+    Py_END_ALLOW_THREADS
+    return st == EAGER_EINVAL ? other_form() : PyLong_FromLong(st);
+}
+
+// layer_norm_backward(dy, ds, s, w, stats, dx, dw, db); ds, dw, db or None
+PyObject *py_layer_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Tensor s, stats;
+    eager_rows r[4];
+    const eager_rows *at[4];
+    void *w, *dw, *db, *stream;
+    int dtype;
+    int64_t bytes;
+    Workspace space;
+    if (n != 8 || !t_f32 || !as_tensor(a[2], &s) || s.dims != 2 || !as_dtype(s, &dtype) || !view_like(a[0], s, &r[0], &at[0]) ||
+        !view_like(a[1], s, &r[1], &at[1]) || !view_like(a[2], s, &r[2], &at[2]) || !gain_of(a[3], s, &w) ||
+        !as_tensor(a[4], &stats) || !table_of(stats, s.device, 2, s.size[0]) || !view_like(a[5], s, &r[3], &at[3]) ||
+        !gain_of(a[6], s, &dw) || !gain_of(a[7], s, &db) || !fits_int(s.size[1]) || !stream_of(s, &stream) ||
+        model.layer_bytes(dtype, s.size[0], static_cast<int32_t>(s.size[1]), &bytes) != EAGER_OK || !space.take(bytes, a[2]))
+        return other_form();
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = model.layer_backward(dtype, s.size[0], static_cast<int32_t>(s.size[1]), at[0], at[1], at[2], w,
+                              static_cast<float *>(stats.data), at[3], dw, db, space.data, bytes, stream);
+    Py_END_ALLOW_THREADS
+    return st == EAGER_EINVAL ? other_form() : PyLong_FromLong(st);
+}
+
+// rotary(q, k, cos, sin, positions, interleaved, q_out, k_out, backward)
+PyObject *py_rotary(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Tensor q, k, c, s, pos, y[2];
+    eager_heads hq, hk, h[2];
+    int dtype;
+    void *stream;
+    if (n != 9 || !t_f32 || !as_tensor(a[0], &q) || !as_tensor(a[1], &k) || !as_tensor(a[2], &c) || !as_tensor(a[3], &s) ||
+        !as_tensor(a[4], &pos) || !PyBool_Check(a[5]) || !as_tensor(a[6], &y[0]) || !as_tensor(a[7], &y[1]) || !PyBool_Check(a[8]))
+        return other_form();
+    if (q.dims != 3 || k.dims != 3 || c.dims != 2 || !as_dtype(q, &dtype) || !heads_like(q, q, q.size[1], &hq) ||
+        !heads_like(k, q, k.size[1], &hk) || !heads_like(y[0], q, q.size[1], &h[0]) || !heads_like(y[1], q, k.size[1], &h[1]) ||
+        !table_of(c, q.device, c.size[0], c.size[1]) || !table_of(s, q.device, c.size[0], c.size[1]) ||
+        !vector_of(pos, t_i32, q.device, q.size[0]) || !fits_int(q.size[1]) || !fits_int(k.size[1]) || !fits_int(q.size[2]) ||
+        c.size[1] > INT_MAX / 2 || !stream_of(q, &stream))
+        return other_form();
+    const eager_packed shape = {q.size[0], static_cast<int32_t>(q.size[1]), static_cast<int32_t>(k.size[1]),
+                                static_cast<int32_t>(q.size[2]), 0, nullptr};
+    const eager_rotation rot = {static_cast<float *>(c.data), static_cast<float *>(s.data), static_cast<int32_t *>(pos.data),
+                                c.size[0]};
+    const auto call = a[8] == Py_True ? model.rotary_backward : model.rotary;
+    const int layout = a[5] == Py_True ? EAGER_ROTARY_INTERLEAVED : EAGER_ROTARY_HALVES;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = call(dtype, &shape, &hq, &hk, &rot, static_cast<int32_t>(2 * c.size[1]), layout, &h[0], &h[1], stream);
+    Py_END_ALLOW_THREADS
+    return st == EAGER_EINVAL ? other_form() : PyLong_FromLong(st);
+}
+
+// distillation(x, w, index, logits, temperature, loss, lse, picked) or
+// (x, w, index, logits, temperature, lse, picked, dloss, dx, dw), dx or dw None: not wanted
+PyObject *py_distillation(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Tensor x, w, index, logits, one, two, three, dx, dw;
+    int dtype;
+    int64_t bytes;
+    float temperature;
+    void *stream;
+    const bool backward = n == 10;
+    if ((n != 8 && n != 10) || !t_f32 || !as_tensor(a[0], &x) || !as_tensor(a[1], &w) || !as_tensor(a[2], &index) ||
+        !as_tensor(a[3], &logits) || !as_float(a[4], &temperature) || !as_tensor(a[5], &one) || !as_tensor(a[6], &two) ||
+        !as_tensor(a[7], &three))
+        return other_form();
+    // loss, lse, picked or lse, picked, dloss
+    const Tensor &picked = backward ? two : three, &last = backward ? three : two;
+    if (x.dims != 2 || w.dims != 2 || index.dims != 2 || !as_dtype(x, &dtype) || !rows_like(x, x) || !rows_like(w, w) ||
+        w.type != x.type || w.device != x.device || w.size[1] != x.size[1] || index.size[0] != x.size[0] ||
+        index.type != t_i64 || index.device != x.device || (index.size[1] > 1 && index.stride[1] != 1) ||
+        (index.size[0] > 1 && index.stride[0] != index.size[1]) || !table_of(logits, x.device, x.size[0], index.size[1]) ||
+        !table_of(picked, x.device, x.size[0], index.size[1]) || !vector_of(one, t_f32, x.device, x.size[0]) ||
+        !vector_of(last, t_f32, x.device, x.size[0]) || !fits_int(x.size[1]) || !fits_int(w.size[0]) || !fits_int(index.size[1]) ||
+        !stream_of(x, &stream))
+        return other_form();
+    dx.data = dw.data = nullptr;
+    if (backward && ((a[8] != Py_None && (!as_tensor(a[8], &dx) || !rows_like(dx, x))) ||
+                     (a[9] != Py_None && (!as_tensor(a[9], &dw) || !rows_like(dw, w)))))
+        return other_form();
+    const eager_projection shape = {x.size[0], static_cast<int32_t>(x.size[1]), static_cast<int32_t>(w.size[0]),
+                                    x.size[0] > 1 ? x.stride[0] : x.size[1], w.size[0] > 1 ? w.stride[0] : w.size[1]};
+    const eager_teacher teacher = {static_cast<int64_t *>(index.data), static_cast<float *>(logits.data),
+                                   static_cast<int32_t>(index.size[1]), temperature};
+    Workspace space;
+    if (model.taught_bytes(dtype, &shape, backward, &bytes) != EAGER_OK || !space.take(bytes, a[0])) return other_form();
+    float *p = static_cast<float *>(one.data), *q = static_cast<float *>(two.data), *r = static_cast<float *>(three.data);
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = backward ? model.taught_backward(dtype, &shape, x.data, w.data, &teacher, p, q, r, dx.data, dw.data, space.data, bytes, stream)
+                  : model.taught(dtype, &shape, x.data, w.data, &teacher, p, q, r, space.data, bytes, stream);
+    Py_END_ALLOW_THREADS
+    return st == EAGER_EINVAL ? other_form() : PyLong_FromLong(st);
+}
+
 // bind_model(addresses, (float32, bfloat16, int32, int64), workspace): workspace(n, like) gives a tensor
 PyObject *py_bind_model(PyObject *, PyObject *args)
 {
@@ -658,6 +810,10 @@ PyMethodDef methods[] = {
     {"qk_norm_rope", FAST(py_norm), nullptr},
     {"attention", FAST(py_attention), nullptr},
     {"cross_entropy", FAST(py_loss), nullptr},
+    {"layer_norm", FAST(py_layer_norm), nullptr},
+    {"layer_norm_backward", FAST(py_layer_norm_backward), nullptr},
+    {"rotary", FAST(py_rotary), nullptr},
+    {"distillation", FAST(py_distillation), nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -107,18 +107,17 @@ bool valid_projection(int dtype, const eager_projection *s)
            (s->vocab / 128 + 1ll) * (s->rows / 64 + 1) <= kMaxGrid && s->rows * (s->width / 8) / 128 < kMaxGrid;
 }
 
-bool fill(eager::CrossEntropyArgs &a, int dtype, const eager_projection *s, const void *x, const void *w,
-          const int64_t *target, void *workspace, int64_t workspace_bytes)
+bool fill(eager::CrossEntropyArgs &a, int dtype, const eager_projection *s, const void *x, const void *w, void *workspace,
+          int64_t workspace_bytes)
 {
     const int64_t c = chunk(dtype);
-    if (!valid_projection(dtype, s) || !aligned(w, 16) || (s->rows && (!aligned(x, 16) || !aligned(target, 8))) || !aligned(workspace, 16) ||
+    if (!valid_projection(dtype, s) || !aligned(w, 16) || (s->rows && !aligned(x, 16)) || !aligned(workspace, 16) ||
         s->x_stride < s->width || s->x_stride > kMaxStride || s->x_stride % c || s->w_stride < s->width ||
         s->w_stride > kMaxStride || s->w_stride % c)
         return false;
     a = {};
     a.x = x;
     a.w = w;
-    a.target = reinterpret_cast<const long long *>(target);
     a.workspace = static_cast<char *>(workspace);
     a.rows = s->rows;
     a.x_stride = s->x_stride;
@@ -126,6 +125,68 @@ bool fill(eager::CrossEntropyArgs &a, int dtype, const eager_projection *s, cons
     a.width = s->width;
     a.vocab = s->vocab;
     a.workspace_bytes = workspace_bytes;
+    return true;
+}
+
+// rows of one array: on 16 bytes, none shares elements with the next one
+bool valid_rows(const eager_rows *r, int dtype, int64_t rows, int32_t width)
+{
+    return r && (aligned(r->data, 16) || rows == 0) && r->stride >= width && r->stride <= kMaxStride && r->stride % chunk(dtype) == 0;
+}
+
+eager::Rows rows_of(const eager_rows *r) { return r ? eager::Rows{r->data, r->stride} : eager::Rows{}; }
+
+bool valid_norm(int dtype, int64_t rows, int32_t width)
+{
+    return valid_dtype(dtype) && rows >= 0 && rows <= kMaxTokens && width >= 8 && width <= EAGER_MAX_NORM_WIDTH && width % 8 == 0;
+}
+static_assert(eager::kNormWidth == EAGER_MAX_NORM_WIDTH, "the lanes of a workgroup hold the widest row");
+
+// forward and backward (sign -1) alike
+int rotate(int dtype, const eager_packed *s, const eager_heads *q, const eager_heads *k, const eager_rotation *r, int32_t part,
+           int layout, const eager_heads *q_out, const eager_heads *k_out, float sign, void *stream)
+{
+    const eager_heads *const x[2] = {q, k}, *const y[2] = {q_out, k_out};
+    if (!valid_dtype(dtype) || !valid_shape(s) || !r || !aligned(r->cos_table, 16) || !aligned(r->sin_table, 16) ||
+        !(aligned(r->positions, 4) || s->tokens == 0) || r->table_rows < 1 || part < 8 || part > s->head_dim || part % 8 ||
+        (layout != EAGER_ROTARY_HALVES && layout != EAGER_ROTARY_INTERLEAVED))
+        return EAGER_EINVAL;
+    for (int i = 0; i < 2; ++i)
+        if (!valid_heads(x[i], dtype, s) || !valid_heads(y[i], dtype, s)) return EAGER_EINVAL;
+    if (s->tokens == 0) return EAGER_OK;
+    eager::RotaryArgs a = {};
+    a.heads[0] = s->q_heads;
+    a.heads[1] = s->kv_heads;
+    for (int i = 0; i < 2; ++i) {
+        a.x[i] = heads(x[i]);
+        a.y[i] = heads(y[i]);
+        a.groups[i] = (a.heads[i] + eager::kTurnedHeads - 1) / eager::kTurnedHeads;
+        a.moved[i] = x[i]->data == y[i]->data ? part : s->head_dim;
+    }
+    a.cos_table = r->cos_table;
+    a.sin_table = r->sin_table;
+    a.positions = r->positions;
+    a.tokens = s->tokens;
+    a.table_rows = r->table_rows;
+    a.half = part / 2;
+    a.sign = sign;
+    return status_of(eager::launch_rotary(a, dtype == EAGER_BF16, layout == EAGER_ROTARY_INTERLEAVED, static_cast<hipStream_t>(stream)));
+}
+
+// The products' grids hold more rows than the lists' kernels, whose workgroups of 1024 threads take 16 each.
+constexpr int64_t kMaxTaught = 1 << 25;
+constexpr float kLeastTemperature = 0x1p-20f;
+
+bool taught(eager::CrossEntropyArgs &a, const eager_teacher *t, int64_t rows)
+{
+    if (!t || rows > kMaxTaught || t->entries < 1 || t->entries > EAGER_MAX_ENTRIES ||
+        !(t->temperature >= kLeastTemperature && t->temperature <= 1.0f / kLeastTemperature) ||
+        (rows && (!aligned(t->index, 8) || !aligned(t->logits, 4))))
+        return false;
+    a.teacher.index = reinterpret_cast<const long long *>(t->index);
+    a.teacher.logits = t->logits;
+    a.teacher.entries = t->entries;
+    a.teacher.temperature = t->temperature;
     return true;
 }
 
@@ -230,11 +291,12 @@ int eager_cross_entropy(int dtype, const eager_projection *shape, const void *x,
 {
     eager::CrossEntropyArgs a;
     int64_t need = 0;
-    if (!fill(a, dtype, shape, x, w, target, workspace, workspace_bytes) ||
-        (shape->rows && (!aligned(loss, 4) || !aligned(lse, 4))) ||
+    if (!fill(a, dtype, shape, x, w, workspace, workspace_bytes) ||
+        (shape->rows && (!aligned(target, 8) || !aligned(loss, 4) || !aligned(lse, 4))) ||
         eager_cross_entropy_workspace_bytes(dtype, shape, 0, &need) != EAGER_OK || workspace_bytes < need)
         return EAGER_EINVAL;
     if (a.rows == 0) return EAGER_OK;
+    a.target = reinterpret_cast<const long long *>(target);
     a.loss = loss;
     a.lse = lse;
     return status_of(eager::launch_cross_entropy(a, dtype == EAGER_BF16, static_cast<hipStream_t>(stream)));
@@ -246,16 +308,161 @@ int eager_cross_entropy_backward(int dtype, const eager_projection *shape, const
 {
     eager::CrossEntropyArgs a;
     int64_t need = 0;
-    if (!fill(a, dtype, shape, x, w, target, workspace, workspace_bytes) ||
-        (shape->rows && (!aligned(lse, 4) || !aligned(dloss, 4))) ||
+    if (!fill(a, dtype, shape, x, w, workspace, workspace_bytes) ||
+        (shape->rows && (!aligned(target, 8) || !aligned(lse, 4) || !aligned(dloss, 4))) ||
         (!dx && !dw && shape->rows) || (dx && !aligned(dx, 16)) || (dw && !aligned(dw, 16)) ||
         eager_cross_entropy_workspace_bytes(dtype, shape, 1, &need) != EAGER_OK || workspace_bytes < need)
         return EAGER_EINVAL;
+    a.target = reinterpret_cast<const long long *>(target);
     a.lse = const_cast<float *>(lse);
     a.dloss = dloss;
     a.dx = dx;
     a.dw = dw;
     return status_of(eager::launch_cross_entropy_backward(a, dtype == EAGER_BF16, static_cast<hipStream_t>(stream)));
+}
+
+int eager_distillation_workspace_bytes(int dtype, const eager_projection *shape, int backward, int64_t *bytes)
+{
+    if (!valid_projection(dtype, shape) || shape->rows > kMaxTaught || !bytes || (backward != 0 && backward != 1)) return EAGER_EINVAL;
+    *bytes = eager::distillation_workspace_bytes(shape->rows, shape->width, shape->vocab, dtype == EAGER_BF16, backward);
+    return EAGER_OK;
+}
+
+int eager_distillation(int dtype, const eager_projection *shape, const void *x, const void *w, const eager_teacher *teacher,
+                       float *loss, float *lse, float *picked, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    eager::CrossEntropyArgs a;
+    int64_t need = 0;
+    if (!fill(a, dtype, shape, x, w, workspace, workspace_bytes) || !taught(a, teacher, shape->rows) ||
+        (shape->rows && (!aligned(loss, 4) || !aligned(lse, 4) || !aligned(picked, 4))) ||
+        eager_distillation_workspace_bytes(dtype, shape, 0, &need) != EAGER_OK || workspace_bytes < need)
+        return EAGER_EINVAL;
+    if (a.rows == 0) return EAGER_OK;
+    a.loss = loss;
+    a.lse = lse;
+    a.teacher.picked = picked;
+    return status_of(eager::launch_cross_entropy(a, dtype == EAGER_BF16, static_cast<hipStream_t>(stream)));
+}
+
+int eager_distillation_backward(int dtype, const eager_projection *shape, const void *x, const void *w,
+                                const eager_teacher *teacher, const float *lse, const float *picked, const float *dloss, void *dx,
+                                void *dw, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    eager::CrossEntropyArgs a;
+    int64_t need = 0;
+    if (!fill(a, dtype, shape, x, w, workspace, workspace_bytes) || !taught(a, teacher, shape->rows) ||
+        (shape->rows && (!aligned(lse, 4) || !aligned(picked, 4) || !aligned(dloss, 4))) || (!dx && !dw && shape->rows) ||
+        (dx && !aligned(dx, 16)) || (dw && !aligned(dw, 16)) ||
+        eager_distillation_workspace_bytes(dtype, shape, 1, &need) != EAGER_OK || workspace_bytes < need)
+        return EAGER_EINVAL;
+    a.lse = const_cast<float *>(lse);
+    a.teacher.picked = const_cast<float *>(picked);
+    a.dloss = dloss;
+    a.dx = dx;
+    a.dw = dw;
+    return status_of(eager::launch_cross_entropy_backward(a, dtype == EAGER_BF16, static_cast<hipStream_t>(stream)));
+}
+
+int eager_layer_norm(int dtype, int64_t rows, int32_t width, const eager_rows *x, const eager_rows *residual, const void *w,
+                     const void *b, float eps, const eager_rows *sum, const eager_rows *y, float *stats, void *stream)
+{
+    if (!valid_norm(dtype, rows, width) || !valid_rows(x, dtype, rows, width) || !valid_rows(y, dtype, rows, width) ||
+        !residual != !sum || (residual && (!valid_rows(residual, dtype, rows, width) || !valid_rows(sum, dtype, rows, width))) ||
+        !aligned(w, 16) || (b && !aligned(b, 16)) || !(eps >= 0.0f) || !std::isfinite(eps) || !(aligned(stats, 4) || rows == 0) ||
+        (rows && sum && sum->data == y->data))
+        return EAGER_EINVAL;
+    if (rows == 0) return EAGER_OK;
+    eager::LayerNormArgs a = {};
+    a.x = rows_of(x);
+    a.residual = rows_of(residual);
+    a.sum = rows_of(sum);
+    a.y = rows_of(y);
+    a.w = w;
+    a.b = b;
+    a.stats = stats;
+    a.rows = rows;
+    a.width = width;
+    a.eps = eps;
+    a.inv_width = 1.0f / static_cast<float>(width);
+    return status_of(eager::launch_layer_norm(a, dtype == EAGER_BF16, static_cast<hipStream_t>(stream)));
+}
+
+int eager_layer_norm_workspace_bytes(int dtype, int64_t rows, int32_t width, int64_t *bytes)
+{
+    if (!valid_norm(dtype, rows, width) || !bytes) return EAGER_EINVAL;
+    *bytes = eager::layer_norm_workspace_bytes(rows, width);
+    return EAGER_OK;
+}
+
+int eager_layer_norm_backward(int dtype, int64_t rows, int32_t width, const eager_rows *dy, const eager_rows *ds,
+                              const eager_rows *s, const void *w, const float *stats, const eager_rows *dx, void *dw, void *db,
+                              void *workspace, int64_t workspace_bytes, void *stream)
+{
+    if (!valid_norm(dtype, rows, width) || !valid_rows(dy, dtype, rows, width) || (ds && !valid_rows(ds, dtype, rows, width)) ||
+        !valid_rows(s, dtype, rows, width) || !valid_rows(dx, dtype, rows, width) || !aligned(w, 16) ||
+        !(aligned(stats, 4) || rows == 0) || (dw && !aligned(dw, 4)) || (db && !aligned(db, 4)) || !aligned(workspace, 16) ||
+        workspace_bytes < eager::layer_norm_workspace_bytes(rows, width))
+        return EAGER_EINVAL;
+    eager::LayerNormArgs a = {};
+    a.x = rows_of(s);
+    a.residual = rows_of(ds);
+    a.sum = rows_of(dx);
+    a.y = rows_of(dy);
+    a.w = w;
+    a.dw = dw;
+    a.db = db;
+    a.stats = const_cast<float *>(stats);
+    a.partials = dw || db ? static_cast<float *>(workspace) : nullptr;
+    a.rows = rows;
+    a.width = width;
+    a.blocks = eager::layer_norm_blocks(rows, width);
+    a.inv_width = 1.0f / static_cast<float>(width);
+    return status_of(eager::launch_layer_norm_backward(a, dtype == EAGER_BF16, static_cast<hipStream_t>(stream)));
+}
+
+int eager_rotary_table(const eager_angles *t, float *cos_table, float *sin_table, void *stream)
+{
+    if (!t || t->positions < 0 || t->positions > kMaxTokens || t->part < 8 || t->part > EAGER_MAX_HEAD_DIM || t->part % 8 ||
+        t->scaling < EAGER_ANGLES_PLAIN || t->scaling > EAGER_ANGLES_PARTS || !(t->base >= 1.0) || !std::isfinite(t->base) ||
+        !std::isfinite(t->magnitude) || (t->positions && (!aligned(cos_table, 16) || !aligned(sin_table, 16))))
+        return EAGER_EINVAL;
+    if (t->scaling != EAGER_ANGLES_PLAIN && (!(t->factor >= 1.0) || !std::isfinite(t->factor))) return EAGER_EINVAL;
+    if (t->scaling == EAGER_ANGLES_PARTS && (!(t->original > 0.0) || !std::isfinite(t->original) || !(t->low >= 0.0) ||
+                                             !(t->high > t->low) || !std::isfinite(t->high)))
+        return EAGER_EINVAL;
+    if (t->positions == 0) return EAGER_OK;
+    constexpr double kPi = 3.14159265358979323846;
+    eager::TableArgs a = {};
+    const double n = t->part, stretched = t->scaling == EAGER_ANGLES_BASE ? t->base * std::pow(t->factor, n / (n - 2)) : t->base;
+    for (int i = 0; i < t->part / 2; ++i) {
+        double f = std::pow(stretched, -2.0 * i / n);
+        if (t->scaling == EAGER_ANGLES_LINEAR) f /= t->factor;
+        if (t->scaling == EAGER_ANGLES_PARTS) {
+            const double turns = t->original * f / (2 * kPi);
+            const double keep = std::fmin(std::fmax((turns - t->low) / (t->high - t->low), 0.0), 1.0);
+            f *= keep + (1 - keep) / t->factor;
+        }
+        a.quarters[i] = f * (2 / kPi);
+    }
+    a.magnitude = t->magnitude;
+    a.cos_table = cos_table;
+    a.sin_table = sin_table;
+    a.positions = t->positions;
+    a.half = t->part / 2;
+    return status_of(eager::launch_rotary_table(a, static_cast<hipStream_t>(stream)));
+}
+
+int eager_rotary(int dtype, const eager_packed *shape, const eager_heads *q, const eager_heads *k, const eager_rotation *rotation,
+                 int32_t part, int layout, const eager_heads *q_out, const eager_heads *k_out, void *stream)
+{
+    return rotate(dtype, shape, q, k, rotation, part, layout, q_out, k_out, 1.0f, stream);
+}
+
+int eager_rotary_backward(int dtype, const eager_packed *shape, const eager_heads *dq_out, const eager_heads *dk_out,
+                          const eager_rotation *rotation, int32_t part, int layout, const eager_heads *dq, const eager_heads *dk,
+                          void *stream)
+{
+    return rotate(dtype, shape, dq_out, dk_out, rotation, part, layout, dq, dk, -1.0f, stream);
 }
 
 }  // extern "C"

@@ -8,6 +8,7 @@ namespace eager {
 inline long long round_up(long long x, long long to) { return (x + to - 1) / to * to; }
 
 constexpr int kUnits = 256;      // compute units
+constexpr long long kMostBlocks = 1 << 20;       // of a grid whose workgroups go on in steps of it (threads stay below 2^32)
 // A quarter of a large tile takes this of its time (bound by shared memory: three reads for two matrix instructions).
 // Measured, three rounds of tiles and 32 more, the 32 whole or in quarters: 2048 rows, width 1024, bf16 135 and 125 us; 1600
 // 186 and 171; fp32 661 (of medium tiles) and 612, 1015 and 943.
@@ -154,6 +155,15 @@ inline long long cross_entropy_workspace_bytes(long long rows, int width, int vo
     return layout_of(cut_of(rows, width, vocab, bytes), rows, width, bytes).end;
 }
 
+// Distillation: the word that each row's teacher favours, in front of the forward pass's statistics and behind the backward
+// pass's arrays.
+inline long long teacher_target_bytes(long long rows) { return round_up(rows * 8, 256); }
+
+inline long long distillation_workspace_bytes(long long rows, int width, int vocab, bool bf16, bool backward)
+{
+    return cross_entropy_workspace_bytes(rows, width, vocab, bf16, backward) + teacher_target_bytes(rows);
+}
+
 // Heads a workgroup takes at a time: two a group of lanes with 4 lanes a head in the forward pass,
 // four in the backward pass, which keeps sums from turn to turn (8192 tokens of 20 heads of 64 in bf16:
 // forward 11.0 us, 12.6 with 256; backward 15.8 us, 20.6 with 128).
@@ -202,5 +212,30 @@ inline long long attention_workspace_bytes(long long tokens, int q_heads, int kv
     const int parts = attention_parts(tokens, q_heads, kv_heads, sequences);
     return 2 * attention_row_bytes(tokens, q_heads) + (parts > 1 ? parts * 2ll * kv_heads * tokens * dim * 4 : 0);
 }
+
+// Lanes that hold a row of a layer norm, 16 values each: 16 (four rows a wavefront), a wavefront or several.
+constexpr int kNormWidth = 16384;
+inline int layer_norm_threads(int width)
+{
+    if (width <= 256) return 16;
+    int threads = 64;
+    while (threads * 16 < width) threads *= 2;
+    return threads;
+}
+
+// Workgroups of its backward pass, and so records of the gains' gradients (2 width values each).
+inline int layer_norm_blocks(long long rows, int width)
+{
+    const int threads = layer_norm_threads(width), groups = std::max(256, threads) / threads;
+    return static_cast<int>(std::min((rows + groups - 1) / groups, 512ll));
+}
+
+inline long long layer_norm_workspace_bytes(long long rows, int width)
+{
+    return std::max(layer_norm_blocks(rows, width), 1) * 2ll * width * 4;
+}
+
+// Heads that one thread of a rotation takes one after the other, with the position's angles in its registers.
+constexpr int kTurnedHeads = 4;
 
 }  // namespace eager

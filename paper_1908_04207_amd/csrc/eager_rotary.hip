@@ -1,0 +1,151 @@
+// Rotation of query and key heads by position, and the table of its cosines and sines.
+//
+//   of a pair (a, b):  a' = a cos - b sin,  b' = b cos + a sin;  gradients: the same with -sin
+//
+// Pairs are i and i + half or 2 i and 2 i + 1 of the first 2 half elements of a head, the others are copied.  A thread
+// holds the cosines and sines of its place in a head and takes that place in several heads of its token, so that
+// their loads are under way together and the table is read once for them.  Bound by memory.
+#include "eager_launch.h"
+#include "eager_model.h"
+#include "eager_model_rules.h"
+#include "eager_vector.h"
+
+namespace eager {
+namespace {
+
+template <typename T, int V> struct Piece;
+template <> struct Piece<__bf16, 8> { typedef bf16x8 type; };
+template <> struct Piece<__bf16, 4> { typedef bf16x4 type; };
+template <> struct Piece<float, 4> { typedef f32x4 type; };
+
+// Places of a head: `turned` of them with 2 V elements of pairs i, i + half (Interleaved: V elements side by side), then
+// those with V elements that are copied.
+template <typename T, int V, bool Interleaved>
+__global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, int places, int turned)
+{
+    typedef typename Piece<T, V>::type vec;
+    constexpr int N = Interleaved ? V / 2 : V;              // pairs a place
+    typedef float angles __attribute__((ext_vector_type(N)));
+    const int units = (a.groups[0] + a.groups[1]) * places;
+    const int tokens = units < 256 ? 256 / units : 1;       // of a workgroup
+    const int mine = units < 256 ? threadIdx.x / units : 0;
+    if (mine >= tokens) return;
+    for (long long token = static_cast<long long>(blockIdx.x) * tokens + mine; token < a.tokens;
+         token += static_cast<long long>(gridDim.x) * tokens) {
+        const int pos = a.positions[token];
+        const bool known = pos >= 0 && pos < a.table_rows;
+        const long long o = static_cast<long long>(known ? pos : 0) * a.half;
+        for (int unit = threadIdx.x - mine * units; unit < units; unit += 256) {
+            int group = unit / places;
+            const int place = unit - group * places;
+            const int which = group >= a.groups[0];
+            if (which) group -= a.groups[0];
+            const int h0 = group * kTurnedHeads, heads = min(kTurnedHeads, a.heads[which] - h0);
+            const long long xh = a.x[which].head, yh = a.y[which].head;
+            const T *x = static_cast<const T *>(a.x[which].data) + token * a.x[which].row + h0 * xh;
+            T *y = static_cast<T *>(a.y[which].data) + token * a.y[which].row + h0 * yh;
+            vec p[kTurnedHeads], q[kTurnedHeads];
+            if (place >= turned) {
+                const int at = 2 * a.half + (place - turned) * V;
+                if (at >= a.moved[which]) continue;
+#pragma unroll
+                for (int h = 0; h < kTurnedHeads; ++h)
+                    if (h < heads) p[h] = *reinterpret_cast<const vec *>(x + h * xh + at);
+#pragma unroll
+                for (int h = 0; h < kTurnedHeads; ++h)
+                    if (h < heads) *reinterpret_cast<vec *>(y + h * yh + at) = p[h];
+                continue;
+            }
+            const int pair = place * N, first = Interleaved ? 2 * pair : pair;
+            angles c = *reinterpret_cast<const angles *>(a.cos_table + o + pair);
+            angles s = *reinterpret_cast<const angles *>(a.sin_table + o + pair);
+#pragma unroll
+            for (int h = 0; h < kTurnedHeads; ++h)
+                if (h < heads) {
+                    p[h] = *reinterpret_cast<const vec *>(x + h * xh + first);
+                    if (!Interleaved) q[h] = *reinterpret_cast<const vec *>(x + h * xh + first + a.half);
+                }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                c[i] = known ? c[i] : __builtin_nanf("");
+                s[i] *= a.sign;
+            }
+#pragma unroll
+            for (int h = 0; h < kTurnedHeads; ++h)
+                if (h < heads) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const float u = static_cast<float>(Interleaved ? p[h][2 * i] : p[h][i]);
+                        const float v = static_cast<float>(Interleaved ? p[h][2 * i + 1] : q[h][i]);
+                        const T left = static_cast<T>(fmaf(u, c[i], -(v * s[i]))), right = static_cast<T>(fmaf(v, c[i], u * s[i]));
+                        if (Interleaved) p[h][2 * i] = left, p[h][2 * i + 1] = right;
+                        else p[h][i] = left, q[h][i] = right;
+                    }
+                    *reinterpret_cast<vec *>(y + h * yh + first) = p[h];
+                    if (!Interleaved) *reinterpret_cast<vec *>(y + h * yh + first + a.half) = q[h];
+                }
+        }
+    }
+}
+
+template <typename T, int V, bool Interleaved>
+hipError_t enqueue(const RotaryArgs &a, hipStream_t stream)
+{
+    const int turned = a.half / (Interleaved ? V / 2 : V);
+    const int most = std::max(a.moved[0], a.moved[1]);
+    const int places = turned + (most - 2 * a.half) / V;
+    const int units = (a.groups[0] + a.groups[1]) * places, tokens = units < 256 ? 256 / units : 1;
+    return launch(rotary_kernel<T, V, Interleaved>, dim3(static_cast<unsigned>(std::min((a.tokens + tokens - 1) / tokens, kMostBlocks))),
+                  dim3(256), 0, stream, a, places, turned);
+}
+
+// Four pairs of a position a thread.  The angle in quarter turns, in 64 bits; what is beyond the nearest whole number
+// of them, at most an eighth of a turn, goes into the series of sine and cosine up to x^11 and x^10, which leave out
+// less than 7e-12 and 2e-10 (pi/4 to the 13th and 12th over the factorials), a hundredth of a rounding of the result.
+__global__ __launch_bounds__(256) void rotary_table_kernel(const TableArgs a)
+{
+    const int quads = a.half / 4, rows = 256 / quads;       // positions of a workgroup
+    const int mine = threadIdx.x / quads, first = (threadIdx.x - mine * quads) * 4;
+    if (mine >= rows) return;
+    double quarters_of[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) quarters_of[i] = a.quarters[first + i];
+    for (long long pos = static_cast<long long>(blockIdx.x) * rows + mine; pos < a.positions; pos += static_cast<long long>(gridDim.x) * rows) {
+        f32x4 c, s;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const double quarters = static_cast<double>(pos) * quarters_of[i], whole = rint(quarters);
+            const double x = (quarters - whole) * 1.5707963267948966, x2 = x * x;
+            const int n = static_cast<int>(static_cast<long long>(whole) & 3);
+            double sine = fma(x2, -1.0 / 39916800, 1.0 / 362880), cosine = fma(x2, -1.0 / 3628800, 1.0 / 40320);
+            sine = fma(x2, sine, -1.0 / 5040), cosine = fma(x2, cosine, -1.0 / 720);
+            sine = fma(x2, sine, 1.0 / 120), cosine = fma(x2, cosine, 1.0 / 24);
+            sine = fma(x2, sine, -1.0 / 6), cosine = fma(x2, cosine, -0.5);
+            sine = fma(x2 * x, sine, x), cosine = fma(x2, cosine, 1.0);
+            const double along = n & 1 ? sine : cosine, across = n & 1 ? cosine : sine;
+            c[i] = static_cast<float>((n == 1 || n == 2 ? -along : along) * a.magnitude);
+            s[i] = static_cast<float>((n & 2 ? -across : across) * a.magnitude);
+        }
+        *reinterpret_cast<f32x4 *>(a.cos_table + pos * a.half + first) = c;
+        *reinterpret_cast<f32x4 *>(a.sin_table + pos * a.half + first) = s;
+    }
+}
+
+}  // namespace
+
+// Places of 16 bytes; halves that are no multiple of 8 take 8 in bf16.
+hipError_t launch_rotary(const RotaryArgs &a, bool bf16, bool interleaved, hipStream_t stream)
+{
+    if (!bf16) return interleaved ? enqueue<float, 4, true>(a, stream) : enqueue<float, 4, false>(a, stream);
+    if (interleaved) return enqueue<__bf16, 8, true>(a, stream);
+    return a.half % 8 == 0 ? enqueue<__bf16, 8, false>(a, stream) : enqueue<__bf16, 4, false>(a, stream);
+}
+
+hipError_t launch_rotary_table(const TableArgs &a, hipStream_t stream)
+{
+    const int rows = 256 / (a.half / 4);
+    return launch(rotary_table_kernel, dim3(static_cast<unsigned>(std::min((a.positions + rows - 1) / rows, kMostBlocks))), dim3(256), 0,
+                  stream, a);
+}
+
+}  // namespace eager
