@@ -38,6 +38,7 @@ __device__ __forceinline__ float2 group_sums(float2 x, float2 *part)
 }
 
 template <int Threads> constexpr int kBlock = Threads < 256 ? 256 : Threads;
+template <int Threads> constexpr int kBackwardBlock = Threads < kNormBackwardBlock ? kNormBackwardBlock : Threads;
 
 template <typename T, int Threads, int C>
 __global__ __launch_bounds__(kBlock<Threads>) void layer_norm_kernel(const LayerNormArgs a)
@@ -103,16 +104,19 @@ __global__ __launch_bounds__(kBlock<Threads>) void layer_norm_kernel(const Layer
 
 // a.x: s, a.y: dy, a.residual: ds, a.sum: dx
 template <typename T, int Threads, int C>
-__global__ __launch_bounds__(kBlock<Threads>) void layer_norm_backward_kernel(const LayerNormArgs a)
+__global__ __launch_bounds__(kBackwardBlock<Threads>) void layer_norm_backward_kernel(const LayerNormArgs a)
 {
-    constexpr int E = kVector<T>, Groups = kBlock<Threads> / Threads;
+    constexpr int E = kVector<T>, Block = kBackwardBlock<Threads>, Groups = Block / Threads;
     typedef typename Vector<T>::type vec;
     __shared__ float2 part[2][16];
-    __shared__ float sums[Groups > 1 ? 2 * Threads * C * E : 1];
+    __shared__ __align__(16) float sums[Groups > 1 ? Groups : 1][Groups > 1 ? Threads * C * E : 4];
     const int lane = threadIdx.x % Threads, group = threadIdx.x / Threads;
+    // the next row is under way while one is worked on
     vec w[C] = {}, s[C], g[C], d[C];
-    float gain[C][E], bias[C][E];
+    float gain[C][E], bias[C][E], next_mean, next_r;
     auto fetch = [&](long long row) {
+        next_mean = row < a.rows ? a.stats[row] : 0.0f;
+        next_r = row < a.rows ? a.stats[a.rows + row] : 0.0f;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int at = (c * Threads + lane) * E;
@@ -137,7 +141,7 @@ __global__ __launch_bounds__(kBlock<Threads>) void layer_norm_backward_kernel(co
     // as many turns for every group of the workgroup
     for (long long first = static_cast<long long>(blockIdx.x) * Groups; first < a.rows; first += step, row += step, turn ^= 1) {
         const bool live = row < a.rows;
-        const float mean = live ? a.stats[row] : 0.0f, r = live ? a.stats[a.rows + row] : 0.0f;
+        const float mean = next_mean, r = next_r;
         float n[C][E], dn[C][E];
         vec rest[C];
         float2 both = make_float2(0.0f, 0.0f);
@@ -171,23 +175,24 @@ __global__ __launch_bounds__(kBlock<Threads>) void layer_norm_backward_kernel(co
     if (!a.partials) return;
     float *out = a.partials + static_cast<long long>(blockIdx.x) * 2 * a.width;
     if (Groups > 1) {
-        constexpr int Columns = Threads * C * E;
-        for (int turns = 0; turns < Groups; ++turns) {
-            if (group == turns) {
+        // one sum after the other, so that shared memory holds those of all groups
 #pragma unroll
-                for (int c = 0; c < C; ++c)
+        for (int which = 0; which < 2; ++which) {
+            if (which) __syncthreads();
 #pragma unroll
-                    for (int i = 0; i < E; ++i) {
-                        const int at = (c * Threads + lane) * E + i;
-                        sums[at] = turns ? sums[at] + gain[c][i] : gain[c][i];
-                        sums[Columns + at] = turns ? sums[Columns + at] + bias[c][i] : bias[c][i];
-                    }
-            }
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < E; i += 4) {
+                    const float *x = (which ? bias[c] : gain[c]) + i;
+                    *reinterpret_cast<f32x4 *>(&sums[group][(c * Threads + lane) * E + i]) = f32x4{x[0], x[1], x[2], x[3]};
+                }
             __syncthreads();
-        }
-        for (int at = threadIdx.x; at < a.width; at += kBlock<Threads>) {
-            out[at] = sums[at];
-            out[a.width + at] = sums[Columns + at];
+            for (int at = threadIdx.x; at < a.width; at += Block) {
+                float sum = sums[0][at];
+#pragma unroll
+                for (int g = 1; g < Groups; ++g) sum += sums[g][at];
+                out[which * a.width + at] = sum;
+            }
         }
         return;
     }
@@ -235,7 +240,7 @@ hipError_t enqueue(const LayerNormArgs &a, bool backward, hipStream_t stream)
         return launch(layer_norm_kernel<T, Threads, C>, dim3(static_cast<unsigned>(std::min((a.rows + Groups - 1) / Groups, kMostBlocks))),
                       dim3(kBlock<Threads>), 0, stream, a);
     hipError_t e = hipSuccess;
-    if (a.blocks) e = launch(layer_norm_backward_kernel<T, Threads, C>, dim3(a.blocks), dim3(kBlock<Threads>), 0, stream, a);
+    if (a.blocks) e = launch(layer_norm_backward_kernel<T, Threads, C>, dim3(a.blocks), dim3(kBackwardBlock<Threads>), 0, stream, a);
     if (e != hipSuccess || !a.partials) return e;
     return launch(layer_norm_columns_kernel<T>, dim3((a.width + 15) / 16, a.db ? 2 : 1), dim3(1024), 0, stream, a);
 }

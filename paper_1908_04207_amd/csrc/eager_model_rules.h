@@ -223,11 +223,15 @@ inline int layer_norm_threads(int width)
     return threads;
 }
 
-// Workgroups of its backward pass, and so records of the gains' gradients (2 width values each).
+// Threads of a workgroup of its backward pass (more where a row takes more), and workgroups: one a compute unit, each of
+// which leaves 2 width sums.  Measured, both kernels, 256 and 512 workgroups: 8192 x 1024 bf16 19.1 and 23.6 us, 2047 x 8192
+// 33.3 and 41.9, 20011 x 1600 fp32 102 and 105, 65536 x 64 bf16 15.0 and 14.0; 256 threads and 512 workgroups 19.3 us, 37.4, 113;
+// 1024 threads spill (47.2, 88.3, 338).
+constexpr int kNormBackwardBlock = 512;
 inline int layer_norm_blocks(long long rows, int width)
 {
-    const int threads = layer_norm_threads(width), groups = std::max(256, threads) / threads;
-    return static_cast<int>(std::min((rows + groups - 1) / groups, 512ll));
+    const int groups = std::max(kNormBackwardBlock / layer_norm_threads(width), 1);
+    return static_cast<int>(std::min<long long>((rows + groups - 1) / groups, kUnits));
 }
 
 inline long long layer_norm_workspace_bytes(long long rows, int width)
@@ -235,7 +239,12 @@ inline long long layer_norm_workspace_bytes(long long rows, int width)
     return std::max(layer_norm_blocks(rows, width), 1) * 2ll * width * 4;
 }
 
-// Heads that one thread of a rotation takes one after the other, with the position's angles in its registers.
-constexpr int kTurnedHeads = 4;
+// Heads that one thread of a rotation takes one after the other, with the position's angles in its registers.  Measured, 1,
+// 2, 4 and 5 of them, us: 8192 tokens of 16 + 4 heads of 64 in bf16, half of each rotated 13.5, 10.5, 10.4, 11.0; 20011 of 25 + 25
+// in fp32 97, 101, 106, 106; 61 of 16 + 4 in bf16 3.8, 4.0, 4.6, 5.2; 16384 of 8 + 2 of 128 23.0, 18.8, 18.5, 19.6.
+constexpr int kTurnedHeads = 2;
+
+// Workgroups of its table, each with several positions: 131072 positions of 64 pairs 15.7 us, 17.7 with one each.
+constexpr long long kTableBlocks = 2048;
 
 }  // namespace eager

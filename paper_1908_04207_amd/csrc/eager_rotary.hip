@@ -18,13 +18,15 @@ template <> struct Piece<__bf16, 8> { typedef bf16x8 type; };
 template <> struct Piece<__bf16, 4> { typedef bf16x4 type; };
 template <> struct Piece<float, 4> { typedef f32x4 type; };
 
-// Places of a head: `turned` of them with 2 V elements of pairs i, i + half (Interleaved: V elements side by side), then
-// those with V elements that are copied.
+// Places of a head: `turned` of them with V elements and their partners (Interleaved: V elements, partners among them),
+// then those of as many elements that are copied.  A wavefront has places of both kinds; they differ in what becomes of
+// the loaded values alone.
 template <typename T, int V, bool Interleaved>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, int places, int turned)
 {
     typedef typename Piece<T, V>::type vec;
     constexpr int N = Interleaved ? V / 2 : V;              // pairs a place
+    constexpr int Pieces = Interleaved ? 1 : 2;
     typedef float angles __attribute__((ext_vector_type(N)));
     const int units = (a.groups[0] + a.groups[1]) * places;
     const int tokens = units < 256 ? 256 / units : 1;       // of a workgroup
@@ -33,46 +35,38 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, int pla
     for (long long token = static_cast<long long>(blockIdx.x) * tokens + mine; token < a.tokens;
          token += static_cast<long long>(gridDim.x) * tokens) {
         const int pos = a.positions[token];
-        const bool known = pos >= 0 && pos < a.table_rows;
-        const long long o = static_cast<long long>(known ? pos : 0) * a.half;
         for (int unit = threadIdx.x - mine * units; unit < units; unit += 256) {
             int group = unit / places;
             const int place = unit - group * places;
-            const int which = group >= a.groups[0];
+            const bool which = group >= a.groups[0], turns = place < turned;
             if (which) group -= a.groups[0];
-            const int h0 = group * kTurnedHeads, heads = min(kTurnedHeads, a.heads[which] - h0);
-            const long long xh = a.x[which].head, yh = a.y[which].head;
-            const T *x = static_cast<const T *>(a.x[which].data) + token * a.x[which].row + h0 * xh;
-            T *y = static_cast<T *>(a.y[which].data) + token * a.y[which].row + h0 * yh;
+            const int moved = which ? a.moved[1] : a.moved[0];
+            const int first = turns ? place * V : 2 * a.half + (place - turned) * Pieces * V, second = first + (turns ? a.half : V);
+            if (first >= moved) continue;
+            const bool both = Pieces == 2 && second < moved;
+            const int h0 = group * kTurnedHeads, heads = min(kTurnedHeads, (which ? a.heads[1] : a.heads[0]) - h0);
+            const Heads from = which ? a.x[1] : a.x[0], to = which ? a.y[1] : a.y[0];
+            const T *x = static_cast<const T *>(from.data) + token * from.row + h0 * from.head;
+            T *y = static_cast<T *>(to.data) + token * to.row + h0 * to.head;
             vec p[kTurnedHeads], q[kTurnedHeads];
-            if (place >= turned) {
-                const int at = 2 * a.half + (place - turned) * V;
-                if (at >= a.moved[which]) continue;
-#pragma unroll
-                for (int h = 0; h < kTurnedHeads; ++h)
-                    if (h < heads) p[h] = *reinterpret_cast<const vec *>(x + h * xh + at);
-#pragma unroll
-                for (int h = 0; h < kTurnedHeads; ++h)
-                    if (h < heads) *reinterpret_cast<vec *>(y + h * yh + at) = p[h];
-                continue;
-            }
-            const int pair = place * N, first = Interleaved ? 2 * pair : pair;
-            angles c = *reinterpret_cast<const angles *>(a.cos_table + o + pair);
-            angles s = *reinterpret_cast<const angles *>(a.sin_table + o + pair);
 #pragma unroll
             for (int h = 0; h < kTurnedHeads; ++h)
                 if (h < heads) {
-                    p[h] = *reinterpret_cast<const vec *>(x + h * xh + first);
-                    if (!Interleaved) q[h] = *reinterpret_cast<const vec *>(x + h * xh + first + a.half);
+                    p[h] = *reinterpret_cast<const vec *>(x + h * from.head + first);
+                    if (both) q[h] = *reinterpret_cast<const vec *>(x + h * from.head + second);
+                }
+            if (turns) {
+                const bool known = pos >= 0 && pos < a.table_rows;
+                const long long o = static_cast<long long>(known ? pos : 0) * a.half + place * N;
+                angles c = *reinterpret_cast<const angles *>(a.cos_table + o);
+                angles s = *reinterpret_cast<const angles *>(a.sin_table + o);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    c[i] = known ? c[i] : __builtin_nanf("");
+                    s[i] *= a.sign;
                 }
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                c[i] = known ? c[i] : __builtin_nanf("");
-                s[i] *= a.sign;
-            }
-#pragma unroll
-            for (int h = 0; h < kTurnedHeads; ++h)
-                if (h < heads) {
+                for (int h = 0; h < kTurnedHeads; ++h) {
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
                         const float u = static_cast<float>(Interleaved ? p[h][2 * i] : p[h][i]);
@@ -81,8 +75,13 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, int pla
                         if (Interleaved) p[h][2 * i] = left, p[h][2 * i + 1] = right;
                         else p[h][i] = left, q[h][i] = right;
                     }
-                    *reinterpret_cast<vec *>(y + h * yh + first) = p[h];
-                    if (!Interleaved) *reinterpret_cast<vec *>(y + h * yh + first + a.half) = q[h];
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < kTurnedHeads; ++h)
+                if (h < heads) {
+                    *reinterpret_cast<vec *>(y + h * to.head + first) = p[h];
+                    if (both) *reinterpret_cast<vec *>(y + h * to.head + second) = q[h];
                 }
         }
     }
@@ -93,7 +92,7 @@ hipError_t enqueue(const RotaryArgs &a, hipStream_t stream)
 {
     const int turned = a.half / (Interleaved ? V / 2 : V);
     const int most = std::max(a.moved[0], a.moved[1]);
-    const int places = turned + (most - 2 * a.half) / V;
+    const int places = turned + (most - 2 * a.half + (Interleaved ? V : 2 * V) - 1) / (Interleaved ? V : 2 * V);
     const int units = (a.groups[0] + a.groups[1]) * places, tokens = units < 256 ? 256 / units : 1;
     return launch(rotary_kernel<T, V, Interleaved>, dim3(static_cast<unsigned>(std::min((a.tokens + tokens - 1) / tokens, kMostBlocks))),
                   dim3(256), 0, stream, a, places, turned);
@@ -114,9 +113,10 @@ __global__ __launch_bounds__(256) void rotary_table_kernel(const TableArgs a)
         f32x4 c, s;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const double quarters = static_cast<double>(pos) * quarters_of[i], whole = rint(quarters);
-            const double x = (quarters - whole) * 1.5707963267948966, x2 = x * x;
-            const int n = static_cast<int>(static_cast<long long>(whole) & 3);
+            // (adding 1.5 2^52 leaves the nearest whole number in the last bits)
+            const double quarters = static_cast<double>(pos) * quarters_of[i], shifted = quarters + 0x1.8p52;
+            const int n = __double2loint(shifted) & 3;
+            const double x = (quarters - (shifted - 0x1.8p52)) * 1.5707963267948966, x2 = x * x;
             double sine = fma(x2, -1.0 / 39916800, 1.0 / 362880), cosine = fma(x2, -1.0 / 3628800, 1.0 / 40320);
             sine = fma(x2, sine, -1.0 / 5040), cosine = fma(x2, cosine, -1.0 / 720);
             sine = fma(x2, sine, 1.0 / 120), cosine = fma(x2, cosine, 1.0 / 24);
@@ -144,7 +144,7 @@ hipError_t launch_rotary(const RotaryArgs &a, bool bf16, bool interleaved, hipSt
 hipError_t launch_rotary_table(const TableArgs &a, hipStream_t stream)
 {
     const int rows = 256 / (a.half / 4);
-    return launch(rotary_table_kernel, dim3(static_cast<unsigned>(std::min((a.positions + rows - 1) / rows, kMostBlocks))), dim3(256), 0,
+    return launch(rotary_table_kernel, dim3(static_cast<unsigned>(std::min((a.positions + rows - 1) / rows, kTableBlocks))), dim3(256), 0,
                   stream, a);
 }
 
