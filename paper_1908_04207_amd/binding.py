@@ -205,7 +205,7 @@ class _CtypesOnly:
 
     plan_participation = plan_quorum = round = step = stash = views = _unknown
     qk_norm_rope = attention = cross_entropy = _unknown
-    layer_norm = layer_norm_backward = rotary = distillation = _unknown
+    layer_norm = layer_norm_backward = rotary_table = rotary = distillation = _unknown
 
     @staticmethod
     def streams(*_):

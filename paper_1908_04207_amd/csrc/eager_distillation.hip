@@ -17,23 +17,26 @@
 #include "eager_model_rules.h"
 #include "eager_vector.h"
 
+#include <type_traits>
+
 namespace eager {
 namespace {
 
-constexpr int kEntries = 256, kOfLane = kEntries / 64;
+constexpr int kEntries = 256;
 
 __device__ __forceinline__ bool counts(long long index, float logit) { return (index >= 0) & (logit != -__builtin_inff()); }
 
-// A row's entries, kOfLane a lane of a wavefront.
+// A row's entries, N a lane of a wavefront.
+template <int N>
 struct List {
-    long long index[kOfLane];
-    float logit[kOfLane];
-    bool used[kOfLane];
+    long long index[N];
+    float logit[N];
+    bool used[N];
 
     __device__ __forceinline__ List(const TeacherArgs &t, long long row, int lane)
     {
 #pragma unroll
-        for (int j = 0; j < kOfLane; ++j) {
+        for (int j = 0; j < N; ++j) {
             const int k = 64 * j + lane;
             index[j] = k < t.entries ? t.index[row * t.entries + k] : -1;
             logit[j] = k < t.entries ? t.logits[row * t.entries + k] : 0.0f;
@@ -45,7 +48,7 @@ struct List {
     {
         float t = -__builtin_inff();
 #pragma unroll
-        for (int j = 0; j < kOfLane; ++j) t = used[j] ? fmaxf(t, logit[j]) : t;
+        for (int j = 0; j < N; ++j) t = used[j] ? fmaxf(t, logit[j]) : t;
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) t = fmaxf(t, __shfl_xor(t, m, 64));
         return t;
@@ -60,7 +63,7 @@ struct List {
         int at = 1 << 30;
         bool beyond = false;
 #pragma unroll
-        for (int j = 0; j < kOfLane; ++j) {
+        for (int j = 0; j < N; ++j) {
             if (!used[j]) continue;
             beyond |= index[j] >= vocab;
             const int rank = 64 * j + lane + (logit[j] == t ? 0 : 1 << 20);
@@ -76,97 +79,110 @@ struct List {
     }
 };
 
-// Four sums over a wavefront at once: after two steps a lane holds a quarter of the lanes' sum of one of them.
-// Sum i is in the lanes whose last two bits are i.
-__device__ __forceinline__ float four_sums(const float (&x)[4], int lane)
+// N sums over a wavefront at once: in the first steps a lane hands one half of its sums on and keeps the other's, so
+// sum i ends in the lanes whose last bits are i.
+template <int N, int M = 1>
+__device__ __forceinline__ float sums_apart(const float (&x)[N], int lane)
 {
-    const bool odd = lane & 1, upper = lane & 2;
-    const float a = (odd ? x[1] : x[0]) + __shfl_xor(odd ? x[0] : x[1], 1, 64);
-    const float b = (odd ? x[3] : x[2]) + __shfl_xor(odd ? x[2] : x[3], 1, 64);
-    float c = (upper ? b : a) + __shfl_xor(upper ? a : b, 2, 64);
+    if constexpr (N == 1) {
+        float c = x[0];
 #pragma unroll
-    for (int m = 4; m < 64; m *= 2) c += __shfl_xor(c, m, 64);
-    return c;
+        for (int m = M; m < 64; m *= 2) c += __shfl_xor(c, m, 64);
+        return c;
+    } else {
+        float half[N / 2];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) half[i] = (lane & M ? x[2 * i + 1] : x[2 * i]) + __shfl_xor(lane & M ? x[2 * i] : x[2 * i + 1], M, 64);
+        return sums_apart<N / 2, 2 * M>(half, lane);
+    }
 }
 
-// One row a workgroup, four entries a wavefront at a time.
-template <typename T>
+constexpr int kPicked = 4;
+
+// One row a workgroup, kPicked entries a wavefront at a time.
+template <typename T, int N>
 __global__ __launch_bounds__(256) void picked_kernel(const CrossEntropyArgs a, long long *favourite)
 {
     constexpr int E = kVector<T>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), entries = a.teacher.entries;
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        if (wave == 0) {
-            const long long word = List(a.teacher, row, lane).favourite(a.vocab, lane);
+        if (wave == 3) {
+            const long long word = List<N>(a.teacher, row, lane).favourite(a.vocab, lane);
             if (lane == 0) favourite[row] = word;
         }
         const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
-        for (int e0 = 4 * wave; e0 < entries; e0 += 16) {
-            const T *w[4];
-            float sum[4] = {};
+        for (int e0 = kPicked * wave; e0 < entries; e0 += 4 * kPicked) {
+            const T *w[kPicked];
+            float sum[kPicked] = {};
             long long mine = -1;
             bool used = false;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < kPicked; ++j) {
                 const int k = min(e0 + j, entries - 1);
                 const long long index = a.teacher.index[row * entries + k];
                 const bool there = counts(index, a.teacher.logits[row * entries + k]);
-                if ((lane & 3) == j) mine = index, used = there;
+                if ((lane & (kPicked - 1)) == j) mine = index, used = there;
                 w[j] = static_cast<const T *>(a.w) + (there && index < a.vocab ? index : 0) * a.w_stride;
             }
             for (int at = lane * E; at < a.width; at += 64 * E) {
                 const auto u = load16(x + at);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < kPicked; ++j) {
                     const auto v = load16(w[j] + at);
 #pragma unroll
                     for (int i = 0; i < E; ++i) sum[j] = fmaf(static_cast<float>(u[i]), static_cast<float>(v[i]), sum[j]);
                 }
             }
-            const float all = four_sums(sum, lane);
-            if (lane < 4 && e0 + lane < entries)
+            const float all = sums_apart(sum, lane);
+            if (lane < kPicked && e0 + lane < entries)
                 a.teacher.picked[row * entries + e0 + lane] = !used ? 0.0f : mine < a.vocab ? all : __builtin_nanf("");
         }
     }
 }
 
 // Four rows a workgroup.
+template <int N>
 __global__ __launch_bounds__(256) void favourites_kernel(const CrossEntropyArgs a, long long *favourite)
 {
     const int lane = threadIdx.x & 63;
     for (long long row = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6); row < a.rows; row += 4ll * gridDim.x) {
-        const long long word = List(a.teacher, row, lane).favourite(a.vocab, lane);
+        const long long word = List<N>(a.teacher, row, lane).favourite(a.vocab, lane);
         if (lane == 0) favourite[row] = word;
     }
 }
 
-// kJoined rows a workgroup: their statistics, then a wavefront for each row's entries.
+// kJoined rows a workgroup: their statistics, then a wavefront for each row's entries (whose loads come first).
+template <int N>
 __global__ __launch_bounds__(1024) void divergence_kernel(const CrossEntropyArgs a, const float2 *stats, const float *right,
                                                           const long long *favourite, int tiles, float scale)
 {
     __shared__ float2 part[16][kJoined];
     __shared__ float tops[kJoined], logs[kJoined];
-    const float2 all = joined_statistics(stats, a.rows, tiles, part);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long row = static_cast<long long>(blockIdx.x) * kJoined + wave, there = min(row, a.rows - 1);
+    const List<N> list(a.teacher, there, lane);
+    const long long word = favourite[there];
+    const float its = right[there];
+    float l[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) l[j] = list.used[j] ? a.teacher.picked[there * a.teacher.entries + 64 * j + lane] : 0.0f;
+    const float2 all = joined_statistics(stats, a.rows, tiles, part);
     if (threadIdx.x < kJoined) {
-        const long long row = static_cast<long long>(blockIdx.x) * kJoined + threadIdx.x;
+        const long long mine = static_cast<long long>(blockIdx.x) * kJoined + threadIdx.x;
         const float log_sum = log1pf(all.y - 1.0f);
         tops[threadIdx.x] = all.x, logs[threadIdx.x] = log_sum;
-        if (row < a.rows) a.lse[row] = fmaf(all.x, kLn2, log_sum);
+        if (mine < a.rows) a.lse[mine] = fmaf(all.x, kLn2, log_sum);
     }
     __syncthreads();
-    const long long row = static_cast<long long>(blockIdx.x) * kJoined + wave;
     if (row >= a.rows) return;
-    const long long word = favourite[row];
     if (word < 0 || word >= a.vocab) {
         if (lane == 0) a.loss[row] = word < 0 ? 0.0f : __builtin_nanf("");
         return;
     }
-    const List list(a.teacher, row, lane);
-    const float top = list.top(), its = right[row];
-    float sum = 0.0f, e[kOfLane], distance[kOfLane], loss = 0.0f;
+    const float top = list.top();
+    float sum = 0.0f, e[N], distance[N], loss = 0.0f;
 #pragma unroll
-    for (int j = 0; j < kOfLane; ++j) {
+    for (int j = 0; j < N; ++j) {
         // logarithms to base two, of q without its sum
         distance[j] = list.used[j] ? (list.logit[j] - top) * scale : 0.0f;
         e[j] = list.used[j] ? exp2_fast(distance[j]) : 0.0f;
@@ -175,10 +191,9 @@ __global__ __launch_bounds__(1024) void divergence_kernel(const CrossEntropyArgs
     sum = lanes_sum<64>(sum);
     const float log_q = log1pf(sum - 1.0f);
 #pragma unroll
-    for (int j = 0; j < kOfLane; ++j) {
+    for (int j = 0; j < N; ++j) {
         if (!list.used[j]) continue;
-        const float l = list.index[j] == word ? its : a.teacher.picked[row * a.teacher.entries + 64 * j + lane];
-        const float apart = distance[j] - fmaf(l, scale, -tops[wave]);
+        const float apart = distance[j] - fmaf(list.index[j] == word ? its : l[j], scale, -tops[wave]);
         const float term = e[j] / sum * (fmaf(apart, kLn2, logs[wave]) - log_q);
         loss += e[j] == 0.0f ? 0.0f : term;
     }
@@ -186,60 +201,67 @@ __global__ __launch_bounds__(1024) void divergence_kernel(const CrossEntropyArgs
     if (lane == 0) a.loss[row] = loss;
 }
 
-// kJoined rows a workgroup, a wavefront for each row's entries.
-template <typename T>
+// kJoined rows a workgroup, a wavefront for each row's entries (whose loads come first).
+template <typename T, int N>
 __global__ __launch_bounds__(1024) void entries_kernel(const CrossEntropyArgs a, const Entries n)
 {
     __shared__ float part[16][kJoined], apart[kJoined];
-    __shared__ int words[kJoined][kEntries];
-    __shared__ float shares[kJoined][kEntries];
+    __shared__ int words[kJoined][64 * N];
+    __shared__ float shares[kJoined][64 * N];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long row = static_cast<long long>(blockIdx.x) * kJoined + wave, there = min(row, a.rows - 1);
+    const int place = row < a.rows ? n.place[there] : -1;
+    const List<N> list(a.teacher, there, lane);
+    float p[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) p[j] = list.used[j] ? a.teacher.picked[there * a.teacher.entries + 64 * j + lane] : 0.0f;
     if (n.others) {
-        const long long row = static_cast<long long>(blockIdx.x) * kJoined + threadIdx.x % kJoined;
-        const float sum = joined_sums(n.others, row < a.rows ? n.place[row] : -1, a.rows, n.tiles, part);
+        const long long mine = static_cast<long long>(blockIdx.x) * kJoined + threadIdx.x % kJoined;
+        const float sum = joined_sums(n.others, mine < a.rows ? n.place[mine] : -1, a.rows, n.tiles, part);
         if (threadIdx.x < kJoined) apart[threadIdx.x] = sum;
         __syncthreads();
     }
-    const long long row = static_cast<long long>(blockIdx.x) * kJoined + wave;
-    const int place = row < a.rows ? n.place[row] : -1;
     if (place < 0) return;
     const long long word = n.favourite[place];
     if (word >= a.vocab) return;                         // the tiles wrote NaN
-    const List list(a.teacher, row, lane);
-    const float top = list.top();
-    float sum = 0.0f, q[kOfLane];
+    const float top = list.top(), lse = n.lse[place] * kLog2e, by = n.dloss[place];
+    float sum = 0.0f, q[N];
 #pragma unroll
-    for (int j = 0; j < kOfLane; ++j) {
+    for (int j = 0; j < N; ++j) {
         q[j] = list.used[j] ? exp2_fast((list.logit[j] - top) * n.scale) : 0.0f;
         sum += q[j];
     }
     sum = lanes_sum<64>(sum);
     float rest = 0.0f;                                   // of q, without the favourite's
 #pragma unroll
-    for (int j = 0; j < kOfLane; ++j) {
-        const int k = 64 * j + lane;
+    for (int j = 0; j < N; ++j) {
         q[j] /= sum;
         if (list.used[j] && list.index[j] != word) rest += q[j];
-        words[wave][k] = list.used[j] ? static_cast<int>(list.index[j]) : -1;
-        shares[wave][k] = q[j];
+        words[wave][64 * j + lane] = list.used[j] ? static_cast<int>(list.index[j]) : -1;
+        shares[wave][64 * j + lane] = q[j];
     }
     rest = lanes_sum<64>(rest);
     __builtin_amdgcn_wave_barrier();
-    const float lse = n.lse[place] * kLog2e, by = n.dloss[place];
+    // a word that stands in several entries is written by the first of them, with all their shares
+    float share[N] = {};
+    bool first[N];
 #pragma unroll
-    for (int j = 0; j < kOfLane; ++j) {
-        const int k = 64 * j + lane;
-        if (!list.used[j] || list.index[j] < n.first || list.index[j] >= n.first + n.live) continue;
-        // a word that stands in several entries is written by the first of them
-        float share = 0.0f;
-        bool first = true;
-        for (int i = 0; i < a.teacher.entries; ++i) {
-            const bool same = words[wave][i] == list.index[j];
-            share += same ? shares[wave][i] : 0.0f;
-            first &= !(same && i < k);
+    for (int j = 0; j < N; ++j) first[j] = list.used[j] && list.index[j] >= n.first && list.index[j] < n.first + n.live;
+#pragma unroll 4
+    for (int i = 0; i < a.teacher.entries; ++i) {
+        const int word_i = words[wave][i];
+        const float share_i = shares[wave][i];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const bool same = list.used[j] && word_i == static_cast<int>(list.index[j]);
+            share[j] += same ? share_i : 0.0f;
+            first[j] &= !(same && i < 64 * j + lane);
         }
-        if (!first) continue;
-        float d = exp2_fast(fmaf(a.teacher.picked[row * a.teacher.entries + k], n.scale, -lse)) - share;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if (!first[j]) continue;
+        float d = exp2_fast(fmaf(p[j], n.scale, -lse)) - share[j];
         if (n.others && list.index[j] == word && apart[wave] < 0.5f) d = rest - apart[wave];
         static_cast<T *>(n.dl)[place * n.stride + list.index[j] - n.first] = static_cast<T>(d * by);
     }
@@ -247,29 +269,47 @@ __global__ __launch_bounds__(1024) void entries_kernel(const CrossEntropyArgs a,
 
 unsigned workgroups(long long rows, int each) { return static_cast<unsigned>(std::min((rows + each - 1) / each, kMostBlocks)); }
 
+// Entries a lane: lists of up to 64, 128 and 256.
+template <typename F>
+hipError_t by_entries(int entries, const F &call)
+{
+    static_assert(kEntries == 256, "four entries a lane at most");
+    if (entries <= 64) return call(std::integral_constant<int, 1>());
+    if (entries <= 128) return call(std::integral_constant<int, 2>());
+    return call(std::integral_constant<int, 4>());
+}
+
 }  // namespace
 
 hipError_t launch_picked(const CrossEntropyArgs &a, long long *favourite, bool bf16, hipStream_t stream)
 {
-    return launch(bf16 ? picked_kernel<__bf16> : picked_kernel<float>, dim3(workgroups(a.rows, 1)), dim3(256), 0, stream, a, favourite);
+    return by_entries(a.teacher.entries, [&](auto n) {
+        return launch(bf16 ? picked_kernel<__bf16, n> : picked_kernel<float, n>, dim3(workgroups(a.rows, 1)), dim3(256), 0, stream, a, favourite);
+    });
 }
 
 hipError_t launch_favourites(const CrossEntropyArgs &a, long long *favourite, hipStream_t stream)
 {
-    return launch(favourites_kernel, dim3(workgroups(a.rows, 4)), dim3(256), 0, stream, a, favourite);
+    return by_entries(a.teacher.entries, [&](auto n) {
+        return launch(favourites_kernel<n>, dim3(workgroups(a.rows, 4)), dim3(256), 0, stream, a, favourite);
+    });
 }
 
 hipError_t launch_divergence(const CrossEntropyArgs &a, const float2 *stats, const float *right, const long long *favourite,
                              int tiles, float scale, hipStream_t stream)
 {
-    return launch(divergence_kernel, dim3(static_cast<unsigned>((a.rows + kJoined - 1) / kJoined)), dim3(1024), 0, stream, a, stats,
-                  right, favourite, tiles, scale);
+    return by_entries(a.teacher.entries, [&](auto n) {
+        return launch(divergence_kernel<n>, dim3(static_cast<unsigned>((a.rows + kJoined - 1) / kJoined)), dim3(1024), 0, stream, a,
+                      stats, right, favourite, tiles, scale);
+    });
 }
 
 hipError_t launch_entries(const CrossEntropyArgs &a, const Entries &n, bool bf16, hipStream_t stream)
 {
-    return launch(bf16 ? entries_kernel<__bf16> : entries_kernel<float>, dim3(static_cast<unsigned>((a.rows + kJoined - 1) / kJoined)),
-                  dim3(1024), 0, stream, a, n);
+    return by_entries(a.teacher.entries, [&](auto each) {
+        return launch(bf16 ? entries_kernel<__bf16, each> : entries_kernel<float, each>,
+                      dim3(static_cast<unsigned>((a.rows + kJoined - 1) / kJoined)), dim3(1024), 0, stream, a, n);
+    });
 }
 
 }  // namespace eager

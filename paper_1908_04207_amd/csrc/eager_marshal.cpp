@@ -348,6 +348,7 @@ struct ModelEntry {
     decltype(&eager_layer_norm) layer;
     decltype(&eager_layer_norm_workspace_bytes) layer_bytes;
     decltype(&eager_layer_norm_backward) layer_backward;
+    decltype(&eager_rotary_table) table;
     decltype(&eager_rotary) rotary;
     decltype(&eager_rotary_backward) rotary_backward;
     decltype(&eager_distillation) taught;
@@ -658,6 +659,33 @@ PyObject *py_layer_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     return st == EAGER_EINVAL ? other_form() : PyLong_FromLong(st);
 }
 
+// rotary_table(positions, part, scaling, base, factor, original, low, high, magnitude, cos, sin)
+PyObject *py_rotary_table(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Tensor c, s;
+    double v[6];
+    void *stream;
+    if (n != 11 || !t_f32 || !PyLong_CheckExact(a[0]) || !PyLong_CheckExact(a[1]) || !PyLong_CheckExact(a[2])) return other_form();
+    for (int i = 0; i < 6; ++i) {
+        if (!PyFloat_Check(a[3 + i]) && !PyLong_CheckExact(a[3 + i])) return other_form();
+        v[i] = PyFloat_AsDouble(a[3 + i]);
+        if (v[i] == -1.0 && PyErr_Occurred()) return other_form();
+    }
+    int over = 0;
+    const long long positions = PyLong_AsLongLongAndOverflow(a[0], &over);
+    int over_part = 0, over_scaling = 0;
+    const long part = PyLong_AsLongAndOverflow(a[1], &over_part), scaling = PyLong_AsLongAndOverflow(a[2], &over_scaling);
+    if (over || over_part || over_scaling || !fits_int(part) || !fits_int(scaling) || !as_tensor(a[9], &c) || !as_tensor(a[10], &s) ||
+        !table_of(c, c.device, positions, part / 2) || !table_of(s, c.device, positions, part / 2) || !stream_of(c, &stream))
+        return other_form();
+    const eager_angles t = {positions, static_cast<int32_t>(part), static_cast<int32_t>(scaling), v[0], v[1], v[2], v[3], v[4], v[5]};
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = model.table(&t, static_cast<float *>(c.data), static_cast<float *>(s.data), stream);
+    Py_END_ALLOW_THREADS
+    return st == EAGER_EINVAL ? other_form() : PyLong_FromLong(st);
+}
+
 // rotary(q, k, cos, sin, positions, interleaved, q_out, k_out, backward)
 PyObject *py_rotary(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -812,6 +840,7 @@ PyMethodDef methods[] = {
     {"cross_entropy", FAST(py_loss), nullptr},
     {"layer_norm", FAST(py_layer_norm), nullptr},
     {"layer_norm_backward", FAST(py_layer_norm_backward), nullptr},
+    {"rotary_table", FAST(py_rotary_table), nullptr},
     {"rotary", FAST(py_rotary), nullptr},
     {"distillation", FAST(py_distillation), nullptr},
     {nullptr, nullptr, 0, nullptr}};

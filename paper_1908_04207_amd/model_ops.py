@@ -57,14 +57,19 @@ def _expect(t, shape, dtype, device, name, contiguous=True):
 
 
 def _workspace(nbytes: int, like):
-    return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=like.device)
+    return like.new_empty(max(nbytes, 16), dtype=torch.uint8)
+
+
+def _result(like):
+    """A contiguous tensor of the same shape and type (in a third of the time of torch.empty with both named)."""
+    return torch.empty_like(like, memory_format=torch.contiguous_format)
 
 
 eb._marshal.bind_model(tuple(ctypes.cast(getattr(eb.lib, f), ctypes.c_void_p).value for f in (
     "eager_qk_norm_rope", "eager_qk_norm_rope_workspace_bytes", "eager_qk_norm_rope_backward",
     "eager_attention", "eager_attention_workspace_bytes", "eager_attention_backward",
     "eager_cross_entropy", "eager_cross_entropy_workspace_bytes", "eager_cross_entropy_backward",
-    "eager_layer_norm", "eager_layer_norm_workspace_bytes", "eager_layer_norm_backward", "eager_rotary",
+    "eager_layer_norm", "eager_layer_norm_workspace_bytes", "eager_layer_norm_backward", "eager_rotary_table", "eager_rotary",
     "eager_rotary_backward", "eager_distillation", "eager_distillation_workspace_bytes", "eager_distillation_backward")),
     (torch.float32, torch.bfloat16, torch.int32, torch.int64), _workspace)
 
@@ -368,12 +373,12 @@ def layer_norm(x, w, b=None, eps: float = 1e-5, residual=None, s=None, y=None):
     """Layer norm of the rows of s = x + residual [rows, width] (of x, without one), with gain w and bias b (or none)
     [width]: y, s (x itself without a residual) and stats, fp32 [2, rows]: means and inverse deviations.  s and y may
     each be x or residual, but not the same one."""
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None else y
+    y = _result(x) if y is None else y
     if residual is not None and s is None:
-        s = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        s = _result(x)
     if x.dim() != 2:
         _refuse(f"expected rows [rows, width], got {tuple(x.shape)}")
-    stats = torch.empty((2, x.shape[0]), dtype=torch.float32, device=x.device)
+    stats = x.new_empty((2, x.shape[0]), dtype=torch.float32)
     if _taken(eb._marshal.layer_norm(x, residual, w, b, eps, s, y, stats), "eager_layer_norm"):
         return y, x if residual is None else s, stats
     if residual is None and s is not None:
@@ -392,7 +397,7 @@ def layer_norm(x, w, b=None, eps: float = 1e-5, residual=None, s=None, y=None):
 def layer_norm_backward(dy, s, w, stats, ds=None, dx=None, dw=None, db=None, want=(True, True)):
     """Gradients dx (of x and of the residual alike), dw, db from those of y and, where the sum s is used elsewhere,
     of s.  want: whether dw and db are formed.  dx may be dy or ds."""
-    dx = torch.empty(s.shape, dtype=s.dtype, device=s.device) if dx is None else dx
+    dx = _result(s) if dx is None else dx
     dw = torch.empty_like(w) if dw is None and want[0] else dw
     db = torch.empty_like(w) if db is None and want[1] else db
     if _taken(eb._marshal.layer_norm_backward(dy, ds, s, w, stats, dx, dw, db), "eager_layer_norm_backward"):
@@ -470,7 +475,10 @@ def rotary_table(positions: int, part: int, base: float = 10000.0, scaling: str 
         _refuse(f"expected a number of positions and of rotated elements, got {positions}, {part}")
     shape = (positions, part // 2)
     cos = torch.empty(shape, dtype=torch.float32, device=device) if cos is None else cos
-    sin = torch.empty(shape, dtype=torch.float32, device=cos.device) if sin is None else sin
+    sin = torch.empty_like(cos) if sin is None else sin
+    if _taken(eb._marshal.rotary_table(positions, part, _SCALINGS[scaling], base, factor, original, low, high, magnitude, cos, sin),
+              "eager_rotary_table"):
+        return cos, sin
     for t, name in ((cos, "cos"), (sin, "sin")):
         _expect(t, shape, torch.float32, cos.device, name)
     if not cos.is_cuda:
@@ -504,8 +512,8 @@ def rotary(q, k, cos, sin, positions, interleaved: bool = False, q_out=None, k_o
     k [tokens, kv_heads, head_dim] turned by the angles of `positions` (int32 [tokens]) in the tables cos, sin (fp32
     [positions, part / 2]); the others as they are.  Pairs are the elements i and i + part / 2, or 2 i and 2 i + 1
     (interleaved).  q_out, k_out may be q, k."""
-    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
-    k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
+    q_out = _result(q) if q_out is None else q_out
+    k_out = _result(k) if k_out is None else k_out
     if not _taken(eb._marshal.rotary(q, k, cos, sin, positions, bool(interleaved), q_out, k_out, False), "eager_rotary"):
         _rotate("rotary", eb.eager_rotary, q, k, cos, sin, positions, interleaved, q_out, k_out, ("q_out", "k_out"))
     return q_out, k_out
@@ -513,8 +521,8 @@ def rotary(q, k, cos, sin, positions, interleaved: bool = False, q_out=None, k_o
 
 def rotary_backward(dq_out, dk_out, cos, sin, positions, interleaved: bool = False, dq=None, dk=None):
     """Gradients dq, dk from those of the outputs: turned back.  dq, dk may be dq_out, dk_out."""
-    dq = torch.empty(dq_out.shape, dtype=dq_out.dtype, device=dq_out.device) if dq is None else dq
-    dk = torch.empty(dk_out.shape, dtype=dk_out.dtype, device=dk_out.device) if dk is None else dk
+    dq = _result(dq_out) if dq is None else dq
+    dk = _result(dk_out) if dk is None else dk
     if not _taken(eb._marshal.rotary(dq_out, dk_out, cos, sin, positions, bool(interleaved), dq, dk, True), "eager_rotary_backward"):
         _rotate("rotary_backward", eb.eager_rotary_backward, dq_out, dk_out, cos, sin, positions, interleaved, dq, dk, ("dq", "dk"))
     return dq, dk
@@ -552,9 +560,8 @@ def distillation(x, w, index, logits, temperature: float = 1.0):
     teacher's `logits` (fp32 [rows, entries]); negative words count nothing, and a row without any has loss 0.  Also the
     log-sum-exps of x w^T / temperature and the student's logits of the entries (fp32 [rows, entries]).  The loss is not
     multiplied by the temperature's square."""
-    loss = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
-    lse = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
-    picked = torch.empty(index.shape, dtype=torch.float32, device=x.device)
+    loss = x.new_empty(x.shape[0], dtype=torch.float32)
+    lse, picked = torch.empty_like(loss), _result(logits)
     if _taken(eb._marshal.distillation(x, w, index, logits, temperature, loss, lse, picked), "eager_distillation"):
         return loss, lse, picked
     dtype = _dtype(x, w)
