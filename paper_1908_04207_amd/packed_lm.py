@@ -11,19 +11,21 @@ padding, and compute the gradients of a decoder-only transformer
     loss = cross entropy of rms(x) Whead, the last token of a sentence masked
 
 with `model_ops` for head norms, attention and loss and plain matrix products in between (application code,
-in torch).  Every process's gradients are accumulated straight into its arena, where the partial
+in torch).  A model may have layer norms with gains and biases in the place of rms, and the rotation of a part of every
+head in that of head norms and rotation (`Model.layer_norm`, `Model.rotary_part`); a student learns from the top logits
+that a trained teacher gives for its batches (`Teacher`) in the place of the sentences' own next words.  Every process's gradients are accumulated straight into its arena, where the partial
 allreduce reads them: one bucket per tensor, fp32 or bf16 gradients, fp32 parameters.
 
 Time is simulated: a process needs time in proportion to what its batch costs, tokens times
 parameters plus pairs of tokens inside a sentence, and the round is triggered as in `hyperplane`.
 
-    python -m paper_1908_04207_amd.packed_lm [--steps N] [--bf16]
+    python -m paper_1908_04207_amd.packed_lm [--steps N] [--bf16] [--layer-norm] [--distill]
 """
 from __future__ import annotations
 
 import math
 import random
-from dataclasses import dataclass, field
+from dataclasses import dataclass, field, replace
 from typing import Callable, List, Optional
 
 from . import binding as eb
@@ -39,15 +41,23 @@ class Model:
     head_dim: int = 64
     ffn: int = 512
     positions: int = 256
+    layer_norm: bool = False        # gains and biases for the norms of the hidden states, which are rms otherwise
+    rotary_part: int = 0            # elements of a head that are rotated, without head norms; 0: head norms and rotation
 
     def tensors(self):
         """Names and shapes in the order of the arena."""
         qkv = (self.q_heads + 2 * self.kv_heads) * self.head_dim
         t = [("embedding", (self.vocab, self.width))]
         for n in range(self.layers):
-            t += [(f"h{n}.qkv", (qkv, self.width)), (f"h{n}.q_gain", (self.head_dim,)), (f"h{n}.k_gain", (self.head_dim,)),
-                  (f"h{n}.out", (self.width, self.q_heads * self.head_dim)), (f"h{n}.fc1", (self.ffn, self.width)),
+            if self.layer_norm:
+                t += [(f"h{n}.{which}{part}", (self.width,)) for which in ("norm1", "norm2") for part in (".gain", ".bias")]
+            t.append((f"h{n}.qkv", (qkv, self.width)))
+            if not self.rotary_part:
+                t += [(f"h{n}.q_gain", (self.head_dim,)), (f"h{n}.k_gain", (self.head_dim,))]
+            t += [(f"h{n}.out", (self.width, self.q_heads * self.head_dim)), (f"h{n}.fc1", (self.ffn, self.width)),
                   (f"h{n}.fc2", (self.width, self.ffn))]
+        if self.layer_norm:
+            t += [("norm.gain", (self.width,)), ("norm.bias", (self.width,))]
         return t + [("head", (self.vocab, self.width))]
 
     def layout(self):
@@ -71,22 +81,80 @@ def _rms(x):
     return (x.float() * torch.rsqrt(x.float().square().mean(-1, keepdim=True) + 1e-6)).to(x.dtype)
 
 
-def loss_of(model: Model, weights, tokens, targets, lens_cu, positions, cos, sin):
-    """Losses of all tokens of a packed batch.  weights: name -> tensor (as in Model.tensors)."""
-    import torch
+def hidden_of(model: Model, weights, tokens, lens_cu, positions, cos, sin):
+    """Hidden states of a packed batch, as the projection onto the vocabulary takes them.  weights: name -> tensor (as in
+    Model.tensors)."""
     import torch.nn.functional as F
     from . import model_ops as ops
     m = model
-    T, sizes = tokens.numel(), (m.q_heads * m.head_dim, m.kv_heads * m.head_dim, m.kv_heads * m.head_dim)
+    T = tokens.numel()
+
+    def heads(n, y):
+        q, k, v = (t.view(T, -1, m.head_dim) for t in (y @ weights[f"h{n}.qkv"].t()).split(
+            (m.q_heads * m.head_dim, m.kv_heads * m.head_dim, m.kv_heads * m.head_dim), dim=1))
+        if m.rotary_part:
+            q, k = ops.Rotary.apply(q, k, cos, sin, positions, False)
+        else:
+            q, k = ops.QKNormRope.apply(q, k, weights[f"h{n}.q_gain"], weights[f"h{n}.k_gain"], cos, sin, positions, 1e-6)
+        return ops.Attention.apply(q, k, v, lens_cu, None).reshape(T, -1) @ weights[f"h{n}.out"].t()
+
+    def feed_forward(n, y):
+        return F.gelu(y @ weights[f"h{n}.fc1"].t()) @ weights[f"h{n}.fc2"].t()
+
     x = weights["embedding"][tokens]
+    if not m.layer_norm:
+        for n in range(m.layers):
+            x = x + heads(n, _rms(x))
+            x = x + feed_forward(n, _rms(x))
+        return _rms(x)
+
+    def norm(name):
+        return weights[name + ".gain"], weights[name + ".bias"], 1e-5
+
+    # a norm takes the sum before it along
+    y = ops.LayerNorm.apply(x, *norm("h0.norm1" if m.layers else "norm"))
     for n in range(m.layers):
-        qkv = _rms(x) @ weights[f"h{n}.qkv"].t()
-        q, k, v = (t.view(T, -1, m.head_dim) for t in torch.split(qkv, sizes, dim=1))
-        q, k = ops.QKNormRope.apply(q, k, weights[f"h{n}.q_gain"], weights[f"h{n}.k_gain"], cos, sin, positions, 1e-6)
-        a = ops.Attention.apply(q, k, v, lens_cu, None)
-        x = x + a.reshape(T, -1) @ weights[f"h{n}.out"].t()
-        x = x + F.gelu(_rms(x) @ weights[f"h{n}.fc1"].t()) @ weights[f"h{n}.fc2"].t()
-    return ops.CrossEntropy.apply(_rms(x), weights["head"], targets)
+        x, y = ops.AddLayerNorm.apply(heads(n, y), x, *norm(f"h{n}.norm2"))
+        x, y = ops.AddLayerNorm.apply(feed_forward(n, y), x, *norm(f"h{n + 1}.norm1" if n + 1 < m.layers else "norm"))
+    return y
+
+
+def loss_of(model: Model, weights, tokens, targets, lens_cu, positions, cos, sin):
+    """Losses of all tokens of a packed batch.  weights: name -> tensor (as in Model.tensors)."""
+    from . import model_ops as ops
+    return ops.CrossEntropy.apply(hidden_of(model, weights, tokens, lens_cu, positions, cos, sin), weights["head"], targets)
+
+
+@dataclass(frozen=True)
+class Teacher:
+    """A trained model whose top logits a student learns from."""
+    model: Model
+    weights: object                 # its flat arena, as Result.weights
+    entries: int = 16
+    temperature: float = 2.0
+
+    def lists(self, tokens, targets, lens_cu, positions, dtype):
+        """The words of its largest logits and these, for every token of a packed batch; none where a target is masked."""
+        import torch
+        views = views_of(self.model, self.weights.to(dtype))
+        with torch.no_grad():
+            y = hidden_of(self.model, views, tokens, lens_cu, positions, *rotation_table(self.model))
+            logits, index = (y @ views["head"].t()).float().topk(self.entries, dim=1)
+        return torch.where((targets >= 0)[:, None], index, -1), logits
+
+    def loss(self, model, weights, tokens, targets, lens_cu, positions, cos, sin):
+        """Divergences of a student of `model` and `weights`, times the temperature, which their gradients of logits are
+        divided by."""
+        from . import model_ops as ops
+        index, logits = self.lists(tokens, targets, lens_cu, positions, weights["head"].dtype)
+        y = hidden_of(model, weights, tokens, lens_cu, positions, cos, sin)
+        return ops.Distillation.apply(y, weights["head"], index, logits, self.temperature) * self.temperature
+
+
+def views_of(model: Model, arena):
+    """name -> view of a flat arena."""
+    off, num, _ = model.layout()
+    return {name: arena[o:o + n].view(shape) for (name, shape), o, n in zip(model.tensors(), off, num)}
 
 
 class Batches:
@@ -128,10 +196,14 @@ class Result:
     sim_ms: float = 0.0
     nap_mean: float = 0.0
     loss: List[float] = field(default_factory=list)       # mean loss of a token over all processes, per step
+    weights: object = None                                # the parameters' flat arena after the last step
 
 
 def rotation_table(model: Model):
     import torch
+    if model.rotary_part:
+        from . import model_ops
+        return model_ops.rotary_table(model.positions, model.rotary_part)
     angle = torch.arange(model.positions, dtype=torch.float64)[:, None] * 10000.0 ** (
         -torch.arange(0, model.head_dim, 2, dtype=torch.float64) / model.head_dim)
     return angle.cos().float().cuda(), angle.sin().float().cuda()
@@ -139,8 +211,8 @@ def rotation_table(model: Model):
 
 def train(mode: str = "majority", steps: int = 60, P: int = 4, model: Model = Model(), sentences: int = 24,
           mean: float = 40.0, spread: float = 0.8, lr: float = 0.3, mu: float = 0.9, bf16: bool = False,
-          seed: int = 1908, on_round: Optional[Callable] = None) -> Result:
-    """mode: "solo", "majority" or "sync" (ordinary synchronous SGD).  on_round(step, plan, grads, w, v), if
+          seed: int = 1908, on_round: Optional[Callable] = None, teacher: Optional[Teacher] = None) -> Result:
+    """mode: "solo", "majority" or "sync" (ordinary synchronous SGD).  teacher: whose logits the losses are taken from.  on_round(step, plan, grads, w, v), if
     given, is called after every round with the device tensors, and once before the first with step -1 and no
     plan."""
     import torch
@@ -151,7 +223,7 @@ def train(mode: str = "majority", steps: int = 60, P: int = 4, model: Model = Mo
     gen = torch.Generator(device="cuda").manual_seed(seed)
     for (name, shape), o, n in zip(model.tensors(), off, num):
         if len(shape) == 1:
-            w[o:o + n] = 1.0
+            w[o:o + n] = 0.0 if name.endswith(".bias") else 1.0
         else:
             w[o:o + n] = torch.randn(n, device="cuda", generator=gen) * (1.0 if name == "embedding" else shape[1] ** -0.5)
     G = [torch.zeros(arena, dtype=dtype, device="cuda") for _ in range(P)]
@@ -173,7 +245,7 @@ def train(mode: str = "majority", steps: int = 60, P: int = 4, model: Model = Mo
             for (name, shape), o, n in zip(model.tensors(), off, num):
                 weights[name] = now[o:o + n].view(shape).detach().requires_grad_()
                 weights[name].grad = G[p][o:o + n].view(shape)       # autograd adds into the arena
-            each = loss_of(model, weights, tokens, targets, cu, positions, cos, sin)
+            each = (teacher.loss if teacher else loss_of)(model, weights, tokens, targets, cu, positions, cos, sin)
             value = each.sum() / (targets >= 0).sum()
             value.backward()
             losses.append(value.detach())
@@ -189,6 +261,7 @@ def train(mode: str = "majority", steps: int = 60, P: int = 4, model: Model = Mo
             on_round(t, plan, G, w, v)
         res.loss.append(float(torch.stack(losses).mean()))
     res.nap_mean = nap / steps
+    res.weights = w
     ctx.close()
     return res
 
@@ -198,11 +271,19 @@ def main() -> None:
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
     ap.add_argument("--steps", type=int, default=60)
     ap.add_argument("--bf16", action="store_true", help="bf16 weights, activations and gradients, fp32 parameters")
+    ap.add_argument("--layer-norm", action="store_true", help="layer norms with gains and biases, half of every head rotated")
+    ap.add_argument("--distill", action="store_true", help="then a student of half the width learns from each run's model")
     a = ap.parse_args()
-    runs = {m: train(m, a.steps, bf16=a.bf16) for m in ("sync", "majority", "solo")}
+    model = Model(layer_norm=True, rotary_part=32) if a.layer_norm else Model()
+    runs = {m: train(m, a.steps, model=model, bf16=a.bf16) for m in ("sync", "majority", "solo")}
     for m, r in runs.items():
         print(f"{m:9s} NAP {r.nap_mean:4.2f}  simulated {r.sim_ms:8.0f} ms ({runs['sync'].sim_ms / r.sim_ms:.2f}x "
               f"synchronous)  loss {r.loss[0]:.3f} -> {sum(r.loss[-5:]) / 5:.3f}")
+    if a.distill:
+        student = replace(model, width=model.width // 2, ffn=model.ffn // 2)
+        for m, r in runs.items():
+            s = train(m, a.steps, model=student, lr=0.1, bf16=a.bf16, teacher=Teacher(model, r.weights))
+            print(f"{m:9s} student of its model  divergence {s.loss[0]:.3f} -> {sum(s.loss[-5:]) / 5:.3f}")
 
 
 if __name__ == "__main__":
