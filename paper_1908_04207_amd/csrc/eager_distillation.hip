@@ -49,9 +49,7 @@ struct List {
         float t = -__builtin_inff();
 #pragma unroll
         for (int j = 0; j < N; ++j) t = used[j] ? fmaxf(t, logit[j]) : t;
-#pragma unroll
-        for (int m = 1; m < 64; m *= 2) t = fmaxf(t, __shfl_xor(t, m, 64));
-        return t;
+        return wave_max(t);
     }
 
     // the word of the largest logit (the first of equal ones; any where none is a number), -1: no entry counts, vocab: an
@@ -69,12 +67,10 @@ struct List {
             const int rank = 64 * j + lane + (logit[j] == t ? 0 : 1 << 20);
             if (rank < at) at = rank, word = index[j];
         }
-#pragma unroll
-        for (int m = 1; m < 64; m *= 2) {
-            const int other = __shfl_xor(at, m, 64);
-            const long long its = __shfl_xor(word, m, 64);
-            if (other < at) at = other, word = its;
-        }
+        // (ranks are whole numbers below 2^24 but for a missing one's, so fp32 holds them)
+        const float best = -wave_max(-static_cast<float>(at));
+        const unsigned long long who = __ballot(static_cast<float>(at) == best);
+        word = __shfl(word, __builtin_ctzll(who), 64);
         return __any(beyond) ? vocab : word;
     }
 };

@@ -28,9 +28,29 @@ __device__ __forceinline__ float moved(float x)
     return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), Control, 0xf, 0xf, false));
 }
 
+// x of the two rows of 16 of a half, and of the two halves of a wavefront, by exchanging rows and halves between two registers.  (Results
+// by way of integers: a cast of the second one itself gives the first.)
+struct Both {
+    float first, second;
+};
+__device__ __forceinline__ Both exchange_rows(float x)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const unsigned even = r[0], odd = r[1];
+    return {__builtin_bit_cast(float, even), __builtin_bit_cast(float, odd)};
+}
+__device__ __forceinline__ Both exchange_halves(float x)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const unsigned low = r[0], high = r[1];
+    return {__builtin_bit_cast(float, low), __builtin_bit_cast(float, high)};
+}
+
 // The sum over `Lanes` neighbouring lanes (16 or 64), the same bits in each of them: pairs, quads, halves and rows of
-// 16 inside the vector unit, rows and halves of the wavefront by exchanging them between two registers.  (Through shared
-// memory's permutation, as __shfl_xor goes, a step takes some 60 clocks and not 8.)
+// 16 inside the vector unit, then rows and halves of the wavefront.  (Through shared memory's permutation, as
+// __shfl_xor goes, a step takes some 60 clocks and not 8.)
 template <int Lanes>
 __device__ __forceinline__ float lanes_sum(float x)
 {
@@ -40,15 +60,19 @@ __device__ __forceinline__ float lanes_sum(float x)
     x += moved<0x141>(x);       // 7 - i
     x += moved<0x140>(x);       // 15 - i
     if (Lanes == 16) return x;
-    // (results by way of integers: a cast of the second one itself gives the first)
-    const unsigned u = __builtin_bit_cast(unsigned, x);
-    const auto rows = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    const unsigned even = rows[0], odd = rows[1];
-    x = __builtin_bit_cast(float, even) + __builtin_bit_cast(float, odd);
-    const unsigned v = __builtin_bit_cast(unsigned, x);
-    const auto halves = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-    const unsigned low = halves[0], high = halves[1];
-    return __builtin_bit_cast(float, low) + __builtin_bit_cast(float, high);
+    const Both r = exchange_rows(x), h = exchange_halves(r.first + r.second);
+    return h.first + h.second;
+}
+
+// The largest of a wavefront.
+__device__ __forceinline__ float wave_max(float x)
+{
+    x = fmaxf(x, moved<0xb1>(x));
+    x = fmaxf(x, moved<0x4e>(x));
+    x = fmaxf(x, moved<0x141>(x));
+    x = fmaxf(x, moved<0x140>(x));
+    const Both r = exchange_rows(x), h = exchange_halves(fmaxf(r.first, r.second));
+    return fmaxf(h.first, h.second);
 }
 
 }  // namespace eager
