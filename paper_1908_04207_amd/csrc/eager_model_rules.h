@@ -223,10 +223,15 @@ inline int layer_norm_threads(int width)
     return threads;
 }
 
+// Workgroups of its forward pass, which go on in steps of them: as many as run at once.  Measured, 1024, 2048, 4096 of them and one
+// for each of the rows' groups: 20011 x 1600 fp32 109, 102, 103, 105 us; 3000 x 8192 fp32 76.8, 76.7, 79.4, 80.6; 8192 x 1024 bf16 14.2,
+// 13.3, 13.4, 13.3.
+constexpr long long kNormBlocks = 2048;
+
 // Threads of a workgroup of its backward pass (more where a row takes more), and workgroups: one a compute unit, each of
 // which leaves 2 width sums.  Measured, both kernels, 256 and 512 workgroups: 8192 x 1024 bf16 19.1 and 23.6 us, 2047 x 8192
 // 33.3 and 41.9, 20011 x 1600 fp32 102 and 105, 65536 x 64 bf16 15.0 and 14.0; 256 threads and 512 workgroups 19.3 us, 37.4, 113;
-// 1024 threads spill (47.2, 88.3, 338).
+// 1024 threads spill (47.2, 88.3, 338).  Two rows under way instead of one: 19.4, 31.8 against 33.3, 104, and 3000 x 8192 fp32 97 against 87.
 constexpr int kNormBackwardBlock = 512;
 inline int layer_norm_blocks(long long rows, int width)
 {
