@@ -75,63 +75,73 @@ struct List {
     }
 };
 
-// N sums over a wavefront at once: in the first steps a lane hands one half of its sums on and keeps the other's, so
-// sum i ends in the lanes whose last bits are i.
-template <int N, int M = 1>
-__device__ __forceinline__ float sums_apart(const float (&x)[N], int lane)
+// Four sums over a wavefront at once: in two steps a lane hands half of its sums on and keeps the others, then the
+// lanes that share their last two bits are added.  Sum i ends in the lanes whose last bits are i.
+__device__ __forceinline__ float sums_apart(const float (&x)[4], int lane)
 {
-    if constexpr (N == 1) {
-        float c = x[0];
-#pragma unroll
-        for (int m = M; m < 64; m *= 2) c += __shfl_xor(c, m, 64);
-        return c;
-    } else {
-        float half[N / 2];
-#pragma unroll
-        for (int i = 0; i < N / 2; ++i) half[i] = (lane & M ? x[2 * i + 1] : x[2 * i]) + __shfl_xor(lane & M ? x[2 * i] : x[2 * i + 1], M, 64);
-        return sums_apart<N / 2, 2 * M>(half, lane);
-    }
+    const bool odd = lane & 1, upper = lane & 2;
+    const float a = (odd ? x[1] : x[0]) + moved<0xb1>(odd ? x[0] : x[1]);       // 1 0 3 2
+    const float b = (odd ? x[3] : x[2]) + moved<0xb1>(odd ? x[2] : x[3]);
+    float c = (upper ? b : a) + moved<0x4e>(upper ? a : b);                     // 2 3 0 1
+    c += moved<0x128>(c);                                                       // 8 on in a row of 16
+    c += moved<0x124>(c);                                                       // 4 on
+    const Both r = exchange_rows(c), h = exchange_halves(r.first + r.second);
+    return h.first + h.second;
 }
 
 constexpr int kPicked = 4;
 
-// One row a workgroup, kPicked entries a wavefront at a time.
+__device__ __forceinline__ float dot(bf16x8 a, bf16x8 b, float c)
+{
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) c = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{a[i], a[i + 1]}, bf16x2{b[i], b[i + 1]}, c, false);
+    return c;
+}
+__device__ __forceinline__ float dot(f32x4 a, f32x4 b, float c)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = fmaf(a[i], b[i], c);
+    return c;
+}
+
+// One row a workgroup, kPicked entries a wavefront at a time: lane k holds entry k, its word goes into a scalar address,
+// and its sum comes back to it.
 template <typename T, int N>
 __global__ __launch_bounds__(256) void picked_kernel(const CrossEntropyArgs a, long long *favourite)
 {
     constexpr int E = kVector<T>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), entries = a.teacher.entries;
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        if (wave == 3) {
-            const long long word = List<N>(a.teacher, row, lane).favourite(a.vocab, lane);
-            if (lane == 0) favourite[row] = word;
-        }
+        const List<N> list(a.teacher, row, lane);
         const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
-        for (int e0 = kPicked * wave; e0 < entries; e0 += 4 * kPicked) {
-            const T *w[kPicked];
-            float sum[kPicked] = {};
-            long long mine = -1;
-            bool used = false;
 #pragma unroll
-            for (int j = 0; j < kPicked; ++j) {
-                const int k = min(e0 + j, entries - 1);
-                const long long index = a.teacher.index[row * entries + k];
-                const bool there = counts(index, a.teacher.logits[row * entries + k]);
-                if ((lane & (kPicked - 1)) == j) mine = index, used = there;
-                w[j] = static_cast<const T *>(a.w) + (there && index < a.vocab ? index : 0) * a.w_stride;
-            }
-            for (int at = lane * E; at < a.width; at += 64 * E) {
-                const auto u = load16(x + at);
+        for (int b = 0; b < N; ++b) {
+            const bool there = list.used[b] && list.index[b] < a.vocab;
+            const unsigned long long any = __ballot(there);
+            const int word = there ? static_cast<int>(list.index[b]) : 0;
+            float mine = 0.0f;
+            for (int i = kPicked * wave; i < 64; i += 4 * kPicked) {
+                if (!(any >> i & ((1ull << kPicked) - 1))) continue;
+                const T *w[kPicked];
+                float sum[kPicked] = {};
 #pragma unroll
-                for (int j = 0; j < kPicked; ++j) {
-                    const auto v = load16(w[j] + at);
+                for (int j = 0; j < kPicked; ++j)
+                    w[j] = static_cast<const T *>(a.w) + __builtin_amdgcn_readlane(word, i + j) * a.w_stride;
+#pragma unroll 2
+                for (int at = lane * E; at < a.width; at += 64 * E) {
+                    const auto u = load16(x + at);
 #pragma unroll
-                    for (int i = 0; i < E; ++i) sum[j] = fmaf(static_cast<float>(u[i]), static_cast<float>(v[i]), sum[j]);
+                    for (int j = 0; j < kPicked; ++j) sum[j] = dot(u, load16(w[j] + at), sum[j]);
                 }
+                const float all = sums_apart(sum, lane);         // sum j in lanes kPicked n + j, i + j among them
+                if (lane / kPicked == i / kPicked) mine = all;
             }
-            const float all = sums_apart(sum, lane);
-            if (lane < kPicked && e0 + lane < entries)
-                a.teacher.picked[row * entries + e0 + lane] = !used ? 0.0f : mine < a.vocab ? all : __builtin_nanf("");
+            if (64 * b + lane < entries && lane / kPicked % 4 == wave)
+                a.teacher.picked[row * entries + 64 * b + lane] = there ? mine : list.used[b] ? __builtin_nanf("") : 0.0f;
+        }
+        if (wave == 3) {
+            const long long word = list.favourite(a.vocab, lane);
+            if (lane == 0) favourite[row] = word;
         }
     }
 }
@@ -211,16 +221,17 @@ __global__ __launch_bounds__(1024) void entries_kernel(const CrossEntropyArgs a,
     float p[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) p[j] = list.used[j] ? a.teacher.picked[there * a.teacher.entries + 64 * j + lane] : 0.0f;
+    const int known = max(place, 0);
+    const long long word = n.favourite[known];
+    const float lse = n.lse[known] * kLog2e, by = n.dloss[known];
     if (n.others) {
         const long long mine = static_cast<long long>(blockIdx.x) * kJoined + threadIdx.x % kJoined;
         const float sum = joined_sums(n.others, mine < a.rows ? n.place[mine] : -1, a.rows, n.tiles, part);
         if (threadIdx.x < kJoined) apart[threadIdx.x] = sum;
         __syncthreads();
     }
-    if (place < 0) return;
-    const long long word = n.favourite[place];
-    if (word >= a.vocab) return;                         // the tiles wrote NaN
-    const float top = list.top(), lse = n.lse[place] * kLog2e, by = n.dloss[place];
+    if (place < 0 || word >= a.vocab) return;            // (beyond the vocabulary: the tiles wrote NaN)
+    const float top = list.top();
     float sum = 0.0f, q[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
