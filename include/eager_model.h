@@ -172,8 +172,9 @@ typedef struct {
  *     y = (s - m) r w + b
  * and stats[row] = m, stats[rows + row] = r, for the backward pass.  The norm is that of the s that is stored.
  * residual and sum may be NULL, both or none: s is x.  b may be NULL: none is added.  sum and y may each be x or
- * residual, but not the same one.  A row of equal values has r = eps^(-1/2), with eps = 0 NaN in y.  Non-finite
- * values stay in their row.
+ * residual (with its stride), but not the same one.  A row of equal values has r = eps^(-1/2), with eps = 0 NaN in y.
+ * Squares are formed in fp32: values some 2^63 away from their mean overflow, 2^-63 count as none.  Non-finite values
+ * stay in their row.
  * Errors: EINVAL (NULL, alignment, strides, sizes, eps negative or not finite), EDEVICE.
  *
  * Backward, from the gradients dy of y and ds of s (NULL: s is used nowhere else):
@@ -226,8 +227,8 @@ typedef enum {
  * The first `part` elements (a multiple of 8, up to head_dim) of every head of q and k turned by the position's
  * angles, the others as they are: of a pair (a, b),
  *     a' = a cos - b sin,  b' = b cos + a sin.
- * rotation: tables of part / 2 columns.  q_out and k_out may be q and k themselves; nothing behind `part` is moved
- * then.  A token whose position is outside the table gets NaN in the first `part` elements of its output heads.
+ * rotation: tables of part / 2 columns.  q_out and k_out may be q and k themselves (with their strides); nothing
+ * behind `part` is moved then.  A token whose position is outside the table gets NaN in the first `part` elements of its output heads.
  * Errors: EINVAL (NULL, alignment, strides, sizes, layout), EDEVICE.
  *
  * Backward: the same with the sines' sign turned, from the gradients of the outputs; dq, dk may be dq_out, dk_out.

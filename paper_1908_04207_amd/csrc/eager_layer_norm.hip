@@ -41,6 +41,14 @@ __device__ __forceinline__ float2 group_sums(float2 x, float2 *part)
     return x;
 }
 
+// Which of a workgroup's groups; a scalar where a wavefront belongs to one, and so are the addresses of its row then.
+template <int Threads>
+__device__ __forceinline__ int group_of()
+{
+    const int group = threadIdx.x / Threads;
+    return Threads < 64 ? group : __builtin_amdgcn_readfirstlane(group);
+}
+
 template <int Threads> constexpr int kBlock = Threads < 256 ? 256 : Threads;
 template <int Threads> constexpr int kBackwardBlock = Threads < kNormBackwardBlock ? kNormBackwardBlock : Threads;
 
@@ -49,10 +57,10 @@ __global__ __launch_bounds__(kBlock<Threads>) void layer_norm_kernel(const Layer
 {
     constexpr int E = kVector<T>, Groups = kBlock<Threads> / Threads;
     __shared__ float2 part[2][16];
-    const int lane = threadIdx.x % Threads;
+    const int lane = threadIdx.x % Threads, group = group_of<Threads>();
     // as many turns for every group of the workgroup
     for (long long first = static_cast<long long>(blockIdx.x) * Groups; first < a.rows; first += static_cast<long long>(gridDim.x) * Groups) {
-        const long long row = first + threadIdx.x / Threads;
+        const long long row = first + group;
         const bool live = row < a.rows;
         float x[C][E], sum = 0.0f;
 #pragma unroll
@@ -114,8 +122,11 @@ __global__ __launch_bounds__(kBackwardBlock<Threads>) void layer_norm_backward_k
     typedef typename Vector<T>::type vec;
     __shared__ float2 part[2][16];
     __shared__ __align__(16) float sums[Groups > 1 ? Groups : 1][Groups > 1 ? Threads * C * E : 4];
-    const int lane = threadIdx.x % Threads, group = threadIdx.x / Threads;
-    // the next row is under way while one is worked on
+    const int lane = threadIdx.x % Threads, group = group_of<Threads>();
+    // Where a row takes 1024 lanes their registers do not hold all of it: the sums of dw and db stand in shared memory, the
+    // gain is read again for every row, and in fp32 the next row is not under way while one is worked on.
+    constexpr bool Held = Threads == 1024, Ahead = !Held || sizeof(T) == 2;
+    __shared__ f32x4 held[Held ? 2 : 1][Held ? C * E / 4 : 1][Held ? Threads : 1];
     vec w[C] = {}, s[C], g[C], d[C];
     float gain[C][E], bias[C][E], next_mean, next_r;
     auto fetch = [&](long long row) {
@@ -133,18 +144,21 @@ __global__ __launch_bounds__(kBackwardBlock<Threads>) void layer_norm_backward_k
     };
     const long long step = static_cast<long long>(gridDim.x) * Groups;
     long long row = static_cast<long long>(blockIdx.x) * Groups + group;
-    fetch(row);
+    if (Ahead) fetch(row);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int at = (c * Threads + lane) * E;
-        if (at < a.width) w[c] = load16(static_cast<const T *>(a.w) + at);
+        if (!Held && at < a.width) w[c] = load16(static_cast<const T *>(a.w) + at);
 #pragma unroll
         for (int i = 0; i < E; ++i) gain[c][i] = bias[c][i] = 0.0f;
+        if (Held)
+            for (int i = 0; i < E / 4; ++i) held[0][c * E / 4 + i][lane] = held[1][c * E / 4 + i][lane] = f32x4{};
     }
     int turn = 0;
     // as many turns for every group of the workgroup
     for (long long first = static_cast<long long>(blockIdx.x) * Groups; first < a.rows; first += step, row += step, turn ^= 1) {
         const bool live = row < a.rows;
+        if (!Ahead) fetch(row);
         const float mean = next_mean, r = next_r;
         float n[C][E], dn[C][E];
         vec rest[C];
@@ -152,6 +166,7 @@ __global__ __launch_bounds__(kBackwardBlock<Threads>) void layer_norm_backward_k
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             rest[c] = d[c];
+            if (Held && (c * Threads + lane) * E < a.width) w[c] = load16(static_cast<const T *>(a.w) + (c * Threads + lane) * E);
 #pragma unroll
             for (int i = 0; i < E; ++i) {
                 const float dy = static_cast<float>(g[c][i]);
@@ -159,11 +174,25 @@ __global__ __launch_bounds__(kBackwardBlock<Threads>) void layer_norm_backward_k
                 dn[c][i] = dy * static_cast<float>(w[c][i]);
                 both.x += dn[c][i];
                 both.y = fmaf(dn[c][i], n[c][i], both.y);
+                if (Held) continue;
                 gain[c][i] = fmaf(dy, n[c][i], gain[c][i]);
                 bias[c][i] += dy;
             }
+            if (Held)
+#pragma unroll
+                for (int i = 0; i < E / 4; ++i) {
+                    f32x4 u = held[0][c * E / 4 + i][lane], v = held[1][c * E / 4 + i][lane];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float dy = static_cast<float>(g[c][4 * i + e]);
+                        u[e] = fmaf(dy, n[c][4 * i + e], u[e]);
+                        v[e] += dy;
+                    }
+                    held[0][c * E / 4 + i][lane] = u;
+                    held[1][c * E / 4 + i][lane] = v;
+                }
         }
-        fetch(row + step);
+        if (Ahead) fetch(row + step);
         both = group_sums<Threads>(both, part[turn]);
         if (!live) continue;
         const float even = both.x * a.inv_width, along = both.y * a.inv_width;
@@ -206,8 +235,10 @@ __global__ __launch_bounds__(kBackwardBlock<Threads>) void layer_norm_backward_k
         if (at >= a.width) continue;
 #pragma unroll
         for (int i = 0; i < E; i += 4) {
-            *reinterpret_cast<f32x4 *>(out + at + i) = f32x4{gain[c][i], gain[c][i + 1], gain[c][i + 2], gain[c][i + 3]};
-            *reinterpret_cast<f32x4 *>(out + a.width + at + i) = f32x4{bias[c][i], bias[c][i + 1], bias[c][i + 2], bias[c][i + 3]};
+            const f32x4 u = {gain[c][i], gain[c][i + 1], gain[c][i + 2], gain[c][i + 3]};
+            const f32x4 v = {bias[c][i], bias[c][i + 1], bias[c][i + 2], bias[c][i + 3]};
+            *reinterpret_cast<f32x4 *>(out + at + i) = Held ? held[0][(c * E + i) / 4][lane] : u;
+            *reinterpret_cast<f32x4 *>(out + a.width + at + i) = Held ? held[1][(c * E + i) / 4][lane] : v;
         }
     }
 }

@@ -128,6 +128,16 @@ bool fill(eager::CrossEntropyArgs &a, int dtype, const eager_projection *s, cons
     return true;
 }
 
+// An output in the place of an input is laid out like it.
+bool same_or_apart(const eager_heads *x, const eager_heads *y, int64_t tokens, int32_t count)
+{
+    return x->data != y->data || ((tokens < 2 || x->row_stride == y->row_stride) && (count < 2 || x->head_stride == y->head_stride));
+}
+bool same_or_apart(const eager_rows *x, const eager_rows *y, int64_t rows)
+{
+    return !x || !y || x->data != y->data || rows < 2 || x->stride == y->stride;
+}
+
 // rows of one array: on 16 bytes, none shares elements with the next one
 bool valid_rows(const eager_rows *r, int dtype, int64_t rows, int32_t width)
 {
@@ -154,6 +164,8 @@ int rotate(int dtype, const eager_packed *s, const eager_heads *q, const eager_h
     for (int i = 0; i < 2; ++i)
         if (!valid_heads(x[i], dtype, s) || !valid_heads(y[i], dtype, s)) return EAGER_EINVAL;
     if (s->tokens == 0) return EAGER_OK;
+    for (int i = 0; i < 2; ++i)
+        if (!same_or_apart(x[i], y[i], s->tokens, i ? s->kv_heads : s->q_heads)) return EAGER_EINVAL;
     eager::RotaryArgs a = {};
     a.heads[0] = s->q_heads;
     a.heads[1] = s->kv_heads;
@@ -371,6 +383,8 @@ int eager_layer_norm(int dtype, int64_t rows, int32_t width, const eager_rows *x
         !aligned(w, 16) || (b && !aligned(b, 16)) || !(eps >= 0.0f) || !std::isfinite(eps) || !(aligned(stats, 4) || rows == 0) ||
         (rows && sum && sum->data == y->data))
         return EAGER_EINVAL;
+    for (const eager_rows *to : {sum, y})
+        if (!same_or_apart(x, to, rows) || !same_or_apart(residual, to, rows)) return EAGER_EINVAL;
     if (rows == 0) return EAGER_OK;
     eager::LayerNormArgs a = {};
     a.x = rows_of(x);
@@ -401,7 +415,7 @@ int eager_layer_norm_backward(int dtype, int64_t rows, int32_t width, const eage
     if (!valid_norm(dtype, rows, width) || !valid_rows(dy, dtype, rows, width) || (ds && !valid_rows(ds, dtype, rows, width)) ||
         !valid_rows(s, dtype, rows, width) || !valid_rows(dx, dtype, rows, width) || !aligned(w, 16) ||
         !(aligned(stats, 4) || rows == 0) || (dw && !aligned(dw, 4)) || (db && !aligned(db, 4)) || !aligned(workspace, 16) ||
-        workspace_bytes < eager::layer_norm_workspace_bytes(rows, width))
+        workspace_bytes < eager::layer_norm_workspace_bytes(rows, width) || !same_or_apart(dy, dx, rows) || !same_or_apart(ds, dx, rows))
         return EAGER_EINVAL;
     eager::LayerNormArgs a = {};
     a.x = rows_of(s);

@@ -68,6 +68,10 @@ def test_layer_norm_refusals(dtype):
     _refused(lambda: forward(sum=None))                  # a residual whose sum goes nowhere
     _refused(lambda: forward(residual=None))             # a sum without a residual
     _refused(lambda: forward(y=_rows(B)))                # the sum and its norm in one place
+    for bad in (dict(sum=_rows(A, 264)), dict(y=_rows(A, 264)), dict(residual=_rows(C, 264))):       # in an input's place, otherwise laid out
+        _refused(lambda: forward(**bad))
+    for bad in (dict(dy=_rows(B), dx=_rows(B, 264)), dict(ds=_rows(C), dx=_rows(C, 512))):
+        _refused(lambda: backward(**bad))
     for name, bad in itertools.product(("x", "residual", "sum", "y"), VIEWS):
         _refused(lambda: forward(**{name: bad and _rows(**bad)}))
     for name, bad in itertools.product(("dy", "s", "dx"), VIEWS):
@@ -133,6 +137,9 @@ def test_rotary_refusals(dtype):
                  dict(head_stride=66), dict(row_stride=2 ** 22)]
         for name, bad in itertools.product(("q", "k", "q_out", "k_out"), views):
             _refused(lambda: call(**{name: bad and heads(**bad)}))
+        for bad in (dict(row_stride=512), dict(head_stride=128, row_stride=512)):
+            _refused(lambda: call(q_out=heads(**bad)))
+            _refused(lambda: call(k_out=heads(**bad)))
         none = heads(data=None)
         call(shape=shape(tokens=0), q=none, k=none, q_out=none, k_out=none, rotation=rot(positions=None))
 
