@@ -207,6 +207,8 @@ __global__ __launch_bounds__(kBackwardBlock<Threads>) void layer_norm_backward_k
     }
     if (!a.partials) return;
     float *out = a.partials + static_cast<long long>(blockIdx.x) * 2 * a.width;
+    T *const to[2] = {static_cast<T *>(a.dw), static_cast<T *>(a.db)};
+    const bool alone = gridDim.x == 1;                   // its sums are those of all rows
     if (Groups > 1) {
         // one sum after the other, so that shared memory holds those of all groups
 #pragma unroll
@@ -224,7 +226,8 @@ __global__ __launch_bounds__(kBackwardBlock<Threads>) void layer_norm_backward_k
                 float sum = sums[0][at];
 #pragma unroll
                 for (int g = 1; g < Groups; ++g) sum += sums[g][at];
-                out[which * a.width + at] = sum;
+                if (!alone) out[which * a.width + at] = sum;
+                else if (to[which]) to[which][at] = static_cast<T>(sum);
             }
         }
         return;
@@ -237,8 +240,14 @@ __global__ __launch_bounds__(kBackwardBlock<Threads>) void layer_norm_backward_k
         for (int i = 0; i < E; i += 4) {
             const f32x4 u = {gain[c][i], gain[c][i + 1], gain[c][i + 2], gain[c][i + 3]};
             const f32x4 v = {bias[c][i], bias[c][i + 1], bias[c][i + 2], bias[c][i + 3]};
-            *reinterpret_cast<f32x4 *>(out + at + i) = Held ? held[0][(c * E + i) / 4][lane] : u;
-            *reinterpret_cast<f32x4 *>(out + a.width + at + i) = Held ? held[1][(c * E + i) / 4][lane] : v;
+            const f32x4 sum[2] = {Held ? held[0][(c * E + i) / 4][lane] : u, Held ? held[1][(c * E + i) / 4][lane] : v};
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                if (!alone) *reinterpret_cast<f32x4 *>(out + which * a.width + at + i) = sum[which];
+                else if (to[which])
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) to[which][at + i + e] = static_cast<T>(sum[which][e]);
+            }
         }
     }
 }
@@ -279,7 +288,7 @@ hipError_t enqueue(const LayerNormArgs &a, bool backward, hipStream_t stream)
                       dim3(kBlock<Threads>), 0, stream, a);
     hipError_t e = hipSuccess;
     if (a.blocks) e = launch(layer_norm_backward_kernel<T, Threads, C>, dim3(a.blocks), dim3(kBackwardBlock<Threads>), 0, stream, a);
-    if (e != hipSuccess || !a.partials) return e;
+    if (e != hipSuccess || !a.partials || a.blocks == 1) return e;
     if (a.width < 2048) return launch(layer_norm_columns_kernel<T, 1>, dim3((a.width + 15) / 16, a.db ? 2 : 1), dim3(1024), 0, stream, a);
     return launch(layer_norm_columns_kernel<T, 4>, dim3((a.width + 63) / 64, a.db ? 2 : 1), dim3(1024), 0, stream, a);
 }

@@ -232,10 +232,14 @@ constexpr long long kNormBlocks = 2048;
 // which leaves 2 width sums.  Measured, both kernels, 256 and 512 workgroups: 8192 x 1024 bf16 19.1 and 23.6 us, 2047 x 8192
 // 33.3 and 41.9, 20011 x 1600 fp32 102 and 105, 65536 x 64 bf16 15.0 and 14.0; 256 threads and 512 workgroups 19.3 us, 37.4, 113;
 // 1024 threads spill (47.2, 88.3, 338).  Two rows under way instead of one: 19.4, 31.8 against 33.3, 104, and 3000 x 8192 fp32 97 against 87.
+// Rows of up to four turns are gone through by one workgroup, which leaves the sums themselves and needs no second kernel: a
+// call of 32 x 1024 bf16 7.3 us and 9.9 with one workgroup for 8 rows (on the GPU alone 7.8 and 7.5), 128 x 64 7.1 and 9.8 (5.7, 6.6),
+// 16 x 1600 fp32 8.5 and 10.0 (9.5, 8.4); 64 x 1024 in eight turns 10.7 and 10.0 (11.6, 7.5).
 constexpr int kNormBackwardBlock = 512;
 inline int layer_norm_blocks(long long rows, int width)
 {
     const int groups = std::max(kNormBackwardBlock / layer_norm_threads(width), 1);
+    if (rows > 0 && rows <= 4 * groups) return 1;
     return static_cast<int>(std::min<long long>((rows + groups - 1) / groups, kUnits));
 }
 
