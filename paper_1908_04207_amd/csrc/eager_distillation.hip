@@ -9,6 +9,11 @@
 // dot product each, in the forward pass; the losses; and the entries' dl, which replace what the tiles wrote there,
 // as p - q is to be rounded and not p.
 //
+// Bound by the products (see there).  Measured, us, 4096 x 1024 x 50257 in bf16 with 64 entries a row: picked logits 39 (435 MB of
+// the projection's rows at 11 TB/s, most from second-level caches; 61 with fmaf and vector addresses), divergences 7, favourites 5,
+// entries of dl 13.5, beside 910 of logits, twice, and 830 of dx and dw; 1019 rows in fp32 with 32 entries 15, 6.5, 5 and 8 beside
+// 1305 and 1180; 61 rows in bf16 with 16 entries 4 and 5.7 beside 19.
+//
 // Differences are formed where they keep their digits: log p from a logit's distance to the row's largest, and the
 // favourite's p - q, where p is beyond a half, from the sums of the others' q and p.
 #include "eager_distillation.h"
