@@ -63,8 +63,8 @@ typedef struct {
     int32_t        q_heads;     /* a multiple of kv_heads: q_heads / kv_heads share a key and value head */
     int32_t        kv_heads;
     int32_t        head_dim;    /* a multiple of 8 up to EAGER_MAX_HEAD_DIM */
-    int32_t        sequences;   /* >= 1 (not used by eager_qk_norm_rope) */
-    const int32_t *cu_seqlens;  /* (not used by eager_qk_norm_rope) */
+    int32_t        sequences;   /* >= 1 (not used by eager_qk_norm_rope and eager_rotary) */
+    const int32_t *cu_seqlens;  /* (not used by eager_qk_norm_rope and eager_rotary) */
 } eager_packed;
 
 /* The rotation's table: cos[p * head_dim/2 + i], sin[...] of position p < table_rows, and the
@@ -264,9 +264,10 @@ typedef struct {
  * Backward, for the upstream gradients dloss[r] (device, fp32), from lse and picked of the forward pass:
  *     dl_v = dloss[r] / temperature (p_v - sum of the q_k with index_k = v),  dx_r = sum_v dl_v w_v,
  *     dw_v = sum_r dl_v x_r
- * in pieces of the vocabulary, as eager_cross_entropy_backward.  Masked rows and rows with a dloss of zero are left
+ * in pieces of the vocabulary, as eager_cross_entropy_backward (rows: at most 2^25).  Masked rows and rows with a dloss of zero are left
  * out from the start.  The dl of the word that the teacher favours most is formed from the others' p and q where its
- * p is beyond a half, as long as one piece holds the vocabulary.  dx or dw may be NULL (not wanted).
+ * p is beyond a half, as long as one piece holds the vocabulary.  dx or dw may be NULL (not wanted).  p comes from lse and
+ * is as far off as lse in fp32 is (2^-24 |lse|): a temperature so low that logits over it reach 10^4 leaves three digits.
  */
 int eager_distillation(int dtype, const eager_projection *shape, const void *x, const void *w,
                        const eager_teacher *teacher, float *loss, float *lse, float *picked, void *workspace,

@@ -18,7 +18,9 @@ take comes back as NotImplemented and is checked and refused, or called, here.
     loss, lse, picked = distillation(x, w, index, logits, temperature)
 
 each with its `_backward`, and `QKNormRope`, `Attention`, `CrossEntropy`, `LayerNorm`, `AddLayerNorm`, `Rotary`,
-`Distillation` for torch's autograd (first derivatives; asked for the derivatives of gradients they raise).
+`Distillation` for torch's autograd (first derivatives; asked for the derivatives of gradients they raise).  All calls
+can be captured into a graph, and so can a backward pass, with leaves of its own: torch ends the process when an eager
+graph of the same leaves is still alive.
 """
 from __future__ import annotations
 
