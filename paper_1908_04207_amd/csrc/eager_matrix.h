@@ -198,13 +198,16 @@ __device__ __forceinline__ f32x8 read_columns(const char *tile, int col0, int k0
     return f;
 }
 
-// Tells the compiler's scheduler to issue Reads reads of shared memory and Loads loads from global
-// memory evenly among the next Products matrix instructions.
+// Tells the compiler's scheduler to issue Reads reads of shared memory evenly among the first three quarters of the next
+// Products matrix instructions, so that the last ones arrive before the step after needs them, and Loads loads from
+// global memory among all.  Measured, reads among all of them and so, 4096 x 1024 x 50257 in bf16: logits 469 and 453 us, the backward
+// pass 1204 and 1199; among half 460 and 1221, a quarter 456 and 1229.
 template <int Products, int Reads, int Loads, int I = 0>
 __device__ __forceinline__ void spread()
 {
     if constexpr (I < Products) {
-        constexpr int reads = (I + 1) * Reads / Products - I * Reads / Products;
+        constexpr int first = (3 * Products + 3) / 4;
+        constexpr int reads = I < first ? (I + 1) * Reads / first - I * Reads / first : 0;
         constexpr int loads = (I + 1) * Loads / Products - I * Loads / Products;
         if constexpr (reads > 0) __builtin_amdgcn_sched_group_barrier(0x100, reads, 0);
         if constexpr (loads > 0) __builtin_amdgcn_sched_group_barrier(0x20, loads, 0);
