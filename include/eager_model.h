@@ -180,7 +180,8 @@ typedef struct {
  * Backward, from the gradients dy of y and ds of s (NULL: s is used nowhere else):
  *     dn = dy w,  n = (s - m) r,  dx = ds + r (dn - mean(dn) - n mean(dn n)),  dw = sum dy n,  db = sum dy
  * dx is the gradient of x and of residual; it may be dy or ds.  dw and db (width values of dtype, the sums over all
- * rows rounded once) may be NULL: not wanted.  w and stats as in the forward pass.
+ * rows rounded once) may be NULL: not wanted.  w and stats as in the forward pass.  Few rows need no workspace
+ * (workspace_bytes gives 0; it may be NULL then).
  */
 int eager_layer_norm(int dtype, int64_t rows, int32_t width, const eager_rows *x, const eager_rows *residual,
                      const void *w, const void *b, float eps, const eager_rows *sum, const eager_rows *y,

@@ -205,7 +205,7 @@ __global__ __launch_bounds__(kBackwardBlock<Threads>) void layer_norm_backward_k
             store16(static_cast<T *>(a.sum.data) + row * a.sum.stride + at, n[c]);
         }
     }
-    if (!a.partials) return;
+    if (!a.dw && !a.db) return;
     float *out = a.partials + static_cast<long long>(blockIdx.x) * 2 * a.width;
     T *const to[2] = {static_cast<T *>(a.dw), static_cast<T *>(a.db)};
     const bool alone = gridDim.x == 1;                   // its sums are those of all rows
@@ -288,7 +288,7 @@ hipError_t enqueue(const LayerNormArgs &a, bool backward, hipStream_t stream)
                       dim3(kBlock<Threads>), 0, stream, a);
     hipError_t e = hipSuccess;
     if (a.blocks) e = launch(layer_norm_backward_kernel<T, Threads, C>, dim3(a.blocks), dim3(kBackwardBlock<Threads>), 0, stream, a);
-    if (e != hipSuccess || !a.partials || a.blocks == 1) return e;
+    if (e != hipSuccess || (!a.dw && !a.db) || a.blocks == 1) return e;
     if (a.width < 2048) return launch(layer_norm_columns_kernel<T, 1>, dim3((a.width + 15) / 16, a.db ? 2 : 1), dim3(1024), 0, stream, a);
     return launch(layer_norm_columns_kernel<T, 4>, dim3((a.width + 63) / 64, a.db ? 2 : 1), dim3(1024), 0, stream, a);
 }

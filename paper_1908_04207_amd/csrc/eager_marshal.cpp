@@ -649,7 +649,7 @@ PyObject *py_layer_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         !view_like(a[1], s, &r[1], &at[1]) || !view_like(a[2], s, &r[2], &at[2]) || !gain_of(a[3], s, &w) ||
         !as_tensor(a[4], &stats) || !table_of(stats, s.device, 2, s.size[0]) || !view_like(a[5], s, &r[3], &at[3]) ||
         !gain_of(a[6], s, &dw) || !gain_of(a[7], s, &db) || !fits_int(s.size[1]) || !stream_of(s, &stream) ||
-        model.layer_bytes(dtype, s.size[0], static_cast<int32_t>(s.size[1]), &bytes) != EAGER_OK || !space.take(bytes, a[2]))
+        model.layer_bytes(dtype, s.size[0], static_cast<int32_t>(s.size[1]), &bytes) != EAGER_OK || (bytes && !space.take(bytes, a[2])))
         return other_form();
     int st;
     Py_BEGIN_ALLOW_THREADS

@@ -412,10 +412,11 @@ int eager_layer_norm_backward(int dtype, int64_t rows, int32_t width, const eage
                               const eager_rows *s, const void *w, const float *stats, const eager_rows *dx, void *dw, void *db,
                               void *workspace, int64_t workspace_bytes, void *stream)
 {
+    const int64_t need = valid_norm(dtype, rows, width) ? eager::layer_norm_workspace_bytes(rows, width) : 0;
     if (!valid_norm(dtype, rows, width) || !valid_rows(dy, dtype, rows, width) || (ds && !valid_rows(ds, dtype, rows, width)) ||
         !valid_rows(s, dtype, rows, width) || !valid_rows(dx, dtype, rows, width) || !aligned(w, 16) ||
-        !(aligned(stats, 4) || rows == 0) || (dw && !aligned(dw, 4)) || (db && !aligned(db, 4)) || !aligned(workspace, 16) ||
-        workspace_bytes < eager::layer_norm_workspace_bytes(rows, width) || !same_or_apart(dy, dx, rows) || !same_or_apart(ds, dx, rows))
+        !(aligned(stats, 4) || rows == 0) || (dw && !aligned(dw, 4)) || (db && !aligned(db, 4)) || (need && !aligned(workspace, 16)) ||
+        workspace_bytes < need || !same_or_apart(dy, dx, rows) || !same_or_apart(ds, dx, rows))
         return EAGER_EINVAL;
     eager::LayerNormArgs a = {};
     a.x = rows_of(s);
@@ -426,7 +427,7 @@ int eager_layer_norm_backward(int dtype, int64_t rows, int32_t width, const eage
     a.dw = dw;
     a.db = db;
     a.stats = const_cast<float *>(stats);
-    a.partials = dw || db ? static_cast<float *>(workspace) : nullptr;
+    a.partials = static_cast<float *>(workspace);
     a.rows = rows;
     a.width = width;
     a.blocks = eager::layer_norm_blocks(rows, width);

@@ -245,7 +245,8 @@ inline int layer_norm_blocks(long long rows, int width)
 
 inline long long layer_norm_workspace_bytes(long long rows, int width)
 {
-    return std::max(layer_norm_blocks(rows, width), 1) * 2ll * width * 4;
+    const int blocks = layer_norm_blocks(rows, width);
+    return blocks > 1 ? blocks * 2ll * width * 4 : 0;
 }
 
 // Heads that one thread of a rotation takes one after the other, with the position's angles in its registers.  Measured, 1,

@@ -20,7 +20,8 @@ int main()
         for (long long rows : {0ll, 1ll, 3ll, 4ll, 17ll, 511ll, 512ll, 513ll, 2047ll, 8192ll, 70000ll, (1ll << 31) - (1ll << 16)}) {
             const int blocks = layer_norm_blocks(rows, width);
             CHECK(blocks >= 0 && blocks <= 1024 && (blocks > 0) == (rows > 0) && blocks <= rows);
-            CHECK(layer_norm_workspace_bytes(rows, width) >= blocks * 2ll * width * 4 && layer_norm_workspace_bytes(rows, width) > 0);
+            // a workgroup alone leaves the sums themselves
+            CHECK(layer_norm_workspace_bytes(rows, width) == (blocks > 1 ? blocks * 2ll * width * 4 : 0));
         }
     }
     for (long long rows : {0ll, 1ll, 255ll, 4096ll, 1ll << 25})

@@ -78,9 +78,11 @@ def test_layer_norm_refusals(dtype):
         _refused(lambda: backward(**{name: bad and _rows(**bad)}))
     for bad in VIEWS[1:]:
         _refused(lambda: backward(ds=_rows(**bad)))
-    need = eb.eager_layer_norm_workspace_bytes(dtype, 5, 256)
+    need = eb.eager_layer_norm_workspace_bytes(dtype, 500, 256)
+    assert need > 0 and eb.eager_layer_norm_workspace_bytes(dtype, 5, 256) == 0
     for bad in (dict(dw=A + 2), dict(db=A + 2), dict(workspace=None), dict(workspace=A + 8), dict(workspace_bytes=need - 1)):
-        _refused(lambda: backward(**bad))
+        _refused(lambda: backward(count=500, **bad))
+    _refused(lambda: backward(workspace_bytes=-1))
     none = _rows(None)
     forward(count=0, x=none, residual=none, sum=none, y=none, stats=None)
     for bad in ((3, 5, 256), (dtype, -1, 256), (dtype, 5, 12)):
