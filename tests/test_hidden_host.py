@@ -40,6 +40,17 @@ def test_rules_on_the_cpu(tmp_path):
     assert r.returncode == 0 and r.stdout.strip() == "ok", (r.stdout[-500:], r.stderr[-2000:])
 
 
+def test_what_the_calls_hand_over(tmp_path):
+    """eager_model_api.cpp without the kernels, under both sanitizers: arguments of every launch, angles in long double."""
+    exe = tmp_path / "hidden_api"
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+                           "-static-libasan", "-Wall", "-Wextra", "-Werror", "-D__HIP_PLATFORM_AMD__", "-isystem", "/opt/rocm/include",
+                           os.path.join(ROOT, "tests", "c", "hidden_api_host.cpp"),
+                           os.path.join(ROOT, "paper_1908_04207_amd", "csrc", "eager_model_api.cpp"), "-o", str(exe)])
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", (r.stdout[-500:], r.stderr[-2000:])
+
+
 def _rows(data=A, stride=256):
     return eb.Rows(data, stride)
 
