@@ -49,16 +49,22 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, int pla
             const int first = turns ? place * V : 2 * a.half + (place - turned) * Pieces * V, second = first + (turns ? a.half : V);
             if (first >= moved) continue;
             const bool both = Pieces == 2 && second < moved;
-            const int h0 = group * kTurnedHeads, heads = min(kTurnedHeads, (which ? a.heads[1] : a.heads[0]) - h0);
+            // A thread's heads lie side by side, or where pairs are halves apart as many on as there are groups, so that the
+            // short pieces of neighbouring threads lie beside each other.  Measured, side by side and apart, us: halves, bf16,
+            // 52083 tokens of 12 heads of 80 53.0 and 47.5, 14568 of 143 of 24 57.5 and 51.9; interleaved, fp32, 19531 of 20 of 64
+            // 47.9 and 50.0.
+            const int apart = Interleaved ? 1 : which ? a.groups[1] : a.groups[0], h0 = Interleaved ? group * kTurnedHeads : group;
+            const int left = (which ? a.heads[1] : a.heads[0]) - h0;
             const Heads from = which ? a.x[1] : a.x[0], to = which ? a.y[1] : a.y[0];
             const T *x = static_cast<const T *>(from.data) + token * from.row + h0 * from.head;
             T *y = static_cast<T *>(to.data) + token * to.row + h0 * to.head;
+            const long long x_step = apart * from.head, y_step = apart * to.head;
             vec p[kTurnedHeads], q[kTurnedHeads];
 #pragma unroll
             for (int h = 0; h < kTurnedHeads; ++h)
-                if (h < heads) {
-                    p[h] = *reinterpret_cast<const vec *>(x + h * from.head + first);
-                    if (both) q[h] = *reinterpret_cast<const vec *>(x + h * from.head + second);
+                if (h * apart < left) {
+                    p[h] = *reinterpret_cast<const vec *>(x + h * x_step + first);
+                    if (both) q[h] = *reinterpret_cast<const vec *>(x + h * x_step + second);
                 }
             if (turns) {
                 const bool known = pos >= 0 && pos < a.table_rows;
@@ -84,9 +90,9 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, int pla
             }
 #pragma unroll
             for (int h = 0; h < kTurnedHeads; ++h)
-                if (h < heads) {
-                    *reinterpret_cast<vec *>(y + h * to.head + first) = p[h];
-                    if (both) *reinterpret_cast<vec *>(y + h * to.head + second) = q[h];
+                if (h * apart < left) {
+                    *reinterpret_cast<vec *>(y + h * y_step + first) = p[h];
+                    if (both) *reinterpret_cast<vec *>(y + h * y_step + second) = q[h];
                 }
         }
     }
