@@ -80,22 +80,6 @@ struct List {
     }
 };
 
-// Four sums over a wavefront at once: in two steps a lane hands half of its sums on and keeps the others, then the
-// lanes that share their last two bits are added.  Sum i ends in the lanes whose last bits are i.
-__device__ __forceinline__ float sums_apart(const float (&x)[4], int lane)
-{
-    const bool odd = lane & 1, upper = lane & 2;
-    const float a = (odd ? x[1] : x[0]) + moved<0xb1>(odd ? x[0] : x[1]);       // 1 0 3 2
-    const float b = (odd ? x[3] : x[2]) + moved<0xb1>(odd ? x[2] : x[3]);
-    float c = (upper ? b : a) + moved<0x4e>(upper ? a : b);                     // 2 3 0 1
-    c += moved<0x128>(c);                                                       // 8 on in a row of 16
-    c += moved<0x124>(c);                                                       // 4 on
-    const Both r = exchange_rows(c), h = exchange_halves(r.first + r.second);
-    return h.first + h.second;
-}
-
-constexpr int kPicked = 4;
-
 __device__ __forceinline__ float dot(bf16x8 a, bf16x8 b, float c)
 {
 #pragma unroll
@@ -109,40 +93,48 @@ __device__ __forceinline__ float dot(f32x4 a, f32x4 b, float c)
     return c;
 }
 
-// One row a workgroup, kPicked entries a wavefront at a time: lane k holds entry k, its word goes into a scalar address,
-// and its sum comes back to it.
+// One row a workgroup.  Eight lanes take an entry, 128 bytes of its word's row at a time, so that rows of any width keep
+// them busy and a load covers eight entries; a wavefront has two such sets of entries under way.
 template <typename T, int N>
 __global__ __launch_bounds__(256) void picked_kernel(const CrossEntropyArgs a, long long *favourite)
 {
     constexpr int E = kVector<T>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), entries = a.teacher.entries;
+    const int in = lane >> 3, first = (lane & 7) * E;
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const List<N> list(a.teacher, row, lane);
         const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
 #pragma unroll
         for (int b = 0; b < N; ++b) {
             const bool there = list.used[b] && list.index[b] < a.vocab;
-            const unsigned long long any = __ballot(there);
+            const unsigned long long known = __ballot(there), used = __ballot(list.used[b]);
             const int word = there ? static_cast<int>(list.index[b]) : 0;
-            float mine = 0.0f;
-            for (int i = kPicked * wave; i < 64; i += 4 * kPicked) {
-                if (!(any >> i & ((1ull << kPicked) - 1))) continue;
-                const T *w[kPicked];
-                float sum[kPicked] = {};
+            const int at[2] = {8 * wave + in, 32 + 8 * wave + in};
+            const T *w[2];
+            float sum[2] = {};
 #pragma unroll
-                for (int j = 0; j < kPicked; ++j)
-                    w[j] = static_cast<const T *>(a.w) + __builtin_amdgcn_readlane(word, i + j) * a.w_stride;
-#pragma unroll 2
-                for (int at = lane * E; at < a.width; at += 64 * E) {
-                    const auto u = load16(x + at);
+            for (int j = 0; j < 2; ++j) w[j] = static_cast<const T *>(a.w) + __shfl(word, at[j], 64) * a.w_stride;
+            const bool both = known >> (32 + 8 * wave) & 0xff;
+            if (both) {
+#pragma unroll 4
+                for (int i = first; i < a.width; i += 8 * E) {
+                    const auto u = load16(x + i);
 #pragma unroll
-                    for (int j = 0; j < kPicked; ++j) sum[j] = dot(u, load16(w[j] + at), sum[j]);
+                    for (int j = 0; j < 2; ++j) sum[j] = dot(u, load16(w[j] + i), sum[j]);
                 }
-                const float all = sums_apart(sum, lane);         // sum j in lanes kPicked n + j, i + j among them
-                if (lane / kPicked == i / kPicked) mine = all;
+            } else if (known >> (8 * wave) & 0xff) {
+#pragma unroll 8
+                for (int i = first; i < a.width; i += 8 * E) sum[0] = dot(load16(x + i), load16(w[0] + i), sum[0]);
             }
-            if (64 * b + lane < entries && lane / kPicked % 4 == wave)
-                a.teacher.picked[row * entries + 64 * b + lane] = there ? mine : list.used[b] ? __builtin_nanf("") : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                sum[j] += moved<0xb1>(sum[j]);          // 1 0 3 2
+                sum[j] += moved<0x4e>(sum[j]);          // 2 3 0 1
+                sum[j] += moved<0x141>(sum[j]);         // 7 - i
+                if (first == 0 && 64 * b + at[j] < entries)
+                    a.teacher.picked[row * entries + 64 * b + at[j]] =
+                        known >> at[j] & 1 ? sum[j] : used >> at[j] & 1 ? __builtin_nanf("") : 0.0f;
+            }
         }
         if (wave == 3) {
             const long long word = list.favourite(a.vocab, lane);
