@@ -10,9 +10,10 @@
 // as p - q is to be rounded and not p.
 //
 // Bound by the products (see there).  Measured, us, 4096 x 1024 x 50257 in bf16 with 64 entries a row: picked logits 39 (435 MB of
-// the projection's rows at 11 TB/s, most from second-level caches; 61 with fmaf and vector addresses), divergences 7, favourites 5,
-// entries of dl 13.5, beside 910 of logits, twice, and 830 of dx and dw; 1019 rows in fp32 with 32 entries 15, 6.5, 5 and 8 beside
-// 1305 and 1180; 61 rows in bf16 with 16 entries 4 and 5.7 beside 19.
+// the projection's rows at 11 TB/s, most from second-level caches; 61 with fmaf for dot instructions and 64 lanes an entry), divergences 7, favourites 5,
+// entries of dl 12, beside 910 of logits, twice, and 830 of dx and dw; 1019 rows in fp32 with 32 entries 16.5, 6.5, 5 and 7.5 beside
+// 1305 and 1180; 61 rows in bf16 with 16 entries 4 and 5.7 beside 19; 300 x 512 x 3000 in bf16 with 128 entries 6.8, 5, 3.3 and 8.2 (27
+// where every list was searched for repeated words with their shares) beside 22 and 10.
 //
 // Differences are formed where they keep their digits: log p from a logit's distance to the row's largest, and the
 // favourite's p - q, where p is beyond a half, from the sums of the others' q and p.
@@ -209,7 +210,8 @@ template <typename T, int N>
 __global__ __launch_bounds__(1024) void entries_kernel(const CrossEntropyArgs a, const Entries n)
 {
     __shared__ float part[16][kJoined], apart[kJoined];
-    __shared__ int words[kJoined][64 * N];
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
+    __shared__ __align__(16) int words[kJoined][64 * N];
     __shared__ float shares[kJoined][64 * N];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long row = static_cast<long long>(blockIdx.x) * kJoined + wave, there = min(row, a.rows - 1);
@@ -246,20 +248,36 @@ __global__ __launch_bounds__(1024) void entries_kernel(const CrossEntropyArgs a,
     }
     rest = lanes_sum<64>(rest);
     __builtin_amdgcn_wave_barrier();
-    // a word that stands in several entries is written by the first of them, with all their shares
-    float share[N] = {};
-    bool first[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) first[j] = list.used[j] && list.index[j] >= n.first && list.index[j] < n.first + n.live;
+    bool first[N], several = false;
+    float share[N];
+    int same[N] = {};
 #pragma unroll 4
-    for (int i = 0; i < a.teacher.entries; ++i) {
-        const int word_i = words[wave][i];
-        const float share_i = shares[wave][i];
+    for (int i = 0; i < a.teacher.entries; i += 4) {
+        const i32x4 four = *reinterpret_cast<const i32x4 *>(&words[wave][i]);
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const bool same = list.used[j] && word_i == static_cast<int>(list.index[j]);
-            share[j] += same ? share_i : 0.0f;
-            first[j] &= !(same && i < 64 * j + lane);
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) same[j] += four[n] == static_cast<int>(list.index[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        several |= list.used[j] && same[j] > 1;
+        first[j] = list.used[j] && list.index[j] >= n.first && list.index[j] < n.first + n.live;
+        share[j] = q[j];
+    }
+    // a word that stands in several entries is written by the first of them, with all their shares
+    if (__any(several)) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) share[j] = 0.0f;
+        for (int i = 0; i < a.teacher.entries; ++i) {
+            const int word_i = words[wave][i];
+            const float share_i = shares[wave][i];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const bool its = list.used[j] && word_i == static_cast<int>(list.index[j]);
+                share[j] += its ? share_i : 0.0f;
+                first[j] &= !(its && i < 64 * j + lane);
+            }
         }
     }
 #pragma unroll
