@@ -259,7 +259,8 @@ typedef struct {
  *     loss[r] = sum_k q_k (log q_k - log p_{index_k}),  lse[r] = log sum_v exp(l_v / temperature),
  *     picked[r * entries + k] = l_{index_k}  (0 where the entry counts nothing)
  * A masked row has loss 0.  An index beyond the vocabulary gives loss and picked NaN.  The student's logits are
- * not stored.  The loss is not multiplied by the temperature's square; dloss may be.
+ * kept only while there are few of them (workspaces hold at most 256 MB of them).  The loss is not multiplied by the
+ * temperature's square; dloss may be.
  * Errors: EINVAL (NULL, alignment, strides, sizes, temperature, workspace too small), EDEVICE.
  *
  * Backward, for the upstream gradients dloss[r] (device, fp32), from lse and picked of the forward pass:
@@ -273,7 +274,8 @@ typedef struct {
 int eager_distillation(int dtype, const eager_projection *shape, const void *x, const void *w,
                        const eager_teacher *teacher, float *loss, float *lse, float *picked, void *workspace,
                        int64_t workspace_bytes, void *stream);
-int eager_distillation_workspace_bytes(int dtype, const eager_projection *shape, int backward, int64_t *bytes);
+int eager_distillation_workspace_bytes(int dtype, const eager_projection *shape, int32_t entries, int backward,
+                                       int64_t *bytes);
 int eager_distillation_backward(int dtype, const eager_projection *shape, const void *x, const void *w,
                                 const eager_teacher *teacher, const float *lse, const float *picked,
                                 const float *dloss, void *dx, void *dw, void *workspace, int64_t workspace_bytes,

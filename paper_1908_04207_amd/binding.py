@@ -188,7 +188,7 @@ def _load() -> ctypes.CDLL:
     lib.eager_rotary.argtypes = [i32, Pk, H, H, Rt, i32, i32, H, H, vp]
     lib.eager_rotary_backward.argtypes = [i32, Pk, H, H, Rt, i32, i32, H, H, vp]
     lib.eager_distillation.argtypes = [i32, Pj, vp, vp, Te, vp, vp, vp, vp, i64, vp]
-    lib.eager_distillation_workspace_bytes.argtypes = [i32, Pj, i32, ctypes.POINTER(i64)]
+    lib.eager_distillation_workspace_bytes.argtypes = [i32, Pj, i32, i32, ctypes.POINTER(i64)]
     lib.eager_distillation_backward.argtypes = [i32, Pj, vp, vp, Te, vp, vp, vp, vp, vp, vp, i64, vp]
     return lib
 
@@ -707,9 +707,9 @@ def eager_distillation(dtype: int, shape: Projection, x, w, teacher: Teacher, lo
                                    _ptr(workspace), workspace_bytes, _stream(stream)), "eager_distillation")
 
 
-def eager_distillation_workspace_bytes(dtype: int, shape: Projection, backward: bool) -> int:
+def eager_distillation_workspace_bytes(dtype: int, shape: Projection, entries: int, backward: bool) -> int:
     return _workspace_bytes(lib.eager_distillation_workspace_bytes, "eager_distillation_workspace_bytes", dtype, shape,
-                            int(backward))
+                            entries, int(backward))
 
 
 def eager_distillation_backward(dtype: int, shape: Projection, x, w, teacher: Teacher, lse, picked, dloss, dx, dw, workspace,

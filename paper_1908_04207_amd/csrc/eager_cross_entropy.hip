@@ -70,7 +70,9 @@ struct Product {
     int counted_k;           // they are k, not the rows of b
 };
 
-enum Epilogue { kStats, kDlogits, kSums, kResult };
+enum Epilogue { kStats, kKept, kDlogits, kSums, kResult };          // kKept: kStats, and the logits too
+
+constexpr bool gives_statistics(int epilogue) { return epilogue == kStats || epilogue == kKept; }
 
 // A tile of one side has Rows * 128 bytes whatever the layout: kDepth values of k are 128 bytes.
 template <typename T> constexpr int kDepth = 128 / sizeof(T);
@@ -161,7 +163,7 @@ __device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b
     const int wave_a = wave % WM * (BM / WM), wave_b = wave / WM * (BN / WN);
     Side a_side = p.a, b_side = p.b;
     int all_steps = p.all_steps;
-    if (Epi != kStats) {
+    if (!gives_statistics(Epi)) {
         const int counted = *p.counted;
         if (p.counted_k) {
             a_side.k = b_side.k = counted;
@@ -235,13 +237,30 @@ __device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b
     __syncthreads();
 
     const int half = lane >> 5;
-    if (Epi == kStats) {
+    if (gives_statistics(Epi)) {
+        if (Epi == kKept) {
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                const long long row = b0 + wave_b + 32 * j + (lane & 31), from = a0 + wave_a + 4 * half;
+                float *const to = static_cast<float *>(p.out) + row * p.out_stride + from;
+                const int left = row < p.b.rows ? static_cast<int>(min(p.live - from, static_cast<long long>(BM))) : 0;
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        f32x4 x;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = c[i][j][4 * r + e];
+                        if (32 * i + 8 * r < left) *reinterpret_cast<f32x4 *>(to + 32 * i + 8 * r) = x;
+                    }
+            }
+        }
         float2 *parts = reinterpret_cast<float2 *>(tile0);             // [WM][BN]
         const int live = static_cast<int>(min(p.live - a0, static_cast<long long>(BM))) - wave_a - 4 * half;
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
             const long long row = b0 + wave_b + 32 * j + (lane & 31);
-            const long long target = row < p.b.rows ? p.target[row] : -1;
+            const long long target = Epi == kStats && row < p.b.rows ? p.target[row] : -1;
             // the target's place among the lane's results, if it has it
             const long long from = target - a0 - wave_a - 4 * half;
             const int at = from >= 0 && from < min(live, 32 * MI) ? static_cast<int>(from) : -1;
@@ -463,7 +482,7 @@ template <typename T, typename Shape, int Epi>
 __global__ __launch_bounds__(Shape::Threads) void logits_kernel(const Product p)
 {
     EAGER_TILES;
-    const int rows = Epi == kStats ? static_cast<int>(p.b.rows) : *p.counted, tiles_b = (rows + Shape::B - 1) / Shape::B;
+    const int rows = gives_statistics(Epi) ? static_cast<int>(p.b.rows) : *p.counted, tiles_b = (rows + Shape::B - 1) / Shape::B;
     const int all = p.tiles_a * tiles_b;
     int id = blockIdx.x, tile_a, tile_b;
     if constexpr (Shape::Quartered) {
@@ -682,9 +701,11 @@ hipError_t forward(const CrossEntropyArgs &a, hipStream_t stream)
 {
     const int shape = logits_shape(a.rows, a.width, a.vocab, sizeof(T));
     const bool taught = a.teacher.index;
-    // a teacher's favourite takes the target's place
+    const bool kept = taught && keeps_logits(a.rows, a.width, a.vocab, a.teacher.entries, sizeof(T));
+    const long long own = taught ? teacher_bytes(a.rows, a.vocab, kept) : 0;
+    // a teacher's favourite takes the target's place, or the logits are kept and the entries' taken from them
     long long *const favourite = reinterpret_cast<long long *>(a.workspace);
-    if (taught) {
+    if (taught && !kept) {
         const hipError_t e = launch_picked(a, favourite, sizeof(T) == 2, stream);
         if (e != hipSuccess) return e;
     }
@@ -696,11 +717,16 @@ hipError_t forward(const CrossEntropyArgs &a, hipStream_t stream)
     p.live = a.vocab;
     p.scale = taught ? kLog2e / a.teacher.temperature : kLog2e;
     p.target = taught ? favourite : a.target;
-    p.stats = reinterpret_cast<float2 *>(a.workspace + (taught ? teacher_target_bytes(a.rows) : 0));
+    p.out = a.workspace;
+    p.out_stride = round_up(a.vocab, 4);
+    p.stats = reinterpret_cast<float2 *>(a.workspace + own);
     p.right = reinterpret_cast<float *>(p.stats + tiles * a.rows);
-    const hipError_t e = launch_logits<T, kStats>(p, shape, stream);
+    const hipError_t e = kept ? launch_logits<T, kKept>(p, shape, stream) : launch_logits<T, kStats>(p, shape, stream);
     if (e != hipSuccess) return e;
-    if (taught) return launch_divergence(a, p.stats, p.right, favourite, static_cast<int>(tiles), p.scale, stream);
+    if (taught) {
+        const Tiled t = {p.stats, p.right, favourite, static_cast<const float *>(p.out), p.out_stride, static_cast<int>(tiles), p.scale};
+        return launch_divergence(a, t, kept, stream);
+    }
     const float2 *stats = p.stats;
     const float *right = p.right;
     return launch(rows_kernel, dim3(static_cast<unsigned>((a.rows + kJoined - 1) / kJoined)), dim3(1024), 0, stream, stats, right,

@@ -18,14 +18,24 @@ struct Entries {
     float scale;                     // log2(e) / temperature
 };
 
+// What there is for the losses: the tiles' statistics, and all logits or the favourites' as the tiles have them.
+struct Tiled {
+    const float2 *stats;             // [tiles][rows]
+    const float *right;
+    const long long *favourite;
+    const float *logits;
+    long long stride;                // of the logits
+    int tiles;
+    float scale;                     // log2(e) / temperature
+};
+
 // Student's logits of the entries, and the word that each row's teacher favours: -1 without an entry that counts, the
 // vocabulary's size where an index is beyond it.
 hipError_t launch_picked(const CrossEntropyArgs &a, long long *favourite, bool bf16, hipStream_t stream);
 // The latter alone.
 hipError_t launch_favourites(const CrossEntropyArgs &a, long long *favourite, hipStream_t stream);
-// Losses and log-sum-exps from the tiles' statistics; right: the favourite's logit as the tiles have it.
-hipError_t launch_divergence(const CrossEntropyArgs &a, const float2 *stats, const float *right, const long long *favourite,
-                             int tiles, float scale, hipStream_t stream);
+// Losses and log-sum-exps; kept: the entries' logits too, from all logits, else launch_picked was before.
+hipError_t launch_divergence(const CrossEntropyArgs &a, const Tiled &t, bool kept, hipStream_t stream);
 // The entries' gradients of logits in place of those of words that no list has.
 hipError_t launch_entries(const CrossEntropyArgs &a, const Entries &n, bool bf16, hipStream_t stream);
 

@@ -5,14 +5,14 @@
 //   loss = sum q (log q - log p),  dl = dloss / temperature (p - q)
 //
 // The products are those of the cross entropy, with the word that the teacher favours in the target's place: tiles
-// leave statistics forward, dl without q backward.  What is left for here: the student's logits of the entries, one
-// dot product each, in the forward pass; the losses; and the entries' dl, which replace what the tiles wrote there,
-// as p - q is to be rounded and not p.
+// leave statistics forward, dl without q backward.  What is left for here: the student's logits of the entries in the
+// forward pass, one dot product each, or out of all logits where these are few enough to be kept (keeps_logits); the
+// losses; and the entries' dl, which replace what the tiles wrote there, as p - q is to be rounded and not p.
 //
 // Bound by the products (see there).  Measured, us, 4096 x 1024 x 50257 in bf16 with 64 entries a row: picked logits 39 (435 MB of
 // the projection's rows at 11 TB/s, most from second-level caches; 61 with fmaf for dot instructions and 64 lanes an entry), divergences 7, favourites 5,
 // entries of dl 12, beside 910 of logits, twice, and 830 of dx and dw; 1019 rows in fp32 with 32 entries 16.5, 6.5, 5 and 7.5 beside
-// 1305 and 1180; 61 rows in bf16 with 16 entries 4 and 5.7 beside 19; 300 x 512 x 3000 in bf16 with 128 entries 6.8, 5, 3.3 and 8.2 (27
+// 1305 and 1180; 300 x 512 x 3000 in bf16 with 128 entries entries of dl 8.2 (27
 // where every list was searched for repeated words with their shares) beside 22 and 10.
 //
 // Differences are formed where they keep their digits: log p from a logit's distance to the row's largest, and the
@@ -156,21 +156,29 @@ __global__ __launch_bounds__(256) void favourites_kernel(const CrossEntropyArgs 
 }
 
 // kJoined rows a workgroup: their statistics, then a wavefront for each row's entries (whose loads come first).
-template <int N>
-__global__ __launch_bounds__(1024) void divergence_kernel(const CrossEntropyArgs a, const float2 *stats, const float *right,
-                                                          const long long *favourite, int tiles, float scale)
+template <int N, bool Kept>
+__global__ __launch_bounds__(1024) void divergence_kernel(const CrossEntropyArgs a, const Tiled t)
 {
     __shared__ float2 part[16][kJoined];
     __shared__ float tops[kJoined], logs[kJoined];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long row = static_cast<long long>(blockIdx.x) * kJoined + wave, there = min(row, a.rows - 1);
     const List<N> list(a.teacher, there, lane);
-    const long long word = favourite[there];
-    const float its = right[there];
+    const long long word = Kept ? list.favourite(a.vocab, lane) : t.favourite[there];
+    const float right = Kept ? 0.0f : t.right[there];
     float l[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) l[j] = list.used[j] ? a.teacher.picked[there * a.teacher.entries + 64 * j + lane] : 0.0f;
-    const float2 all = joined_statistics(stats, a.rows, tiles, part);
+    for (int j = 0; j < N; ++j) {
+        const int k = 64 * j + lane;
+        if (Kept) {
+            const bool known = list.used[j] && list.index[j] < a.vocab;
+            l[j] = known ? t.logits[there * t.stride + list.index[j]] : list.used[j] ? __builtin_nanf("") : 0.0f;
+            if (row < a.rows && k < a.teacher.entries) a.teacher.picked[row * a.teacher.entries + k] = l[j];
+        } else {
+            l[j] = list.used[j] ? a.teacher.picked[there * a.teacher.entries + k] : 0.0f;
+        }
+    }
+    const float2 all = joined_statistics(t.stats, a.rows, t.tiles, part);
     if (threadIdx.x < kJoined) {
         const long long mine = static_cast<long long>(blockIdx.x) * kJoined + threadIdx.x;
         const float log_sum = log1pf(all.y - 1.0f);
@@ -188,7 +196,7 @@ __global__ __launch_bounds__(1024) void divergence_kernel(const CrossEntropyArgs
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         // logarithms to base two, of q without its sum
-        distance[j] = list.used[j] ? (list.logit[j] - top) * scale : 0.0f;
+        distance[j] = list.used[j] ? (list.logit[j] - top) * t.scale : 0.0f;
         e[j] = list.used[j] ? exp2_fast(distance[j]) : 0.0f;
         sum += e[j];
     }
@@ -197,7 +205,9 @@ __global__ __launch_bounds__(1024) void divergence_kernel(const CrossEntropyArgs
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         if (!list.used[j]) continue;
-        const float apart = distance[j] - fmaf(list.index[j] == word ? its : l[j], scale, -tops[wave]);
+        // the favourite's logit is the tiles' own, as the row's largest is
+        const float its = !Kept && list.index[j] == word ? right : l[j];
+        const float apart = distance[j] - fmaf(its, t.scale, -tops[wave]);
         const float term = e[j] / sum * (fmaf(apart, kLn2, logs[wave]) - log_q);
         loss += e[j] == 0.0f ? 0.0f : term;
     }
@@ -317,12 +327,11 @@ hipError_t launch_favourites(const CrossEntropyArgs &a, long long *favourite, hi
     });
 }
 
-hipError_t launch_divergence(const CrossEntropyArgs &a, const float2 *stats, const float *right, const long long *favourite,
-                             int tiles, float scale, hipStream_t stream)
+hipError_t launch_divergence(const CrossEntropyArgs &a, const Tiled &t, bool kept, hipStream_t stream)
 {
     return by_entries(a.teacher.entries, [&](auto n) {
-        return launch(divergence_kernel<n>, dim3(static_cast<unsigned>((a.rows + kJoined - 1) / kJoined)), dim3(1024), 0, stream, a,
-                      stats, right, favourite, tiles, scale);
+        return launch(kept ? divergence_kernel<n, true> : divergence_kernel<n, false>,
+                      dim3(static_cast<unsigned>((a.rows + kJoined - 1) / kJoined)), dim3(1024), 0, stream, a, t);
     });
 }
 

@@ -748,7 +748,7 @@ PyObject *py_distillation(PyObject *, PyObject *const *a, Py_ssize_t n)
     const eager_teacher teacher = {static_cast<int64_t *>(index.data), static_cast<float *>(logits.data),
                                    static_cast<int32_t>(index.size[1]), temperature};
     Workspace space;
-    if (model.taught_bytes(dtype, &shape, backward, &bytes) != EAGER_OK || !space.take(bytes, a[0])) return other_form();
+    if (model.taught_bytes(dtype, &shape, teacher.entries, backward, &bytes) != EAGER_OK || !space.take(bytes, a[0])) return other_form();
     float *p = static_cast<float *>(one.data), *q = static_cast<float *>(two.data), *r = static_cast<float *>(three.data);
     int st;
     Py_BEGIN_ALLOW_THREADS

@@ -333,10 +333,12 @@ int eager_cross_entropy_backward(int dtype, const eager_projection *shape, const
     return status_of(eager::launch_cross_entropy_backward(a, dtype == EAGER_BF16, static_cast<hipStream_t>(stream)));
 }
 
-int eager_distillation_workspace_bytes(int dtype, const eager_projection *shape, int backward, int64_t *bytes)
+int eager_distillation_workspace_bytes(int dtype, const eager_projection *shape, int32_t entries, int backward, int64_t *bytes)
 {
-    if (!valid_projection(dtype, shape) || shape->rows > kMaxTaught || !bytes || (backward != 0 && backward != 1)) return EAGER_EINVAL;
-    *bytes = eager::distillation_workspace_bytes(shape->rows, shape->width, shape->vocab, dtype == EAGER_BF16, backward);
+    if (!valid_projection(dtype, shape) || shape->rows > kMaxTaught || entries < 1 || entries > EAGER_MAX_ENTRIES || !bytes ||
+        (backward != 0 && backward != 1))
+        return EAGER_EINVAL;
+    *bytes = eager::distillation_workspace_bytes(shape->rows, shape->width, shape->vocab, entries, dtype == EAGER_BF16, backward);
     return EAGER_OK;
 }
 
@@ -347,7 +349,7 @@ int eager_distillation(int dtype, const eager_projection *shape, const void *x, 
     int64_t need = 0;
     if (!fill(a, dtype, shape, x, w, workspace, workspace_bytes) || !taught(a, teacher, shape->rows) ||
         (shape->rows && (!aligned(loss, 4) || !aligned(lse, 4) || !aligned(picked, 4))) ||
-        eager_distillation_workspace_bytes(dtype, shape, 0, &need) != EAGER_OK || workspace_bytes < need)
+        eager_distillation_workspace_bytes(dtype, shape, teacher->entries, 0, &need) != EAGER_OK || workspace_bytes < need)
         return EAGER_EINVAL;
     if (a.rows == 0) return EAGER_OK;
     a.loss = loss;
@@ -365,7 +367,7 @@ int eager_distillation_backward(int dtype, const eager_projection *shape, const 
     if (!fill(a, dtype, shape, x, w, workspace, workspace_bytes) || !taught(a, teacher, shape->rows) ||
         (shape->rows && (!aligned(lse, 4) || !aligned(picked, 4) || !aligned(dloss, 4))) || (!dx && !dw && shape->rows) ||
         (dx && !aligned(dx, 16)) || (dw && !aligned(dw, 16)) ||
-        eager_distillation_workspace_bytes(dtype, shape, 1, &need) != EAGER_OK || workspace_bytes < need)
+        eager_distillation_workspace_bytes(dtype, shape, teacher->entries, 1, &need) != EAGER_OK || workspace_bytes < need)
         return EAGER_EINVAL;
     a.lse = const_cast<float *>(lse);
     a.teacher.picked = const_cast<float *>(picked);

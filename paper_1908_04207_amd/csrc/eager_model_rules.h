@@ -159,9 +159,29 @@ inline long long cross_entropy_workspace_bytes(long long rows, int width, int vo
 // pass's arrays.
 inline long long teacher_target_bytes(long long rows) { return round_up(rows * 8, 256); }
 
-inline long long distillation_workspace_bytes(long long rows, int width, int vocab, bool bf16, bool backward)
+// The forward pass: whether all logits are kept, in fp32, and the entries' taken from them, or these are formed before as
+// dot products of their own.  Keeping them costs their bytes at 4 to 8 TB/s in the products' epilogue; forming them, a
+// launch and the projection's rows at 10 to 20 TB/s.  Measured, us of the whole pass, formed and kept: 8191 x 1600 x 1000
+// in bf16 with 64 entries 118 and 46; 300 x 512 x 3000 with 128 20.8 and 17.0; one row x 1024 x 50257 with one 28.6 and
+// 25.8; 4096 x 1024 x 8192 with 64 109 and 99; 61 x 1024 x 50257 with 16 30.4 and 29.8; 4096 x 1024 x 50257 with 64 459 and
+// 637, 1019 rows 131 and 169; 4096 x 328 x 8000 in fp32 with 4 146 and 155.
+// 256 MB of logits are the most that are kept, as this operator is for logits that are not to be stored.
+inline bool keeps_logits(long long rows, int width, int vocab, int entries, int bytes)
 {
-    return cross_entropy_workspace_bytes(rows, width, vocab, bf16, backward) + teacher_target_bytes(rows);
+    const double formed = 4 + static_cast<double>(rows) * entries * width * bytes / 12e6, kept = static_cast<double>(rows) * vocab;
+    return kept <= 1 << 26 && kept * 4 / 4e6 < formed;
+}
+
+// In front of the forward pass's arrays: the logits, or the favourites.
+inline long long teacher_bytes(long long rows, int vocab, bool kept)
+{
+    return kept ? round_up(rows * round_up(vocab, 4) * 4, 256) : teacher_target_bytes(rows);
+}
+
+inline long long distillation_workspace_bytes(long long rows, int width, int vocab, int entries, bool bf16, bool backward)
+{
+    const bool kept = !backward && keeps_logits(rows, width, vocab, entries, bf16 ? 2 : 4);
+    return cross_entropy_workspace_bytes(rows, width, vocab, bf16, backward) + teacher_bytes(rows, vocab, kept);
 }
 
 // Heads a workgroup takes at a time: two a group of lanes with 4 lanes a head in the forward pass,

@@ -569,7 +569,7 @@ def distillation(x, w, index, logits, temperature: float = 1.0):
     dtype = _dtype(x, w)
     shape = _sides(x, w)
     teacher = _teacher(x, index, logits, temperature)
-    nbytes = eb.eager_distillation_workspace_bytes(dtype, shape, False)
+    nbytes = eb.eager_distillation_workspace_bytes(dtype, shape, index.shape[1], False)
     with _on(x):
         eb.eager_distillation(dtype, shape, x, w, teacher, loss, lse, picked, _workspace(nbytes, x), nbytes)
     return loss, lse, picked
@@ -596,7 +596,7 @@ def distillation_backward(dloss, x, w, index, logits, lse, picked, temperature: 
             _expect(given, t.shape, t.dtype, t.device, name, False)
             if given.stride(1) != 1 or (t.shape[0] > 1 and given.stride(0) != t.stride(0)):
                 _refuse(f"{name}: expected strides {t.stride()}, got {given.stride()}")
-    nbytes = eb.eager_distillation_workspace_bytes(dtype, shape, True)
+    nbytes = eb.eager_distillation_workspace_bytes(dtype, shape, index.shape[1], True)
     with _on(x):
         eb.eager_distillation_backward(dtype, shape, x, w, teacher, lse, picked, dloss, dx, dw, _workspace(nbytes, x), nbytes)
     return dx, dw

@@ -114,8 +114,8 @@ static void teachers()
     const eager_projection shape = {70, 64, 999, 64, 72};
     const eager_teacher t = {static_cast<int64_t *>(at(0)), floats(1), 17, 3.0f};
     int64_t forward = 0, backward = 0;
-    CHECK(eager_distillation_workspace_bytes(EAGER_BF16, &shape, 0, &forward) == EAGER_OK);
-    CHECK(eager_distillation_workspace_bytes(EAGER_BF16, &shape, 1, &backward) == EAGER_OK);
+    CHECK(eager_distillation_workspace_bytes(EAGER_BF16, &shape, 17, 0, &forward) == EAGER_OK);
+    CHECK(eager_distillation_workspace_bytes(EAGER_BF16, &shape, 17, 1, &backward) == EAGER_OK);
     launches = 0;
     CHECK(eager_distillation(EAGER_BF16, &shape, at(2), at(3), &t, floats(4), floats(5), floats(6), at(7), forward, nullptr) == EAGER_OK);
     CHECK(launches == 1 && last_bf16 && loss.teacher.index == at(0) && loss.teacher.logits == at(1) && loss.teacher.entries == 17 &&

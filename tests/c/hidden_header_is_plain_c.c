@@ -29,7 +29,7 @@ int main(void)
     eager_angles angles = {0, 64, EAGER_ANGLES_PLAIN, 10000.0, 0.0, 0.0, 0.0, 0.0, 1.0};
     int64_t bytes = 0, more = 0;
     if (eager_layer_norm_workspace_bytes(EAGER_BF16, 1000, 1024, &bytes) != EAGER_OK || bytes < 2 * 1024 * 4) return 1;
-    if (eager_distillation_workspace_bytes(EAGER_F32, &projection, 1, &more) != EAGER_OK ||
+    if (eager_distillation_workspace_bytes(EAGER_F32, &projection, 16, 1, &more) != EAGER_OK ||
         eager_cross_entropy_workspace_bytes(EAGER_F32, &projection, 1, &bytes) != EAGER_OK || more < bytes + 800) return 2;
     if (eager_rotary_table(&angles, 0, 0, 0) != EAGER_OK) return 3;             /* a table of no positions */
     angles.part = 12;

@@ -31,8 +31,14 @@ int main()
                     for (int backward = 0; backward < 2; ++backward) {
                         const long long own = teacher_target_bytes(rows);
                         CHECK(own >= rows * 8 && own % 256 == 0);
-                        CHECK(distillation_workspace_bytes(rows, width, vocab, bf16, backward) ==
-                              own + cross_entropy_workspace_bytes(rows, width, vocab, bf16, backward));
+                        for (int entries : {1, 16, 256}) {
+                            const bool kept = !backward && keeps_logits(rows, width, vocab, entries, bf16 ? 2 : 4);
+                            const long long first = teacher_bytes(rows, vocab, kept);
+                            // quads of every row's logits, in front of statistics on 256 bytes
+                            if (kept) CHECK(first >= rows * ((vocab + 3) / 4 * 4) * 4 && first % 256 == 0 && rows * vocab <= 1 << 26);
+                            CHECK(distillation_workspace_bytes(rows, width, vocab, entries, bf16, backward) ==
+                                  first + cross_entropy_workspace_bytes(rows, width, vocab, bf16, backward));
+                        }
                     }
     std::puts("ok");
     return 0;

@@ -57,7 +57,8 @@ def _compare(ops, x, w, index, logits, g, tau):
     (8192, 8, 40003, 3, 1.0),        # several pieces
     (17003, 16, 300, 4, 2.0),        # rows counted by a kernel of their own
     (40, 1024, 2000, 33, 1.0),       # few rows: narrow tiles, dx in slices
-    (2100, 328, 4097, 12, 0.7)])
+    (2100, 328, 4097, 12, 0.7),
+    (2100, 328, 4097, 128, 0.7)])    # the same with all logits in the workspace
 def test_distillation(ops, dtype, rows, width, vocab, entries, tau):
     args = _inputs(rows, width, vocab, entries, dtype, rows + vocab)
     x, w, index, logits, g = args
@@ -80,7 +81,7 @@ def test_a_word_in_several_entries(ops, dtype, vocab):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("rows,vocab", [(300, 500), (20000, 64)])
+@pytest.mark.parametrize("rows,vocab", [(300, 500), (20000, 64), (3001, 2000)])
 def test_masked_rows_reach_no_gradient(ops, dtype, rows, vocab):
     """Whatever stands in rows without an entry or without a weight, and in entries that count nothing."""
     x, w, index, logits, g = _inputs(rows, 64, vocab, 12, dtype, 6, empty=0.0)
@@ -123,9 +124,10 @@ def test_all_rows_masked_and_no_rows(ops, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-def test_numbers_that_are_none(ops, dtype):
+@pytest.mark.parametrize("vocab", [200, 80000])
+def test_numbers_that_are_none(ops, dtype, vocab):
     """NaN and infinities of a teacher that count: the row says so, the others do not know."""
-    x, w, index, logits, g = _inputs(60, 64, 200, 6, dtype, 11, unused=0.0, empty=0.0)
+    x, w, index, logits, g = _inputs(60, 64, vocab, 6, dtype, 11, unused=0.0, empty=0.0)
     clean = _run(ops, x, w, index, logits, g, 1.0)
     logits[4, 2], logits[9, 0], logits[11] = math.nan, math.inf, math.nan
     bad = torch.zeros(60, dtype=torch.bool, device="cuda")

@@ -186,7 +186,7 @@ def test_distillation_refusals(dtype):
         for name in ("x", "w", "lse", "picked", "workspace"):
             _refused(lambda: call(**{name: None}))
             _refused(lambda: call(**{name: A + 2}))
-        need = eb.eager_distillation_workspace_bytes(dtype, shape(), backward_too)
+        need = eb.eager_distillation_workspace_bytes(dtype, shape(), 8, backward_too)
         _refused(lambda: call(workspace_bytes=need - 1))
     _refused(lambda: forward(loss=None))
     _refused(lambda: backward(dloss=None))
@@ -194,7 +194,8 @@ def test_distillation_refusals(dtype):
     _refused(lambda: backward(dx=A + 8))
     _refused(lambda: backward(dw=A + 8))
     forward(shape=shape(rows=0), x=None, teacher=teacher(index=None, logits=None), loss=None, lse=None, picked=None)
-    _refused(lambda: eb.eager_distillation_workspace_bytes(dtype, shape(rows=2 ** 25 + 1), False))
+    for bad in ((shape(rows=2 ** 25 + 1), 8), (shape(), 0), (shape(), 257), (None, 8)):
+        _refused(lambda: eb.eager_distillation_workspace_bytes(dtype, *bad, False))
 
 
 def test_tensors_off_the_gpu_are_refused():
