@@ -221,8 +221,9 @@ def rotary(x, cos, sin, positions, interleaved, back=False):
     return y, torch.where(moved, u * y.abs() + 2 * E * size, 0.0) * 1.01
 
 
-def distillation(x, w, index, logits, tau, dloss=None):
-    """dict of loss, lse, picked and, with dloss, dx, dw: (value, bound).  Words lie in the vocabulary or are negative."""
+def distillation(x, w, index, logits, tau, dloss=None, pieces=1):
+    """dict of loss, lse, picked and, with dloss, dx, dw: (value, bound).  Words lie in the vocabulary or are negative.
+    pieces: 2 where the gradients of logits are kept with what their first rounding leaves, rounded in turn."""
     u = U[x.dtype]
     x, w = x.to(F), w.to(F)
     rows, d = x.shape
@@ -255,8 +256,9 @@ def distillation(x, w, index, logits, tau, dloss=None):
     share_err.scatter_add_(1, at, q * q_err)
     g = torch.where(counted[:, 0], dloss.to(F), 0.0)[:, None] / tau
     dl = g * (p - share)
-    dl_err = u * dl.abs() + g.abs() * (p * (s_err + l_err / tau) + share_err + 4 * E * (p + share))
+    dl_err = u ** pieces * dl.abs() + g.abs() * (p * (s_err + l_err / tau) + share_err + 4 * E * (p + share))
     dx, dw = dl @ w, dl.t() @ x
-    result["dx"] = (dx, (dl_err @ w.abs() + (V + 8) * E * (dl.abs() @ w.abs())) * 1.01 + u * dx.abs())
-    result["dw"] = (dw, (dl_err.t() @ x.abs() + (rows + 8) * E * (dl.abs().t() @ x.abs())) * 1.01 + u * dw.abs())
+    # (two pieces are two terms of a sum each)
+    result["dx"] = (dx, (dl_err @ w.abs() + (pieces * V + 8) * E * (dl.abs() @ w.abs())) * 1.01 + u * dx.abs())
+    result["dw"] = (dw, (dl_err.t() @ x.abs() + (pieces * rows + 8) * E * (dl.abs().t() @ x.abs())) * 1.01 + u * dw.abs())
     return result

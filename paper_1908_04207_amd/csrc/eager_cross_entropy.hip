@@ -68,11 +68,18 @@ struct Product {
     float *others;           // [a tile][b row]: sums of p without the target's, or NULL
     const int *counted;      // device: rows of x that count (gather_kernel), or NULL: all of them
     int counted_k;           // they are k, not the rows of b
+    long long low;           // bytes from dl to what its rounding left, where that is kept
+    const float *common;     // factor that dl leaves out and its products put in
 };
 
-enum Epilogue { kStats, kKept, kDlogits, kSums, kResult };          // kKept: kStats, and the logits too
+// kKept: kStats, and the logits too.  kShared: kDlogits without the factor p.common.  kParted: kDlogits in two pieces, what
+// rounding leaves of each in the second
+enum Epilogue { kStats, kKept, kDlogits, kShared, kParted, kSums, kResult };
+// dl as the gradients' products find it
+enum Form { kPlain, kFactored, kTwice };
 
 constexpr bool gives_statistics(int epilogue) { return epilogue == kStats || epilogue == kKept; }
+constexpr bool gives_dlogits(int epilogue) { return epilogue == kDlogits || epilogue == kShared || epilogue == kParted; }
 
 // A tile of one side has Rows * 128 bytes whatever the layout: kDepth values of k are 128 bytes.
 template <typename T> constexpr int kDepth = 128 / sizeof(T);
@@ -121,6 +128,14 @@ struct Source {
         bytes -= advance;
         if (!Columns) chunks_left -= 8;
     }
+
+    // from the first of the last `tiles` on once more, `far` bytes away
+    __device__ __forceinline__ void again(int tiles, long long far)
+    {
+        base += far - tiles * advance;
+        bytes += tiles * advance;
+        if (!Columns) chunks_left += 8 * tiles;
+    }
 };
 
 template <typename T, int Rows, bool Columns>
@@ -152,7 +167,7 @@ __device__ __forceinline__ void place(int n, int tiles_a, int tiles_b, int &tile
 // turns: while one is multiplied, the next is on its way into the other.  A step's operands are
 // read while the step before is multiplied, the first step's of a tile during the last one of the
 // tile before, so the barrier between tiles stands in the shadow of matrix instructions.
-template <typename T, typename Shape, bool ColumnsA, bool ColumnsB, int Epi>
+template <typename T, typename Shape, bool ColumnsA, bool ColumnsB, int Epi, int Form = kPlain>
 __device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b, int slice, char *tile0, char *tile1)
 {
     constexpr int BM = Shape::A, BN = Shape::B, WM = Shape::WavesA, WN = Shape::WavesB;
@@ -174,11 +189,15 @@ __device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b
         }
     }
     const int first = slice * p.steps;
-    const int count = max(0, min(p.steps, all_steps - first));
+    const int once = max(0, min(p.steps, all_steps - first)), count = Form == kTwice ? 2 * once : once;
     const long long k0 = static_cast<long long>(first) * kDepth<T>;
     Source<T, BM, ColumnsA, Waves> side_a(a_side, a0, k0, wave, lane);
     Source<T, BN, ColumnsB, Waves> side_b(b_side, b0, k0, wave, lane);
     auto stage = [&](char *tile, int t) {
+        if (Form == kTwice && t == once) {                             // b's second pieces
+            side_a.again(once, 0);
+            side_b.again(once, p.low);
+        }
         side_a.load(tile, t < count);
         side_b.load(tile + BM * 128, t < count);
     };
@@ -325,7 +344,7 @@ __device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b
     };
     const int live = static_cast<int>(min(p.live - a0, static_cast<long long>(BM)));
     const long long rows = Epi == kResult ? p.live : b_side.rows;
-    if constexpr (Epi == kDlogits) {
+    if constexpr (gives_dlogits(Epi)) {
         float g[NI], others[NI], scale[NI];
         int target[NI];
 #pragma unroll
@@ -337,6 +356,7 @@ __device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b
                 const long long v = p.target[row], from = v - p.first - a0;
                 lse = p.lse[row] * kLog2e;
                 g[j] = v >= p.vocab ? __builtin_nanf("") : p.dloss[row];
+                if (Epi == kShared) g[j] /= *p.common;
                 target[j] = from >= wave_a && from < wave_a + 32 * MI ? static_cast<int>(from) : -1;
             }
 #pragma unroll
@@ -431,12 +451,19 @@ __device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b
                 for (int r = 0; r < 16; ++r) c[i][j][r] *= by;
         }
     }
+    if (Epi == kResult && Form == kFactored) {
+        const float by = *p.common;
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int i = 0; i < MI; ++i) c[i][j] *= by;
+    }
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
         const int in_b = wave_b + 32 * j + (lane & 31);
         const long long row = b0 + in_b;
         const long long from = a0 + wave_a + 4 * half;
-        const int limit = Epi == kDlogits ? BM : row < rows ? static_cast<int>(min(p.a.rows - from, static_cast<long long>(BM))) : 0;
+        const int limit = gives_dlogits(Epi) ? BM : row < rows ? static_cast<int>(min(p.a.rows - from, static_cast<long long>(BM))) : 0;
         float *const sums = static_cast<float *>(p.out) + (slice * p.b.rows + row) * p.out_stride + from;
         T *const out = static_cast<T *>(p.out) + row * p.out_stride + from;
 #pragma unroll
@@ -459,16 +486,35 @@ __device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b
                 }
             }
     }
-    if (Across) {
+    auto store_across = [&](char *to) {
         __syncthreads();
 #pragma unroll 4
         for (int id = threadIdx.x; id < BN * RowChunks; id += 64 * Waves) {
             const int in_b = id / RowChunks, chunk = id % RowChunks;
             const long long row = b0 + in_b, at = a0 + chunk * 8;
-            if (Epi == kDlogits || (row < rows && at < p.a.rows))
-                *reinterpret_cast<bf16x8 *>(static_cast<T *>(p.out) + row * p.out_stride + at) =
+            if (gives_dlogits(Epi) || (row < rows && at < p.a.rows))
+                *reinterpret_cast<bf16x8 *>(reinterpret_cast<T *>(to) + row * p.out_stride + at) =
                     *reinterpret_cast<const bf16x8 *>(place_of(in_b, chunk));
         }
+    };
+    if (Across) store_across(static_cast<char *>(p.out));
+    if constexpr (Epi == kParted) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            const int in_b = wave_b + 32 * j + (lane & 31);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    f32x4 x;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = c[i][j][4 * r + e];
+                    x -= __builtin_convertvector(to_quad(x, type), f32x4);
+                    *reinterpret_cast<quad *>(place_of(in_b, (wave_a + 32 * i + 8 * r) >> 3) + 8 * half) = to_quad(x, type);
+                }
+        }
+        store_across(static_cast<char *>(p.out) + p.low);
     }
 }
 
@@ -504,24 +550,24 @@ __global__ __launch_bounds__(Shape::Threads) void logits_kernel(const Product p)
 }
 
 // The tile of workgroup `id` of a product in slices.
-template <typename T, typename Shape, bool ColumnsB, int Epi>
+template <typename T, typename Shape, bool ColumnsB, int Epi, int Form>
 __device__ __forceinline__ void gradient(const Product &p, int id, char *tile0, char *tile1)
 {
     const int all = p.tiles_a * p.tiles_b, slice = id / all;
     int tile_a, tile_b;
     place(in_order(id - slice * all, all), p.tiles_a, p.tiles_b, tile_a, tile_b);
-    product<T, Shape, true, ColumnsB, Epi>(p, tile_a, tile_b, slice, tile0, tile1);
+    product<T, Shape, true, ColumnsB, Epi, Form>(p, tile_a, tile_b, slice, tile0, tile1);
 }
 
 // dw and dx of a piece in one launch: what one leaves idle in its last round the other fills.
 // SumsOfDw: dw in slices of the rows, as sums in the workspace.
-template <typename T, typename Shape, bool SumsOfDw>
+template <typename T, typename Shape, bool SumsOfDw, int Form>
 __global__ __launch_bounds__(Shape::Threads) void gradients_kernel(const Product dw, const Product dx, int dw_tiles)
 {
     EAGER_TILES;
     const int id = blockIdx.x;
-    if (id < dw_tiles) gradient<T, Shape, true, SumsOfDw ? kSums : kResult>(dw, id, tile0, tile1);
-    else gradient<T, Shape, false, kSums>(dx, id - dw_tiles, tile0, tile1);
+    if (id < dw_tiles) gradient<T, Shape, true, SumsOfDw ? kSums : kResult, Form>(dw, id, tile0, tile1);
+    else gradient<T, Shape, false, kSums, Form>(dx, id - dw_tiles, tile0, tile1);
 }
 
 // loss and lse of 16 rows from the tiles' statistics: 64 threads a row share the tiles, four loads of each under way at
@@ -557,6 +603,7 @@ struct Gather {
     float *lse_out, *dloss_out;
     int *place;              // per row: where it went, -1: nowhere
     int *counted;
+    float *common;           // the first weight with an exponent of 0, or NULL
 };
 
 __device__ __forceinline__ bool counts(const Gather &g, long long row) { return (g.target[row] >= 0) & (g.dloss[row] != 0.0f); }
@@ -589,9 +636,14 @@ __global__ __launch_bounds__(1024) void gather_kernel(const Gather g)
         if (in) {
             g.target_out[to] = g.target[row];
             g.lse_out[to] = g.lse[row];
-            g.dloss_out[to] = g.dloss[row] * g.by;
+            const float weight = g.dloss[row] * g.by;
+            g.dloss_out[to] = weight;
+            if (g.common && to == 0) *g.common = __uint_as_float((__float_as_uint(weight) & 0x7fffff) | 0x3f800000);
         }
-        if (lane == 0 && first + kGathered >= g.rows) *g.counted = before + __popcll(mask);
+        if (lane == 0 && first + kGathered >= g.rows) {
+            *g.counted = before + __popcll(mask);
+            if (g.common && before == 0 && mask == 0) *g.common = 1.0f;
+        }
     }
     __syncthreads();
     constexpr int E = 16 / sizeof(T);
@@ -656,8 +708,9 @@ struct Sums {
     void *out;
     long long stride, rows, rows_padded;
     int slices;
+    const float *common;     // factor
 };
-template <typename T>
+template <typename T, bool Factored>
 __global__ __launch_bounds__(256) void sums_kernel(const Sums dx, const Sums dw, int width)
 {
     const Sums &s = blockIdx.y ? dw : dx;
@@ -671,6 +724,7 @@ __global__ __launch_bounds__(256) void sums_kernel(const Sums dx, const Sums dw,
         x = *from;
 #pragma unroll 4
         for (int n = 1; n < s.slices; ++n) x += from[n * s.rows_padded * quads];
+        if (Factored) x *= *s.common;
     }
     *reinterpret_cast<typename Operand<T>::quad *>(static_cast<T *>(s.out) + row * s.stride + at) = to_quad(x, static_cast<T *>(nullptr));
 }
@@ -694,6 +748,15 @@ hipError_t launch_logits(Product &p, int shape, hipStream_t stream)
     if (shape == kLarge) return launch(logits_kernel<T, Large, Epi>, grid, dim3(Large::Threads), 0, stream, p);
     if (shape == kMedium) return launch(logits_kernel<T, Medium, Epi>, grid, dim3(Medium::Threads), 0, stream, p);
     return launch(logits_kernel<T, Narrow, Epi>, grid, dim3(Narrow::Threads), 0, stream, p);
+}
+
+template <typename T, int Form>
+hipError_t launch_gradients(const Cut &c, const Product &dw, const Product &dx, int dw_tiles, dim3 grid, hipStream_t stream)
+{
+    if (c.gradients == kLarge)
+        return launch(gradients_kernel<T, Large, false, Form>, grid, dim3(Large::Threads), 0, stream, dw, dx, dw_tiles);
+    return launch(c.dw_slices > 1 ? gradients_kernel<T, Medium, true, Form> : gradients_kernel<T, Medium, false, Form>, grid,
+                  dim3(Medium::Threads), 0, stream, dw, dx, dw_tiles);
 }
 
 template <typename T>
@@ -737,14 +800,18 @@ template <typename T>
 hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
 {
     hipError_t e = hipSuccess;
-    const Cut c = cut_of(a.rows, a.width, a.vocab, sizeof(T));
+    constexpr bool Rounded = sizeof(T) == 2;
+    const bool taught = a.teacher.index;
+    const Form form = !taught || !Rounded ? kPlain : dlogits_pieces(a.rows, a.width, a.vocab, sizeof(T)) == 2 ? kTwice : kFactored;
+    const Cut c = cut_of(a.rows, a.width, a.vocab, sizeof(T), form == kTwice ? 2 : 1);
     const Layout l = layout_of(c, a.rows, a.width, sizeof(T));
+    const long long low = l.end + teacher_target_bytes(a.rows) - l.dl;       // behind the favourites
     const T *w = static_cast<const T *>(a.w);
     T *dl = reinterpret_cast<T *>(a.workspace + l.dl), *x = reinterpret_cast<T *>(a.workspace + l.x);
     float *sums = reinterpret_cast<float *>(a.workspace + l.dx_sums), *dw_sums = reinterpret_cast<float *>(a.workspace + l.dw_sums);
     int *counted = reinterpret_cast<int *>(a.workspace + l.counted), *place = reinterpret_cast<int *>(a.workspace + l.place);
+    float *const common = form == kFactored ? reinterpret_cast<float *>(counted + 4) : nullptr;
     Sums of_dx = {}, of_dw = {};
-    const bool taught = a.teacher.index;
     const float scale = taught ? kLog2e / a.teacher.temperature : kLog2e;
     const long long *target = a.target;
     if (taught) {
@@ -754,7 +821,7 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
     }
     Gather g = {a.x, target, a.lse, a.dloss, a.rows, a.x_stride, a.width, taught ? 1.0f / a.teacher.temperature : 1.0f, nullptr, x,
                 reinterpret_cast<long long *>(a.workspace + l.target), reinterpret_cast<float *>(a.workspace + l.lse),
-                reinterpret_cast<float *>(a.workspace + l.dloss), place, counted};
+                reinterpret_cast<float *>(a.workspace + l.dloss), place, counted, common};
     if (e == hipSuccess && a.rows > kCountedByEach) {
         int *before = reinterpret_cast<int *>(a.workspace + l.before);
         e = launch(before_kernel, dim3(1), dim3(1024), 0, stream, g, before);
@@ -784,9 +851,13 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
             p.out = dl;
             p.out_stride = padded;
             p.others = c.pieces == 1 && !p.whole ? reinterpret_cast<float *>(a.workspace + l.others) : nullptr;
-            e = launch_logits<T, kDlogits>(p, c.logits, stream);
+            p.low = form == kTwice ? low : 0;
+            p.common = common;
+            if (form == kTwice) e = launch_logits<T, Rounded ? kParted : kDlogits>(p, c.logits, stream);
+            else if (form == kFactored) e = launch_logits<T, Rounded ? kShared : kDlogits>(p, c.logits, stream);
+            else e = launch_logits<T, kDlogits>(p, c.logits, stream);
             if (e == hipSuccess && taught) {
-                const Entries n = {place, g.target_out, g.lse_out, g.dloss_out, p.others, p.tiles_a, dl, padded, first, live, scale};
+                const Entries n = {place, g.target_out, g.lse_out, g.dloss_out, common, p.others, p.tiles_a, dl, p.low, padded, first, live, scale};
                 e = launch_entries(a, n, sizeof(T) == 2, stream);
             } else if (e == hipSuccess && p.others)
                 e = launch(targets_kernel<T>, dim3(static_cast<unsigned>((a.rows + kJoined - 1) / kJoined)), dim3(1024), 0, stream, p, dl);
@@ -799,6 +870,7 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
             dx.a = {w + first * a.w_stride, a.w_stride, a.width, live};
             dx.b = {dl, padded, a.rows, round_up(live, 16 / sizeof(T))};
             dx.counted = counted;
+            dx.low = low;
             dx.slices = c.dx_slices;
             dx.out = sums;
             dx.out_stride = a.width;
@@ -808,6 +880,8 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
         if (a.dw) {
             dw.a = {x, a.width, a.width, a.rows};
             dw.counted = counted;
+            dw.low = low;
+            dw.common = common;
             dw.counted_k = 1;
             dw.b = {dl, padded, padded, a.rows};
             dw.slices = c.dw_slices;
@@ -819,18 +893,16 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
         }
         const dim3 grid(dx_tiles + dw_tiles);
         if (!(dx_tiles + dw_tiles)) continue;
-        if (c.gradients == kLarge)
-            e = launch(gradients_kernel<T, Large, false>, grid, dim3(Large::Threads), 0, stream, dw, dx, dw_tiles);
-        else
-            e = launch(c.dw_slices > 1 ? gradients_kernel<T, Medium, true> : gradients_kernel<T, Medium, false>, grid,
-                       dim3(Medium::Threads), 0, stream, dw, dx, dw_tiles);
+        if (form == kTwice) e = launch_gradients<T, Rounded ? kTwice : kPlain>(c, dw, dx, dw_tiles, grid, stream);
+        else if (form == kFactored) e = launch_gradients<T, Rounded ? kFactored : kPlain>(c, dw, dx, dw_tiles, grid, stream);
+        else e = launch_gradients<T, kPlain>(c, dw, dx, dw_tiles, grid, stream);
     }
     if (e != hipSuccess) return e;
-    if (a.dx && a.rows) of_dx = {sums, place, a.dx, a.x_stride, a.rows, a.rows, c.dx_slices};
-    if (a.dw && c.dw_slices > 1) of_dw = {dw_sums, nullptr, a.dw, a.w_stride, a.vocab, of_dw.rows_padded, c.dw_slices};
+    if (a.dx && a.rows) of_dx = {sums, place, a.dx, a.x_stride, a.rows, a.rows, c.dx_slices, common};
+    if (a.dw && c.dw_slices > 1) of_dw = {dw_sums, nullptr, a.dw, a.w_stride, a.vocab, of_dw.rows_padded, c.dw_slices, common};
     const long long quads = std::max(of_dx.rows, of_dw.rows) * (a.width / 4);
     if (!quads) return hipSuccess;
-    return launch(sums_kernel<T>, dim3(static_cast<unsigned>((quads + 255) / 256), of_dw.rows ? 2 : 1), dim3(256), 0, stream, of_dx,
+    return launch(form == kFactored ? sums_kernel<T, Rounded> : sums_kernel<T, false>, dim3(static_cast<unsigned>((quads + 255) / 256), of_dw.rows ? 2 : 1), dim3(256), 0, stream, of_dx,
                   of_dw, a.width);
 }
 

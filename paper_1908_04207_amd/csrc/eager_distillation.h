@@ -10,9 +10,11 @@ struct Entries {
     const int *place;                // per row: its place among those that count, -1: none
     const long long *favourite;      // of a place, as lse and dloss (the latter over the temperature)
     const float *lse, *dloss;
+    const float *common;             // factor that dl leaves out, or NULL
     const float *others;             // [tiles][rows]: sums of p without the favourite's, or NULL
     int tiles;
     void *dl;
+    long long low;                   // bytes from dl to its second pieces, 0: there are none
     long long stride, first;         // first: word of dl's column 0
     int live;                        // words of the piece
     float scale;                     // log2(e) / temperature

@@ -15,6 +15,12 @@
 // 1305 and 1180; 300 x 512 x 3000 in bf16 with 128 entries entries of dl 8.2 (27
 // where every list was searched for repeated words with their shares) beside 22 and 10.
 //
+// dl beside bf16 inputs is bf16 itself, in two pieces for few rows (dlogits_pieces).  For more, what is rounded leaves out the
+// digits of the first row's weight, which the products' sums are multiplied by: a mean gives every row the same weight, and
+// rounded with it dl of all words that the student does not know yet (p - q near -1) would be off by the same part,
+// up to 2^-8, and so would be the gradients; numbers just below 1 are rounded by 2^-9 at most.  (Rows of one to three entries:
+// dx 0.0029 of its norm off before, 0.0021 since; no time.)
+//
 // Differences are formed where they keep their digits: log p from a logit's distance to the row's largest, and the
 // favourite's p - q, where p is beyond a half, from the sums of the others' q and p.
 #include "eager_distillation.h"
@@ -232,7 +238,7 @@ __global__ __launch_bounds__(1024) void entries_kernel(const CrossEntropyArgs a,
     for (int j = 0; j < N; ++j) p[j] = list.used[j] ? a.teacher.picked[there * a.teacher.entries + 64 * j + lane] : 0.0f;
     const int known = max(place, 0);
     const long long word = n.favourite[known];
-    const float lse = n.lse[known] * kLog2e, by = n.dloss[known];
+    const float lse = n.lse[known] * kLog2e, by = n.common ? n.dloss[known] / *n.common : n.dloss[known];
     if (n.others) {
         const long long mine = static_cast<long long>(blockIdx.x) * kJoined + threadIdx.x % kJoined;
         const float sum = joined_sums(n.others, mine < a.rows ? n.place[mine] : -1, a.rows, n.tiles, part);
@@ -295,7 +301,9 @@ __global__ __launch_bounds__(1024) void entries_kernel(const CrossEntropyArgs a,
         if (!first[j]) continue;
         float d = exp2_fast(fmaf(p[j], n.scale, -lse)) - share[j];
         if (n.others && list.index[j] == word && apart[wave] < 0.5f) d = rest - apart[wave];
-        static_cast<T *>(n.dl)[place * n.stride + list.index[j] - n.first] = static_cast<T>(d * by);
+        T *const at = static_cast<T *>(n.dl) + place * n.stride + list.index[j] - n.first;
+        *at = static_cast<T>(d * by);
+        if (n.low) *reinterpret_cast<T *>(reinterpret_cast<char *>(at) + n.low) = static_cast<T>(d * by - static_cast<float>(static_cast<T>(d * by)));
     }
 }
 

@@ -51,14 +51,15 @@ double logits_time(long long rows, int width, long long vocab, int bytes)
     return rounds * (round_up(width, 128 / bytes) / (128 / bytes) * c.step + c.rest);
 }
 
-// dw and dx of a piece: their tiles follow each other, so only the last round is not full
+// dw and dx of a piece: their tiles follow each other, so only the last round is not full.  They are gone through so many
+// times (two where dl is in two pieces).
 template <typename Shape>
-double gradients_time(long long rows, int width, long long live, int dw_slices, int dx_slices, int bytes)
+double gradients_time(long long rows, int width, long long live, int dw_slices, int dx_slices, int bytes, int times)
 {
     const Cost c = cost_of<Shape>(bytes);
     const long long depth = 128 / bytes, tiles_w = round_up(width, Shape::A) / Shape::A;
-    const double dw = ((rows + depth - 1) / depth + dw_slices - 1) / dw_slices * c.step + c.rest;
-    const double dx = ((live + depth - 1) / depth + dx_slices - 1) / dx_slices * c.step + c.rest;
+    const double dw = ((rows + depth - 1) / depth + dw_slices - 1) / dw_slices * times * c.step + c.rest;
+    const double dx = ((live + depth - 1) / depth + dx_slices - 1) / dx_slices * times * c.step + c.rest;
     const long long dw_tiles = tiles_w * (round_up(live, Shape::B) / Shape::B) * dw_slices;
     const long long dx_tiles = tiles_w * (round_up(rows, Shape::B) / Shape::B) * dx_slices;
     // a slice's sums are written, read and, from the second piece on, read again
@@ -85,11 +86,15 @@ inline int logits_shape(long long rows, int width, long long vocab, int bytes)
 
 constexpr int kSides[3][2] = {{Large::A, Large::B}, {Medium::A, Medium::B}, {Narrow::A, Narrow::B}};
 
-inline Cut cut_of(long long rows, int width, int vocab, int bytes)
+inline Cut cut_of(long long rows, int width, int vocab, int bytes, int times = 1)
 {
     const long long padded = round_up(std::max(rows, 1ll), 256);
     const long long fit = std::max(4096ll, (1ll << 29) / bytes / padded / 256 * 256);
     const long long fewest = (vocab + fit - 1) / fit;
+    // (what is gone through twice takes more slices while all of them run at once: 61 x 128 x 50257 67 us with 32, 55 with
+    // 64; 100 x 64 x 20000 40 with 64, 44 with 256)
+    const long long at_once = 256 / (round_up(std::max(rows, 1ll), 128) / 128 * (round_up(width, 128) / 128));
+    const int most = times > 1 ? static_cast<int>(std::clamp(at_once, 32ll, 64ll)) : 32;
     Cut best = {padded, 0, 1, 1, 0, 0, 0};
     double least = 0;
     for (long long n = fewest; n < fewest + 6; ++n) {
@@ -97,11 +102,11 @@ inline Cut cut_of(long long rows, int width, int vocab, int bytes)
         const int shape = logits_shape(rows, width, piece, bytes);
         const double logits = std::min({logits_time<Large>(rows, width, piece, bytes), logits_time<Medium>(rows, width, piece, bytes),
                                         logits_time<Narrow>(rows, width, piece, bytes)});
-        for (int dx = 1; dx <= 32; dx *= 2)
+        for (int dx = 1; dx <= most; dx *= 2)
             for (int dw = 1; dw <= (pieces > 1 ? 1 : 32); dw *= 2)
                 for (int g = dw > 1 ? kMedium : kLarge; g <= kMedium; ++g) {
-                    const double one = g == kLarge ? gradients_time<Large>(rows, width, piece, dw, dx, bytes)
-                                                   : gradients_time<Medium>(rows, width, piece, dw, dx, bytes);
+                    const double one = g == kLarge ? gradients_time<Large>(rows, width, piece, dw, dx, bytes, times)
+                                                   : gradients_time<Medium>(rows, width, piece, dw, dx, bytes, times);
                     const double last = std::max(0.2, static_cast<double>(vocab - (pieces - 1) * piece) / piece);
                     const double cost = (logits + one) * (pieces > 1 ? pieces - 1 + last : 1);
                     if (!best.piece || cost < least) {
@@ -143,7 +148,7 @@ inline Layout layout_of(const Cut &c, long long rows, int width, int bytes)
     l.dloss = take(rows * 4);
     l.place = take(rows * 4);
     l.before = take((rows + kGathered - 1) / kGathered * 4);
-    l.counted = take(4);
+    l.counted = take(32);        // the number, and the factor that weights have in common
     l.end = at;
     return l;
 }
@@ -178,10 +183,25 @@ inline long long teacher_bytes(long long rows, int vocab, bool kept)
     return kept ? round_up(rows * round_up(vocab, 4) * 4, 256) : teacher_target_bytes(rows);
 }
 
+// The backward pass with bf16 inputs: whether dl goes into the products rounded to bf16, or in two pieces, the second what
+// the first one's rounding left.  The roundings of many entries average, to 0.0024 of the gradients' norm beside 0.0017 of
+// their own rounding; of few rows a few entries decide, and one in eight such batches had gradients 1.5 to 2.3 times as far
+// off as their own rounding.  Two pieces leave that one alone.  The backward pass, one piece and two, us: 2 x 848 x 469 29.3 and
+// 30.7; 159 x 312 x 330 29.4 and 31.6; 61 x 1024 x 50257 99 and 124; 500 x 1024 x 8192, which stays with one, 71 and 93.
+inline int dlogits_pieces(long long rows, int width, int vocab, int bytes)
+{
+    return bytes == 2 && (rows <= 128 || static_cast<double>(rows) * width * vocab <= 1 << 29) ? 2 : 1;
+}
+
 inline long long distillation_workspace_bytes(long long rows, int width, int vocab, int entries, bool bf16, bool backward)
 {
-    const bool kept = !backward && keeps_logits(rows, width, vocab, entries, bf16 ? 2 : 4);
-    return cross_entropy_workspace_bytes(rows, width, vocab, bf16, backward) + teacher_bytes(rows, vocab, kept);
+    const int bytes = bf16 ? 2 : 4;
+    if (!backward)
+        return teacher_bytes(rows, vocab, keeps_logits(rows, width, vocab, entries, bytes)) +
+               cross_entropy_workspace_bytes(rows, width, vocab, bf16, false);
+    const int pieces = dlogits_pieces(rows, width, vocab, bytes);
+    const Cut c = cut_of(rows, width, vocab, bytes, pieces);
+    return layout_of(c, rows, width, bytes).end + teacher_target_bytes(rows) + (pieces - 1) * c.rows_padded * c.piece * bytes;
 }
 
 // Heads a workgroup takes at a time: two a group of lanes with 4 lanes a head in the forward pass,

@@ -36,8 +36,16 @@ int main()
                             const long long first = teacher_bytes(rows, vocab, kept);
                             // quads of every row's logits, in front of statistics on 256 bytes
                             if (kept) CHECK(first >= rows * ((vocab + 3) / 4 * 4) * 4 && first % 256 == 0 && rows * vocab <= 1 << 26);
-                            CHECK(distillation_workspace_bytes(rows, width, vocab, entries, bf16, backward) ==
-                                  first + cross_entropy_workspace_bytes(rows, width, vocab, bf16, backward));
+                            const int bytes = bf16 ? 2 : 4, pieces = backward ? dlogits_pieces(rows, width, vocab, bytes) : 1;
+                            long long rest = cross_entropy_workspace_bytes(rows, width, vocab, bf16, backward);
+                            if (pieces == 2) {
+                                // second pieces behind all else, in the same order as the first ones
+                                const Cut c = cut_of(rows, width, vocab, bytes, 2);
+                                const Layout l = layout_of(c, rows, width, bytes);
+                                CHECK(bf16 && c.piece > 0 && l.others - l.dl >= c.rows_padded * c.piece * 2);
+                                rest = l.end + c.rows_padded * c.piece * 2;
+                            }
+                            CHECK(distillation_workspace_bytes(rows, width, vocab, entries, bf16, backward) == first + rest);
                         }
                     }
     std::puts("ok");

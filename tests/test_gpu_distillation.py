@@ -42,7 +42,8 @@ def _run(ops, x, w, index, logits, g, tau):
 
 
 def _compare(ops, x, w, index, logits, g, tau):
-    got, want = _run(ops, x, w, index, logits, g, tau), mo.distillation(x, w, index, logits, tau, g)
+    pieces = 2 if x.dtype == torch.bfloat16 and (len(x) <= 128 or x.numel() * len(w) <= 2 ** 29) else 1
+    got, want = _run(ops, x, w, index, logits, g, tau), mo.distillation(x, w, index, logits, tau, g, pieces)
     for name in NAMES:
         _check(name, got[name], *(t.cpu() for t in want[name]))
     return got
@@ -213,6 +214,32 @@ def test_gradients_are_those_of_the_definition(ops):
             value.append(float((mo.distillation(at["x"].double(), at["w"].double(), index, logits, 2.0)["loss"][0] * g.double()).sum()))
         slope, grad = (value[0] - value[1]) / (2 * h), dev[name].grad.double()
         assert abs(slope - float((grad * way).sum())) < 1e-4 * float(grad.norm() * way.norm()), name
+
+
+@pytest.mark.parametrize("weight", [1 + 2.0 ** -8, -3.5e-4, 1e-40, 2.4e38])
+def test_a_weight_of_all_rows_is_not_rounded(ops, weight):
+    """A student that knows nothing, a teacher sure of one word: every row's dl there is all but the weight itself.  The
+    weights' rounding to bf16 (up to 2^-8) would scale the gradients.  The gradients' own rounding is not counted: it may
+    scale them as well (a word of one row has dw = x (1 + 2^-8) where x has 8 digits: always rounded up, by up to 2^-9).
+    What else is rounded, to 2^-8 of itself at most, is so independently: along the gradient of n normal numbers that comes
+    to 2^-8 sqrt(3 / n) at most (rms), 5e-5 for dx, a twentieth of the 2^-10 allowed.  bf16 numbers are 2^-133 apart at
+    the least, so dl of 1e-40 is off by half of that, 0.46 of itself."""
+    rows, width, vocab = 300, 64, 40003
+    gen = torch.Generator().manual_seed(7)
+    x, w = _normal(gen, rows, width, dtype=torch.bfloat16, sigma=1e-2).cuda(), _normal(gen, vocab, width, dtype=torch.bfloat16).cuda()
+    index, logits = torch.randint(0, vocab, (rows, 1), generator=gen).cuda(), torch.zeros(rows, 1, device="cuda")
+    g = torch.full((rows,), weight, device="cuda")
+    if abs(weight) > 1e-30:
+        g[::3] *= 0.25                                   # as others have it but for a power of two
+    got, want = _run(ops, x, w, index, logits, g, 1.0), mo.distillation(x, w, index, logits, 1.0, g)
+    for name in ("dx", "dw"):
+        fits, unit = want[name][0].abs() < 3e38, abs(weight)     # (2.4e38 w is beyond what there is where w is above 1.4)
+        value, here = want[name][0][fits].to(torch.bfloat16).double(), got[name][fits].double()
+        if not value.any():                              # dw of 1e-40 x with x below 0.4
+            assert not here.any(), name
+            continue
+        scale = float((here / unit * (value / unit)).sum() / (value / unit).square().sum())
+        assert abs(scale - 1) < 2.0 ** -10 + 2.0 ** -134 / unit, (name, scale)
 
 
 def test_the_cross_entropy_keeps_its_results(ops):
