@@ -27,6 +27,7 @@
 // Slower: the compiler's own order of matrix instructions and reads (10 to 15 %, see spread()), 4 wavefronts of 256 x 256
 // (8 %), wavefronts of raised priority (no effect).
 #include "eager_distillation.h"
+#include "eager_gather.h"
 #include "eager_joined.h"
 #include "eager_launch.h"
 #include "eager_matrix.h"
@@ -590,22 +591,6 @@ __global__ __launch_bounds__(1024) void rows_kernel(const float2 *stats, const f
 // The rows that count in the backward pass - those with a target and a weight - side by side: the
 // products leave the others out, whatever stands in them.  Bound by one copy of x; 4096 x 1024 in bf16 7.4 us, and with
 // a tenth of the targets masked the products have a tenth less to do.
-struct Gather {
-    const void *x;
-    const long long *target;
-    const float *lse, *dloss;
-    long long rows, stride;
-    int width;
-    float by;                // of dloss
-    const int *before;       // per workgroup: counted rows in front of them, or NULL: each counts them
-    void *x_out;             // [counted][width]
-    long long *target_out;
-    float *lse_out, *dloss_out;
-    int *place;              // per row: where it went, -1: nowhere
-    int *counted;
-    float *common;           // the first weight with an exponent of 0, or NULL
-};
-
 __device__ __forceinline__ bool counts(const Gather &g, long long row) { return (g.target[row] >= 0) & (g.dloss[row] != 0.0f); }
 
 // kGathered rows a workgroup
@@ -628,33 +613,11 @@ __global__ __launch_bounds__(1024) void gather_kernel(const Gather g)
         if (!g.before)
             for (int w = 0; w < 16; ++w) before += sums[w];
         const long long row = first + lane;
-        const bool mine = lane < kGathered && row < g.rows, in = mine && counts(g, row);
-        const unsigned long long mask = __ballot(in);
-        const int to = in ? before + __popcll(mask & ((1ull << lane) - 1)) : -1;
-        if (lane < kGathered) place[lane] = to;
-        if (mine) g.place[row] = to;
-        if (in) {
-            g.target_out[to] = g.target[row];
-            g.lse_out[to] = g.lse[row];
-            const float weight = g.dloss[row] * g.by;
-            g.dloss_out[to] = weight;
-            if (g.common && to == 0) *g.common = __uint_as_float((__float_as_uint(weight) & 0x7fffff) | 0x3f800000);
-        }
-        if (lane == 0 && first + kGathered >= g.rows) {
-            *g.counted = before + __popcll(mask);
-            if (g.common && before == 0 && mask == 0) *g.common = 1.0f;
-        }
+        const bool mine = lane < kGathered && row < g.rows;
+        place_rows(g, first, before, mine ? g.target[row] : -1, place);
     }
     __syncthreads();
-    constexpr int E = 16 / sizeof(T);
-    const int chunks = g.width / E;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < kGathered * chunks; i += 1024) {
-        const int in = i / chunks, at = (i - in * chunks) * E;
-        if (place[in] >= 0)
-            *reinterpret_cast<f32x4 *>(static_cast<T *>(g.x_out) + static_cast<long long>(place[in]) * g.width + at) =
-                *reinterpret_cast<const f32x4 *>(static_cast<const T *>(g.x) + (first + in) * g.stride + at);
-    }
+    move_rows<T>(g, first, place);
 }
 
 // `before` of many rows, by one workgroup: 1024 times kGathered rows at a time
@@ -813,10 +776,11 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
     float *const common = form == kFactored ? reinterpret_cast<float *>(counted + 4) : nullptr;
     Sums of_dx = {}, of_dw = {};
     const float scale = taught ? kLog2e / a.teacher.temperature : kLog2e;
+    const bool few = taught && a.rows && a.rows <= kFewTaught;
     const long long *target = a.target;
     if (taught) {
         long long *const favourite = reinterpret_cast<long long *>(a.workspace + l.end);
-        if (a.rows) e = launch_favourites(a, favourite, stream);
+        if (a.rows && !few) e = launch_favourites(a, favourite, stream);
         target = favourite;
     }
     Gather g = {a.x, target, a.lse, a.dloss, a.rows, a.x_stride, a.width, taught ? 1.0f / a.teacher.temperature : 1.0f, nullptr, x,
@@ -828,7 +792,9 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
         g.before = before;
     }
     // (without rows one workgroup says that none count)
-    if (e == hipSuccess)
+    if (few)
+        e = launch_taught_rows(a, g, sizeof(T) == 2, stream);
+    else if (e == hipSuccess)
         e = launch(gather_kernel<T>, dim3(static_cast<unsigned>(std::max((a.rows + kGathered - 1) / kGathered, 1ll))), dim3(1024), 0,
                    stream, g);
     for (long long first = 0; e == hipSuccess && first < a.vocab; first += c.piece) {

@@ -1,6 +1,7 @@
 // What the projection's products (eager_cross_entropy.hip) ask of distillation's own kernels (eager_distillation.hip).
 #pragma once
 
+#include "eager_gather.h"
 #include "eager_model.h"
 
 namespace eager {
@@ -36,6 +37,9 @@ struct Tiled {
 hipError_t launch_picked(const CrossEntropyArgs &a, long long *favourite, bool bf16, hipStream_t stream);
 // The latter alone.
 hipError_t launch_favourites(const CrossEntropyArgs &a, long long *favourite, hipStream_t stream);
+// Of up to kFewTaught rows those that count, with the latter.
+constexpr long long kFewTaught = 64;
+hipError_t launch_taught_rows(const CrossEntropyArgs &a, const Gather &g, bool bf16, hipStream_t stream);
 // Losses and log-sum-exps; kept: the entries' logits too, from all logits, else launch_picked was before.
 hipError_t launch_divergence(const CrossEntropyArgs &a, const Tiled &t, bool kept, hipStream_t stream);
 // The entries' gradients of logits in place of those of words that no list has.

@@ -11,9 +11,9 @@
 //
 // Bound by the products (see there).  Measured, us, 4096 x 1024 x 50257 in bf16 with 64 entries a row: picked logits 39 (435 MB of
 // the projection's rows at 11 TB/s, most from second-level caches; 61 with fmaf for dot instructions and 64 lanes an entry), divergences 7, favourites 5,
-// entries of dl 12, beside 910 of logits, twice, and 830 of dx and dw; 1019 rows in fp32 with 32 entries 16.5, 6.5, 5 and 7.5 beside
-// 1305 and 1180; 300 x 512 x 3000 in bf16 with 128 entries entries of dl 8.2 (27
-// where every list was searched for repeated words with their shares) beside 22 and 10.
+// entries of dl 11.3, beside 910 of logits, twice, and 830 of dx and dw; 1019 rows in fp32 with 32 entries 16.5, 6.5, 5 and 7.1 beside
+// 1305 and 1180; 64 x 512 x 1000 in bf16 with 256 entries: entries of dl 5.7 (20.8 where every entry was compared with every
+// other of its row for repeated words), beside 22 and 7.
 //
 // dl beside bf16 inputs is bf16 itself, in two pieces for few rows (dlogits_pieces).  For more, what is rounded leaves out the
 // digits of the first row's weight, which the products' sums are multiplied by: a mean gives every row the same weight, and
@@ -35,6 +35,9 @@ namespace eager {
 namespace {
 
 constexpr int kEntries = 256;
+constexpr int kPlaceBits = 13, kPlaces = 1 << kPlaceBits;    // of a row's words, to find equal ones
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+static_assert(kPlaces / 32 == 4 * 64, "four words of bits a lane");
 
 __device__ __forceinline__ bool counts(long long index, float logit) { return (index >= 0) & (logit != -__builtin_inff()); }
 
@@ -161,6 +164,38 @@ __global__ __launch_bounds__(256) void favourites_kernel(const CrossEntropyArgs 
     }
 }
 
+// Favourites and rows that count in one launch, kGathered rows a workgroup, a wavefront each; all of them look at the lists of
+// the rows in front for whether these count.  The whole backward pass, us, beside two launches: 2 x 848 x 469 with 31 entries
+// 29.3 for 30.6, 17 x 512 x 3000 with 128 35.4 for 37.1, 61 x 1024 x 50257 with 16 123.4 both; 128 x 512 x 1000 with 64 alike and
+// with 256 56 for 51, so up to 64 rows.
+template <typename T, int N>
+__global__ __launch_bounds__(1024) void taught_rows_kernel(const CrossEntropyArgs a, const Gather g)
+{
+    __shared__ int sums[16], place[kGathered];
+    __shared__ long long words[kGathered];
+    static_assert(kGathered == 16, "a wavefront a row");
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long first = static_cast<long long>(blockIdx.x) * kGathered;
+    const long long word = List<N>(a.teacher, min(first + wave, a.rows - 1), lane).favourite(a.vocab, lane);
+    int before = 0;
+    for (long long row = wave; row < first; row += 16) {
+        const List<N> list(a.teacher, row, lane);
+        bool any = false;
+#pragma unroll
+        for (int j = 0; j < N; ++j) any |= list.used[j];
+        before += __any(any) && g.dloss[row] != 0.0f;
+    }
+    if (lane == 0) words[wave] = word, sums[wave] = before;
+    __syncthreads();
+    if (wave == 0) {
+        before = 0;
+        for (int w = 0; w < 16; ++w) before += sums[w];
+        place_rows(g, first, before, lane < kGathered ? words[lane] : -1, place);
+    }
+    __syncthreads();
+    move_rows<T>(g, first, place);
+}
+
 // kJoined rows a workgroup: their statistics, then a wavefront for each row's entries (whose loads come first).
 template <int N, bool Kept>
 __global__ __launch_bounds__(1024) void divergence_kernel(const CrossEntropyArgs a, const Tiled t)
@@ -226,9 +261,9 @@ template <typename T, int N>
 __global__ __launch_bounds__(1024) void entries_kernel(const CrossEntropyArgs a, const Entries n)
 {
     __shared__ float part[16][kJoined], apart[kJoined];
-    typedef int i32x4 __attribute__((ext_vector_type(4)));
-    __shared__ __align__(16) int words[kJoined][64 * N];
+    __shared__ int words[kJoined][64 * N];
     __shared__ float shares[kJoined][64 * N];
+    __shared__ __align__(16) unsigned seen[kJoined][kPlaces / 32];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long row = static_cast<long long>(blockIdx.x) * kJoined + wave, there = min(row, a.rows - 1);
     const int place = row < a.rows ? n.place[there] : -1;
@@ -259,32 +294,40 @@ __global__ __launch_bounds__(1024) void entries_kernel(const CrossEntropyArgs a,
     for (int j = 0; j < N; ++j) {
         q[j] /= sum;
         if (list.used[j] && list.index[j] != word) rest += q[j];
-        words[wave][64 * j + lane] = list.used[j] ? static_cast<int>(list.index[j]) : -1;
-        shares[wave][64 * j + lane] = q[j];
     }
     rest = lanes_sum<64>(rest);
+    // which entries find their word's bit set already; one of two equal words does, and few others
+    reinterpret_cast<u32x4 *>(seen[wave])[lane] = u32x4{};
     __builtin_amdgcn_wave_barrier();
-    bool first[N], several = false;
-    float share[N];
-    int same[N] = {};
-#pragma unroll 4
-    for (int i = 0; i < a.teacher.entries; i += 4) {
-        const i32x4 four = *reinterpret_cast<const i32x4 *>(&words[wave][i]);
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-#pragma unroll
-            for (int n = 0; n < 4; ++n) same[j] += four[n] == static_cast<int>(list.index[j]);
-    }
+    unsigned met[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-        several |= list.used[j] && same[j] > 1;
+        const unsigned at = static_cast<unsigned>(list.index[j]) * 0x9e3779b1u >> (32 - kPlaceBits);
+        met[j] = list.used[j] ? atomicOr(&seen[wave][at >> 5], 1u << (at & 31)) >> (at & 31) & 1 : 0;
+    }
+    bool first[N], several = false;
+    float share[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        for (unsigned long long left = __ballot(met[j]); left && !several; left &= left - 1) {
+            const int its = __builtin_amdgcn_readlane(static_cast<int>(list.index[j]), __builtin_ctzll(left));
+            int equal = 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i) equal += __popcll(__ballot(list.used[i] && static_cast<int>(list.index[i]) == its));
+            several |= equal > 1;
+        }
         first[j] = list.used[j] && list.index[j] >= n.first && list.index[j] < n.first + n.live;
         share[j] = q[j];
     }
     // a word that stands in several entries is written by the first of them, with all their shares
-    if (__any(several)) {
+    if (several) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) share[j] = 0.0f;
+        for (int j = 0; j < N; ++j) {
+            words[wave][64 * j + lane] = list.used[j] ? static_cast<int>(list.index[j]) : -1;
+            shares[wave][64 * j + lane] = q[j];
+            share[j] = 0.0f;
+        }
+        __builtin_amdgcn_wave_barrier();
         for (int i = 0; i < a.teacher.entries; ++i) {
             const int word_i = words[wave][i];
             const float share_i = shares[wave][i];
@@ -332,6 +375,14 @@ hipError_t launch_favourites(const CrossEntropyArgs &a, long long *favourite, hi
 {
     return by_entries(a.teacher.entries, [&](auto n) {
         return launch(favourites_kernel<n>, dim3(workgroups(a.rows, 4)), dim3(256), 0, stream, a, favourite);
+    });
+}
+
+hipError_t launch_taught_rows(const CrossEntropyArgs &a, const Gather &g, bool bf16, hipStream_t stream)
+{
+    return by_entries(a.teacher.entries, [&](auto n) {
+        return launch(bf16 ? taught_rows_kernel<__bf16, n> : taught_rows_kernel<float, n>,
+                      dim3(static_cast<unsigned>((a.rows + kGathered - 1) / kGathered)), dim3(1024), 0, stream, a, g);
     });
 }
 
