@@ -725,8 +725,8 @@ hipError_t launch_gradients(const Cut &c, const Product &dw, const Product &dx, 
 template <typename T>
 hipError_t forward(const CrossEntropyArgs &a, hipStream_t stream)
 {
-    const int shape = logits_shape(a.rows, a.width, a.vocab, sizeof(T));
     const bool taught = a.teacher.index;
+    const int shape = logits_shape(a.rows, a.width, a.vocab, sizeof(T), taught);
     const bool kept = taught && keeps_logits(a.rows, a.width, a.vocab, a.teacher.entries, sizeof(T));
     const long long own = taught ? teacher_bytes(a.rows, a.vocab, kept) : 0;
     // a teacher's favourite takes the target's place, or the logits are kept and the entries' taken from them
@@ -766,7 +766,7 @@ hipError_t backward(const CrossEntropyArgs &a, hipStream_t stream)
     constexpr bool Rounded = sizeof(T) == 2;
     const bool taught = a.teacher.index;
     const Form form = !taught || !Rounded ? kPlain : dlogits_pieces(a.rows, a.width, a.vocab, sizeof(T)) == 2 ? kTwice : kFactored;
-    const Cut c = cut_of(a.rows, a.width, a.vocab, sizeof(T), form == kTwice ? 2 : 1);
+    const Cut c = cut_of(a.rows, a.width, a.vocab, sizeof(T), taught, form == kTwice ? 2 : 1);
     const Layout l = layout_of(c, a.rows, a.width, sizeof(T));
     const long long low = l.end + teacher_target_bytes(a.rows) - l.dl;       // behind the favourites
     const T *w = static_cast<const T *>(a.w);

@@ -41,12 +41,15 @@ template <> inline Cost cost_of<Narrow>(int bytes) { return bytes == 2 ? Cost{0.
 template <typename Shape>
 double rounds_of(long long tiles) { return static_cast<double>((tiles + 256 * Shape::OfUnit - 1) / (256 * Shape::OfUnit)); }
 
+// Quarters of large tiles cost what they do behind full rounds; alone they are no better than whole ones, and distillation
+// counts them so (bf16, forward and backward, us, large and narrow: 2 x 848 x 469 45.1 and 40.7, 300 x 512 x 3000 61.3 and 57.5,
+// 2916 x 288 x 858 66.4 and 63.9).
 template <typename Shape>
-double logits_time(long long rows, int width, long long vocab, int bytes)
+double logits_time(long long rows, int width, long long vocab, int bytes, bool taught)
 {
     const Cost c = cost_of<Shape>(bytes);
     const long long tiles = round_up(rows, Shape::B) / Shape::B * (round_up(vocab, Shape::A) / Shape::A);
-    const long long last = Shape::Quartered ? tiles % kUnits : 0;
+    const long long last = Shape::Quartered && (tiles >= kUnits || !taught) ? tiles % kUnits : 0;
     const double rounds = last && last <= kUnits / 4 ? static_cast<double>(tiles / kUnits) + kQuarter : rounds_of<Shape>(tiles);
     return rounds * (round_up(width, 128 / bytes) / (128 / bytes) * c.step + c.rest);
 }
@@ -77,16 +80,16 @@ struct Cut {
     long long pieces;
 };
 
-inline int logits_shape(long long rows, int width, long long vocab, int bytes)
+inline int logits_shape(long long rows, int width, long long vocab, int bytes, bool taught = false)
 {
-    const double t[3] = {logits_time<Large>(rows, width, vocab, bytes), logits_time<Medium>(rows, width, vocab, bytes),
-                         logits_time<Narrow>(rows, width, vocab, bytes)};
+    const double t[3] = {logits_time<Large>(rows, width, vocab, bytes, taught), logits_time<Medium>(rows, width, vocab, bytes, taught),
+                         logits_time<Narrow>(rows, width, vocab, bytes, taught)};
     return static_cast<int>(std::min_element(t, t + 3) - t);
 }
 
 constexpr int kSides[3][2] = {{Large::A, Large::B}, {Medium::A, Medium::B}, {Narrow::A, Narrow::B}};
 
-inline Cut cut_of(long long rows, int width, int vocab, int bytes, int times = 1)
+inline Cut cut_of(long long rows, int width, int vocab, int bytes, bool taught = false, int times = 1)
 {
     const long long padded = round_up(std::max(rows, 1ll), 256);
     const long long fit = std::max(4096ll, (1ll << 29) / bytes / padded / 256 * 256);
@@ -99,9 +102,9 @@ inline Cut cut_of(long long rows, int width, int vocab, int bytes, int times = 1
     double least = 0;
     for (long long n = fewest; n < fewest + 6; ++n) {
         const long long piece = round_up((vocab + n - 1) / n, 256), pieces = (vocab + piece - 1) / piece;
-        const int shape = logits_shape(rows, width, piece, bytes);
-        const double logits = std::min({logits_time<Large>(rows, width, piece, bytes), logits_time<Medium>(rows, width, piece, bytes),
-                                        logits_time<Narrow>(rows, width, piece, bytes)});
+        const int shape = logits_shape(rows, width, piece, bytes, taught);
+        const double logits = std::min({logits_time<Large>(rows, width, piece, bytes, taught), logits_time<Medium>(rows, width, piece, bytes, taught),
+                                        logits_time<Narrow>(rows, width, piece, bytes, taught)});
         for (int dx = 1; dx <= most; dx *= 2)
             for (int dw = 1; dw <= (pieces > 1 ? 1 : 32); dw *= 2)
                 for (int g = dw > 1 ? kMedium : kLarge; g <= kMedium; ++g) {
@@ -200,7 +203,7 @@ inline long long distillation_workspace_bytes(long long rows, int width, int voc
         return teacher_bytes(rows, vocab, keeps_logits(rows, width, vocab, entries, bytes)) +
                cross_entropy_workspace_bytes(rows, width, vocab, bf16, false);
     const int pieces = dlogits_pieces(rows, width, vocab, bytes);
-    const Cut c = cut_of(rows, width, vocab, bytes, pieces);
+    const Cut c = cut_of(rows, width, vocab, bytes, true, pieces);
     return layout_of(c, rows, width, bytes).end + teacher_target_bytes(rows) + (pieces - 1) * c.rows_padded * c.piece * bytes;
 }
 

@@ -38,12 +38,12 @@ int main()
                             if (kept) CHECK(first >= rows * ((vocab + 3) / 4 * 4) * 4 && first % 256 == 0 && rows * vocab <= 1 << 26);
                             const int bytes = bf16 ? 2 : 4, pieces = backward ? dlogits_pieces(rows, width, vocab, bytes) : 1;
                             long long rest = cross_entropy_workspace_bytes(rows, width, vocab, bf16, backward);
-                            if (pieces == 2) {
+                            if (backward) {
                                 // second pieces behind all else, in the same order as the first ones
-                                const Cut c = cut_of(rows, width, vocab, bytes, 2);
+                                const Cut c = cut_of(rows, width, vocab, bytes, true, pieces);
                                 const Layout l = layout_of(c, rows, width, bytes);
-                                CHECK(bf16 && c.piece > 0 && l.others - l.dl >= c.rows_padded * c.piece * 2);
-                                rest = l.end + c.rows_padded * c.piece * 2;
+                                CHECK(c.piece > 0 && l.others - l.dl >= c.rows_padded * c.piece * bytes && (bf16 || pieces == 1));
+                                rest = l.end + (pieces - 1) * c.rows_padded * c.piece * 2;
                             }
                             CHECK(distillation_workspace_bytes(rows, width, vocab, entries, bf16, backward) == first + rest);
                         }

@@ -60,7 +60,7 @@ def _compare(ops, x, w, index, logits, g, tau):
     (40, 1024, 2000, 33, 1.0),       # few rows: narrow tiles, dx in slices
     (2100, 328, 4097, 12, 0.7),
     (2100, 328, 4097, 128, 0.7),     # the same with all logits in the workspace
-    (1500, 136, 13000, 256, 1.0), (1500, 64, 4097, 200, 3.0), (3000, 64, 4097, 256, 1.0), (100, 8, 50257, 2, 1.0),   # in other tiles
+    (1500, 136, 13000, 256, 1.0), (1500, 64, 4097, 200, 3.0), (3000, 64, 4097, 256, 1.0), (4100, 136, 4097, 256, 1.0), (100, 8, 50257, 2, 1.0),   # in other tiles
     (1500, 8, 13000, 2, 1.0), (1500, 136, 4097, 1, 1.0),
     (129, 1600, 4097, 1, 1.0), (2600, 1600, 130, 2, 1.0),            # gradients with the weights' factor: large tiles, slices
     (129, 136, 30001, 2, 2.0)])      # gradients in two pieces: large tiles
