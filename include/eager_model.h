@@ -173,7 +173,8 @@ typedef struct {
  * and stats[row] = m, stats[rows + row] = r, for the backward pass.  The norm is that of the s that is stored.
  * residual and sum may be NULL, both or none: s is x.  b may be NULL: none is added.  sum and y may each be x or
  * residual (with its stride), but not the same one.  A row of equal values has r = eps^(-1/2), with eps = 0 NaN in y.
- * Squares are formed in fp32: values up to 2^56 away from their mean do not overflow, below 2^-63 they lose digits.
+ * The mean that y is formed with is good to 47 bits; m is stored rounded to fp32, so the backward pass's n is off by up to
+ * 2^-24 |m| r.  Squares are formed in fp32: values up to 2^56 away from their mean do not overflow, below 2^-63 they lose digits.
  * Non-finite values stay in their row.
  * Errors: EINVAL (NULL, alignment, strides, sizes, eps negative or not finite), EDEVICE.
  *

@@ -153,20 +153,24 @@ def layer_norm(s, w, b, eps, dy=None, ds=None):
     rows, d = s.shape
     depth = min(d, ROW) + 2
     m = s.mean(1, keepdim=True)
-    m_err = depth * E * s.abs().mean(1, keepdim=True) + E * m.abs()
+    # the mean is formed in 64 bits, up to 42 roundings one after the other, and used to 48 bits; it is rounded once to fp32
+    # where it is stored, for the backward pass
+    m_err = 2.0 ** -47 * s.abs().mean(1, keepdim=True)
+    stored = m_err + E * m.abs()
     c = s - m
     var = c.square().mean(1, keepdim=True)
     r = (var + eps) ** -0.5
     # squares around a mean that is off by m_err are larger by its square; the root halves, and rounds itself
-    rel_r = ((depth + 4) * E * var + m_err.square() + 2 * E * m_err * c.abs().mean(1, keepdim=True)) * r.square() / 2 + 4 * E
+    rel_r = ((depth + 8) * E * var + m_err.square() + 2 * E * m_err * c.abs().mean(1, keepdim=True)) * r.square() / 2 + 4 * E
     n = c * r
-    n_err = (m_err + E * c.abs()) * r + n.abs() * (rel_r + 2 * E)
+    n_err = (m_err + 2 * E * c.abs()) * r + n.abs() * (rel_r + 2 * E)
     y = n * w + (0 if b is None else b.to(F))
     size = (n * w).abs() + (0 if b is None else b.to(F).abs())
-    out = {"y": (y, (w.abs() * n_err + 3 * E * size) * 1.01 + u * y.abs()), "mean": (m[:, 0], m_err[:, 0]),
+    out = {"y": (y, (w.abs() * n_err + 3 * E * size) * 1.01 + u * y.abs()), "mean": (m[:, 0], stored[:, 0] * 1.01),
            "r": (r[:, 0], (rel_r * r)[:, 0])}
     if dy is None:
         return out
+    n_err = (stored + E * (c.abs() + stored)) * r + n.abs() * (rel_r + 2 * E)
     dy = dy.to(F)
     dn = dy * w
     even, even_err = dn.mean(1, keepdim=True), (depth + 2) * E * dn.abs().mean(1, keepdim=True)

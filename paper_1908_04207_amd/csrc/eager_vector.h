@@ -64,6 +64,38 @@ __device__ __forceinline__ float lanes_sum(float x)
     return h.first + h.second;
 }
 
+// The same in 64 bits: both words of a number are moved.
+template <int Control>
+__device__ __forceinline__ double moved(double x)
+{
+    return __hiloint2double(__builtin_amdgcn_mov_dpp(__double2hiint(x), Control, 0xf, 0xf, false),
+                            __builtin_amdgcn_mov_dpp(__double2loint(x), Control, 0xf, 0xf, false));
+}
+__device__ __forceinline__ double rows_sum(double x)
+{
+    const auto h = __builtin_amdgcn_permlane16_swap(__double2hiint(x), __double2hiint(x), false, false);
+    const auto l = __builtin_amdgcn_permlane16_swap(__double2loint(x), __double2loint(x), false, false);
+    const unsigned h0 = h[0], h1 = h[1], l0 = l[0], l1 = l[1];
+    return __hiloint2double(h0, l0) + __hiloint2double(h1, l1);
+}
+__device__ __forceinline__ double halves_sum(double x)
+{
+    const auto h = __builtin_amdgcn_permlane32_swap(__double2hiint(x), __double2hiint(x), false, false);
+    const auto l = __builtin_amdgcn_permlane32_swap(__double2loint(x), __double2loint(x), false, false);
+    const unsigned h0 = h[0], h1 = h[1], l0 = l[0], l1 = l[1];
+    return __hiloint2double(h0, l0) + __hiloint2double(h1, l1);
+}
+template <int Lanes>
+__device__ __forceinline__ double lanes_sum(double x)
+{
+    static_assert(Lanes == 16 || Lanes == 64, "a row or a wavefront");
+    x += moved<0xb1>(x);
+    x += moved<0x4e>(x);
+    x += moved<0x141>(x);
+    x += moved<0x140>(x);
+    return Lanes == 16 ? x : halves_sum(rows_sum(x));
+}
+
 // The largest of a wavefront.
 __device__ __forceinline__ float wave_max(float x)
 {
