@@ -603,7 +603,8 @@ def distillation_backward(dloss, x, w, index, logits, lse, picked, temperature: 
 
 
 class Distillation(torch.autograd.Function):
-    """losses = Distillation.apply(x, w, index, logits, temperature)"""
+    """losses = Distillation.apply(x, w, index, logits, temperature); the teacher's logits are constants: a backward pass
+    through ones that require a gradient is refused"""
 
     @staticmethod
     def forward(ctx, x, w, index, logits, temperature):
@@ -614,6 +615,8 @@ class Distillation(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dloss):
+        if ctx.needs_input_grad[3]:
+            _refuse("Distillation: gradients of the teacher's logits are not formed; detach them")
         x, w, index, logits, lse, picked = ctx.saved_tensors
         if not any(ctx.needs_input_grad[:2]):
             return None, None, None, None, None
