@@ -531,7 +531,8 @@ def rotary_backward(dq_out, dk_out, cos, sin, positions, interleaved: bool = Fal
 
 
 class Rotary(torch.autograd.Function):
-    """q, k = Rotary.apply(q, k, cos, sin, positions, interleaved)"""
+    """q, k = Rotary.apply(q, k, cos, sin, positions, interleaved); the tables are constants: a backward pass through ones
+    that require a gradient is refused"""
 
     @staticmethod
     def forward(ctx, q, k, cos, sin, positions, interleaved):
@@ -541,6 +542,8 @@ class Rotary(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dq_out, dk_out):
+        if any(ctx.needs_input_grad[2:4]):
+            _refuse("Rotary: gradients of the tables are not formed; detach them")
         cos, sin, positions = ctx.saved_tensors
         grads = rotary_backward(_upstream(dq_out), _upstream(dk_out), cos, sin, positions, ctx.interleaved)
         return (*_once("Rotary", grads, dq_out, dk_out), None, None, None, None)

@@ -33,3 +33,30 @@ def test_a_teacher_out_of_the_graph(plain):                                     
     with torch.no_grad():
         loss = ops.Distillation.apply(x, w, index, logits, 2.0)
     assert not loss.requires_grad
+
+
+def _heads():
+    gen = torch.Generator().manual_seed(1)
+    q, k = torch.randn(5, 4, 8, generator=gen).requires_grad_(), torch.randn(5, 2, 8, generator=gen).requires_grad_()
+    angle = torch.randn(4, generator=gen)
+    return q, k, angle.cos(), angle.sin(), torch.arange(5, dtype=torch.int32)
+
+
+@pytest.mark.parametrize("which", [(2,), (3,), (2, 3)])
+@pytest.mark.parametrize("fixed", [False, True])
+def test_tables_that_are_trained_along_are_refused(plain, which, fixed):            # noqa: F811
+    args = list(_heads())
+    if fixed:
+        args[:2] = args[0].detach(), args[1].detach()
+    for n in which:
+        args[n].requires_grad_()
+    q, k = ops.Rotary.apply(*args, False)
+    with pytest.raises(eb.EagerError, match="tables") as e:
+        (q.sum() + k.sum()).backward()
+    assert e.value.status == eb.EINVAL and args[0].grad is None and args[2].grad is None
+
+
+def test_tables_out_of_the_graph(plain):                                            # noqa: F811
+    q, k, cos, sin, pos = _heads()
+    sum(t.sum() for t in ops.Rotary.apply(q, k, (cos.requires_grad_() * 1).detach(), sin, pos, False)).backward()
+    assert q.grad.any() and k.grad.any() and cos.grad is None
