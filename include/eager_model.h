@@ -260,7 +260,7 @@ typedef struct {
  *     loss[r] = sum_k q_k (log q_k - log p_{index_k}),  lse[r] = log sum_v exp(l_v / temperature),
  *     picked[r * entries + k] = l_{index_k}  (0 where the entry counts nothing)
  * A masked row has loss 0.  An index beyond the vocabulary gives loss and picked NaN.  The student's logits are
- * kept only while there are few of them (workspaces hold at most 256 MB of them).  The loss is not multiplied by the
+ * kept only while there are few of them (workspaces hold at most 256 MiB of them).  The loss is not multiplied by the
  * temperature's square; dloss may be.
  * Errors: EINVAL (NULL, alignment, strides, sizes, temperature, workspace too small), EDEVICE.
  *

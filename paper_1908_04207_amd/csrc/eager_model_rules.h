@@ -173,10 +173,10 @@ inline long long teacher_target_bytes(long long rows) { return round_up(rows * 8
 // in bf16 with 64 entries 118 and 46; 300 x 512 x 3000 with 128 20.8 and 17.0; one row x 1024 x 50257 with one 28.6 and
 // 25.8; 4096 x 1024 x 8192 with 64 109 and 99; 61 x 1024 x 50257 with 16 30.4 and 29.8; 4096 x 1024 x 50257 with 64 459 and
 // 637, 1019 rows 131 and 169; 4096 x 328 x 8000 in fp32 with 4 146 and 155.
-// 256 MB of logits are the most that are kept, as this operator is for logits that are not to be stored.
+// 256 MiB of logits, in rows of whole quads, are the most that are kept, as this operator is for logits that are not to be stored.
 inline bool keeps_logits(long long rows, int width, int vocab, int entries, int bytes)
 {
-    const double formed = 4 + static_cast<double>(rows) * entries * width * bytes / 12e6, kept = static_cast<double>(rows) * vocab;
+    const double formed = 4 + static_cast<double>(rows) * entries * width * bytes / 12e6, kept = static_cast<double>(rows) * round_up(vocab, 4);
     return kept <= 1 << 26 && kept * 4 / 4e6 < formed;
 }
 
