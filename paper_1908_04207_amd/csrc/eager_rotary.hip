@@ -33,6 +33,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, int pla
     constexpr int N = Interleaved ? V / 2 : V;              // pairs a place
     constexpr int Pieces = Interleaved ? 1 : 2;
     typedef float angles __attribute__((ext_vector_type(N)));
+    typedef angles placed __attribute__((aligned(N < 4 ? 4 * N : 16)));      // tables are on 16 bytes
     const int units = (a.groups[0] + a.groups[1]) * places;
     const int tokens = units < 256 ? 256 / units : 1;       // of a workgroup
     const int mine = units < 256 ? threadIdx.x / units : 0;
@@ -69,8 +70,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, int pla
             if (turns) {
                 const bool known = pos >= 0 && pos < a.table_rows;
                 const long long o = static_cast<long long>(known ? pos : 0) * a.half + place * N;
-                angles c = *reinterpret_cast<const angles *>(a.cos_table + o);
-                angles s = *reinterpret_cast<const angles *>(a.sin_table + o);
+                angles c = *reinterpret_cast<const placed *>(a.cos_table + o);
+                angles s = *reinterpret_cast<const placed *>(a.sin_table + o);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     c[i] = known ? c[i] : __builtin_nanf("");
