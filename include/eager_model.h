@@ -267,7 +267,9 @@ typedef struct {
  * Backward, for the upstream gradients dloss[r] (device, fp32), from lse and picked of the forward pass:
  *     dl_v = dloss[r] / temperature (p_v - sum of the q_k with index_k = v),  dx_r = sum_v dl_v w_v,
  *     dw_v = sum_r dl_v x_r
- * in pieces of the vocabulary, as eager_cross_entropy_backward (rows: at most 2^25).  Masked rows and rows with a dloss of zero are left
+ * in pieces of the vocabulary, as eager_cross_entropy_backward (rows: at most 2^25).  In bf16 dl is rounded as said above for
+ * more than 128 rows with rows * width * vocab beyond 2^29; up to there it is kept in two pieces, and dx and dw are as far off
+ * as their own rounding.  Masked rows and rows with a dloss of zero are left
  * out from the start.  The dl of the word that the teacher favours most is formed from the others' p and q where its
  * p is beyond a half, as long as one piece holds the vocabulary.  dx or dw may be NULL (not wanted).  p comes from lse and
  * is as far off as lse in fp32 is (2^-24 |lse|): a temperature so low that logits over it reach 10^4 leaves three digits.

@@ -210,7 +210,7 @@ __device__ __forceinline__ void product(const Product &p, int tile_a, int tile_b
 #pragma unroll
         for (int j = 0; j < NI; ++j) b[set][j] = read_side<T, BN, ColumnsB>(tile + BM * 128, wave_b + 32 * j, step, lane);
     };
-    // reads of shared memory a step, spread evenly over its matrix instructions
+    // of a step: reads of shared memory, among the first three quarters of its matrix instructions, and loads, among all (spread)
     constexpr int Reads = MI * (ColumnsA ? 2 : 1) + NI * (ColumnsB ? 2 : 1), Products = MI * NI;
     constexpr int Loads = (BM + BN) / 8 / Waves;
     auto body = [&](char *here, char *next, int t) {

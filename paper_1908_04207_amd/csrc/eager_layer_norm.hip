@@ -8,13 +8,13 @@
 // bits, and s - m with the mean's fp32 value and what that leaves: a row of one value gives zeros, and a row far from zero
 // what the same row next to zero gives.  (With the sum in fp32 1600 values around 1e4 of deviation one were 8e-4 off and a row of
 // 1234.567 had r = 315.99 for 316.23; the sum in 64 bits costs 65536 x 64 in bf16 9.2 us for 8.3, 8192 x 1024 12.9 for 12.4, fp32
-// rows nothing.)  Squares are summed in fp32.  The backward pass takes m, rounded to fp32, and r from the forward pass; its workgroups go through rows at equal steps and keep the sums of dw
-// and db in registers; the groups of a workgroup are added in shared memory in order, the workgroups by a second
-// kernel.
+// rows nothing.)  Squares are summed in fp32.  The backward pass takes m, rounded to fp32, and r from the forward pass; its
+// workgroups go through rows at equal steps and keep the sums of dw and db in registers; the groups of a workgroup are added
+// in shared memory in order, the workgroups by a second kernel.
 //
 // Bound by memory, every array once.  Measured (x, residual, s, y forward; dy, ds, s, dx backward): 20011 x 1600 fp32 (128 MB
-// an array) forward 102 us (5.0 TB/s), backward 97 and 4.5 for the sums over rows; 8192 x 1024 bf16 (17 MB, which the last
-// cache holds) 12.3, 14.6 and 3.1 us; 2047 x 8192 bf16 (x, y; dy, s, dx) 14.4, 21.5 and 4.9 us; 37 x 1024 forward 4.4 us, a launch.
+// an array) forward 91 us (5.6 TB/s), backward 107 and 4.9 for the sums over rows; 8192 x 1024 bf16 (17 MB, which the last
+// cache holds) 13.4, 13.5 and 3.8 us; 2047 x 8192 bf16 (x, y; dy, s, dx) 14.5, 19.8 and 4.0 us; 37 x 1024 forward 4.5 us, a launch.
 #include "eager_launch.h"
 #include "eager_model.h"
 #include "eager_model_rules.h"
@@ -309,6 +309,9 @@ hipError_t enqueue(const LayerNormArgs &a, bool backward, hipStream_t stream)
     hipError_t e = hipSuccess;
     if (a.blocks) e = launch(layer_norm_backward_kernel<T, Threads, C>, dim3(a.blocks), dim3(kBackwardBlock<Threads>), 0, stream, a);
     if (e != hipSuccess || (!a.dw && !a.db) || a.blocks == 1) return e;
+    // One column a thread or four: wide rows' records are more than a few loads of 4 bytes a thread bring, narrow ones leave too few
+    // workgroups of four.  Backward, bf16, us, one and four: 8192 x 264 9.4 and 9.7, 520 12.2 and 12.5, 1024 14.9 and 14.8, 1600 20.0
+    // and 20.0; 4096 x 2040 16.8 and 16.2, 2048 16.5 and 16.5, 3000 21.2 and 20.3; 2047 x 8192 27.6 and 24.7, 300 x 8192 20.7 and 16.6.
     if (a.width < 2048) return launch(layer_norm_columns_kernel<T, 1>, dim3((a.width + 15) / 16, a.db ? 2 : 1), dim3(1024), 0, stream, a);
     return launch(layer_norm_columns_kernel<T, 4>, dim3((a.width + 63) / 64, a.db ? 2 : 1), dim3(1024), 0, stream, a);
 }
@@ -318,6 +321,9 @@ hipError_t dispatch(const LayerNormArgs &a, bool backward, hipStream_t stream)
 {
     constexpr int C = 16 / kVector<T>;                      // 16 values a lane
     const int threads = layer_norm_threads(a.width);
+    // Half as many values a lane where they hold the row, so that no lane of 16 or 64 is without any at half the width.  Measured,
+    // 8 values and 16, forward and backward, us: 65536 x 64 bf16 7.8 and 8.2, 12.1 and 14.1, x 128 8.9 and 9.2, 14.8 and 15.9; 8192 x 264
+    // 5.5 and 5.7, 9.4 and 10.4, x 512 6.0 and 6.1, 10.2 and 11.2; 16384 x 512 fp32 12.6 and 12.7, 20.7 and 21.6.
     if (threads == 16)
         return a.width <= 128 ? enqueue<T, 16, C / 2>(a, backward, stream) : enqueue<T, 16, C>(a, backward, stream);
     if (threads == 64)

@@ -200,8 +200,9 @@ __device__ __forceinline__ f32x8 read_columns(const char *tile, int col0, int k0
 
 // Tells the compiler's scheduler to issue Reads reads of shared memory evenly among the first three quarters of the next
 // Products matrix instructions, so that the last ones arrive before the step after needs them, and Loads loads from
-// global memory among all.  Measured, reads among all of them and so, 4096 x 1024 x 50257 in bf16: logits 469 and 453 us, the backward
-// pass 1204 and 1199; among half 460 and 1221, a quarter 456 and 1229.
+// global memory among all.  Measured in turns, whole calls in bf16, reads among all of them, three quarters, half, a quarter:
+// 4096 x 1024 x 50257 forward 463, 450, 446, 447 us, backward 1236, 1226, 1251, 1262; 8191 x 1600 x 50257 1137, 1134, 1132, 1134
+// and 3661, 3671, 3740, 3814.
 template <int Products, int Reads, int Loads, int I = 0>
 __device__ __forceinline__ void spread()
 {

@@ -144,7 +144,8 @@ class Teacher:
 
     def loss(self, model, weights, tokens, targets, lens_cu, positions, cos, sin):
         """Divergences of a student of `model` and `weights`, times the temperature, which their gradients of logits are
-        divided by."""
+        divided by: these are p - q then, as a cross entropy's are, and get smaller with a higher temperature as p and q come
+        closer.  The temperature's square would hold their size instead; here that is left to the learning rate."""
         from . import model_ops as ops
         index, logits = self.lists(tokens, targets, lens_cu, positions, weights["head"].dtype)
         y = hidden_of(model, weights, tokens, lens_cu, positions, cos, sin)
